@@ -323,6 +323,39 @@ int32_t audiokv_decode_attend(const audiokv_params* params,
                               float* out_dev,
                               void* workspace, size_t workspace_bytes, void* stream);
 
+/* Accumulated attention weight of ALL queries (paper Sec. 4: one of the evictions
+ * compared there ranks tokens by it): what audiokv_score does for a window of a
+ * few dozen queries, for the queries of a whole prompt, or of one chunk of a
+ * chunked prefill. For KV head h of item i with Q_i queries, the last of which
+ * sits at position L_i - 1:
+ *   weights[h, j] += sum over query heads q of h's group and queries r of
+ *                    softmax_j(scale * <q[q, r], K[h, j]>),
+ * query r seeing keys j <= L_i - Q_i + r (params->causal = 1) or all of them.
+ * A query whose logits are all -infinity adds nothing.
+ *   q          bf16, packed: item i starts at element cu_queries[i] * n_q_heads
+ *              * head_dim and is [n_q_heads][Q_i][head_dim] (kv_layout 0) or
+ *              [Q_i][n_q_heads][head_dim] (kv_layout 1)
+ *   k          as everywhere (kv_layout or the explicit strides)
+ *   cu_queries_dev, queries_host   exclusive prefix sum (device) and the Q_i
+ *              (host), 0 <= Q_i <= L_i; the two must agree
+ *   lse_dev    NULL, or fp32, item i at cu_queries[i] * n_q_heads and
+ *              [n_q_heads][Q_i] there: natural log of each query's softmax
+ *              denominator, as a prefill's attention returns it; one pass over
+ *              the (query, key) pairs instead of two
+ *   weights    fp32, added to: clear it before a prompt's first chunk.
+ *              weights_pitch 0: packed like scores (what audiokv_select reads);
+ *              otherwise head (i, h) starts at (i * n_kv_heads + h) * pitch
+ *              (pitch >= every L_i), which stays where it is as a cache grows.
+ * params->window and the pooling are not used. Lengths L_i >= 1. */
+int32_t audiokv_accumulate_workspace_bytes(const audiokv_params* params, int32_t n_items, const int32_t* seqlens_host,
+                                           const int32_t* queries_host, size_t* out_bytes);
+int32_t audiokv_accumulate(const audiokv_params* params,
+                           const void* q, const void* k, const float* lse_dev,
+                           const int32_t* cu_seqlens_dev, const int32_t* seqlens_host,
+                           const int32_t* cu_queries_dev, const int32_t* queries_host, int32_t n_items,
+                           float* weights, int64_t weights_pitch,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement aid, not part of the method (used by the benchmark to time the
  * kernels of audiokv_evict where they run). While enabled, audiokv_evict records
  * HIP events on the caller's stream between its kernels; audiokv_profile_read

@@ -30,6 +30,13 @@ What it computes (paper: AudioKV, Sec. 3):
             head attends to the retained rows of its KV head only (plain
             scaled-dot-product attention over b_h rows; the definition itself).
 
+  accumulate     the attention weight that every token has received from ALL
+            queries of a prompt, or of its newest chunk (Sec. 4: one of the
+            compared evictions ranks tokens by it).
+  decode_weights  one decoding step with the weights of its rows.
+  evict_accumulated  which rows of a growing cache stay, and where, when it is
+            cut to a budget by recency and accumulated weight.
+
 The method is a heuristic pipeline rather than a fast route to a textbook
 quantity, so each function takes the steps in the paper's order, in float64
 (decode_attend alone has a plain definition, and is that definition).
@@ -419,6 +426,71 @@ def decode_attend(q: np.ndarray, k_rows: Sequence[np.ndarray], v_rows: Sequence[
         e = np.exp(z)
         out[j] = (e / e.sum()) @ V
     return out
+
+
+def accumulate(q: np.ndarray, k: np.ndarray, *, causal: bool = True, scale: Optional[float] = None) -> np.ndarray:
+    """Attention weight of every token, summed over all queries and over the query heads of its KV head's group.
+    q: [H_q, Q, d], the queries of the last Q of the L positions; k: [H_kv, L, d]. Query r sees tokens
+    j <= L - Q + r (causal) or all. A query whose logits are all -inf gives nothing. Returns [H_kv, L]."""
+    q = np.asarray(q, dtype=np.float64)
+    k = np.asarray(k, dtype=np.float64)
+    H_q, Q, d = q.shape
+    H_kv, L, _ = k.shape
+    G = H_q // H_kv
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    out = np.zeros((H_kv, L))
+    for j in range(H_q):
+        for r in range(Q):
+            seen = L - Q + r + 1 if causal else L
+            z = scale * (k[j // G, :seen] @ q[j, r])
+            top = z.max()
+            if top == -np.inf:
+                continue
+            e = np.exp(z - top)
+            out[j // G, :seen] += e / e.sum()
+    return out
+
+
+def decode_weights(q: np.ndarray, k_rows: Sequence[np.ndarray], v_rows: Sequence[np.ndarray], *,
+                   scale: Optional[float] = None) -> Tuple[np.ndarray, List[np.ndarray]]:
+    """decode_attend with what it weights its rows with: (out [H_q, d], per KV head the weight of each row summed over
+    the query heads of its group). A head without rows, or whose logits are all -inf, gives zeros."""
+    q = np.asarray(q, dtype=np.float64)
+    H_q, d = q.shape
+    G = H_q // len(k_rows)
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    out = np.zeros((H_q, d))
+    weights = [np.zeros(len(K)) for K in k_rows]
+    for j in range(H_q):
+        K, V = np.asarray(k_rows[j // G], dtype=np.float64), np.asarray(v_rows[j // G], dtype=np.float64)
+        z = scale * (K @ q[j])
+        if len(z) == 0 or z.max() == -np.inf:
+            continue
+        e = np.exp(z - z.max())
+        p = e / e.sum()
+        out[j] = p @ V
+        weights[j // G] += p
+    return out, weights
+
+
+def evict_accumulated(weights: np.ndarray, positions: np.ndarray, budget: int, recent: int) -> List[int]:
+    """One head's rows cut to a budget. Row t has accumulated weight weights[t] and stands at positions[t]. The first in
+    this order stay: rows at positions above newest - recent; then by weight, the largest first (NaN last); equal ones
+    by slot. Kept rows in slots from `budget` on take, in order, the slots below it that became free, in order.
+    Returns, for every slot that stays, the slot that its row comes from."""
+    n = len(weights)
+    if n <= budget:
+        return list(range(n))
+    newest = int(max(positions))
+
+    def rank(t):
+        if int(positions[t]) > newest - recent:
+            return (0, 0.0, t)
+        w = float(weights[t])
+        return (2, 0.0, t) if math.isnan(w) else (1, -w, t)
+    kept = set(sorted(range(n), key=rank)[:budget])
+    movers = iter(t for t in range(budget, n) if t in kept)
+    return [t if t in kept else next(movers) for t in range(budget)]
 
 
 # ---------------------------------------------------------------------------

@@ -110,12 +110,15 @@ def _load() -> C.CDLL:
                                           vp, vp, vp, vp, vp, vp]
     lib.audiokv_decode_workspace_bytes.argtypes = [pp, i32, i64, C.POINTER(C.c_size_t)]
     lib.audiokv_decode_attend.argtypes = [pp, vp, vp, vp, vp, i32, i64, vp, vp, C.c_size_t, vp]
+    lib.audiokv_accumulate_workspace_bytes.argtypes = [pp, i32, vp, vp, C.POINTER(C.c_size_t)]
+    lib.audiokv_accumulate.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, vp, C.c_size_t, vp]
     lib.audiokv_profile_enable.argtypes = [i32]
     lib.audiokv_profile_enable.restype = i32
     lib.audiokv_profile_read.argtypes = [C.POINTER(C.c_float)]
     lib.audiokv_profile_read.restype = i32
     for name in ("total_kept", "workspace_bytes", "score", "allocate", "smooth", "smooth_cutoffs", "select", "compact", "evict",
-                 "decode_workspace_bytes", "decode_attend", "score_lse", "evict_lse", "evict_noalloc"):
+                 "decode_workspace_bytes", "decode_attend", "score_lse", "evict_lse", "evict_noalloc",
+                 "accumulate_workspace_bytes", "accumulate"):
         getattr(lib, "audiokv_" + name).restype = i32
     return lib
 
@@ -394,6 +397,53 @@ def decode_attend(p: Params, q: torch.Tensor, k_cache: torch.Tensor, v_cache: to
     _check(_lib.audiokv_decode_attend(C.byref(cp), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(cu_budgets),
                                       int(n_items), int(total_rows), _ptr(out), _ptr(ws), ws.numel(), _stream()))
     return out
+
+
+def accumulate_workspace_bytes(p: Params, seqlens: Sequence[int], queries: Sequence[int]) -> int:
+    if len(queries) != len(seqlens):
+        raise ValueError(f"{len(queries)} numbers of queries for {len(seqlens)} lengths")
+
+    def compute():
+        out = C.c_size_t(0)
+        cp = p.c()
+        _check(_lib.audiokv_accumulate_workspace_bytes(C.byref(cp), len(seqlens), _host_lens(seqlens), _host_lens(queries),
+                                                       C.byref(out)))
+        return out.value
+    return _cached(("accumulate", p.key(), tuple(seqlens), tuple(queries)), compute)
+
+
+def accumulate(p: Params, q: torch.Tensor, k: torch.Tensor, seqlens: Sequence[int], queries: Sequence[int], *,
+               weights: Optional[torch.Tensor] = None, pitch: int = 0, lse: Optional[torch.Tensor] = None,
+               cu_seqlens: Optional[torch.Tensor] = None, cu_queries: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Adds the attention weight that every token receives from the last queries[i] positions of each item to `weights`
+    (fp32; zeros of the scores' layout if not given) and returns it. `pitch`: distance between heads of `weights`, 0:
+    packed like scores. `lse`: fp32, [n_q_heads][queries[i]] of item after item."""
+    _need(q, torch.bfloat16, "q"); _need(k, torch.bfloat16, "k")
+    if len(queries) != len(seqlens):
+        raise ValueError(f"{len(queries)} numbers of queries for {len(seqlens)} lengths")
+    dev = k.device
+    if q.numel() < sum(queries) * p.n_q_heads * p.head_dim:
+        raise ValueError("q is smaller than its queries")
+    cu = cu_seqlens if cu_seqlens is not None else _cu(seqlens, dev)
+    cu_q = cu_queries if cu_queries is not None else _cu(queries, dev)
+    total = (pitch * len(seqlens) if pitch else sum(int(x) for x in seqlens)) * p.n_kv_heads
+    if weights is None:
+        weights = torch.zeros(total, dtype=torch.float32, device=dev)
+    _need(weights, torch.float32, "weights")
+    if weights.numel() < total:
+        raise ValueError(f"weights has {weights.numel()} values, {total} needed")
+    if lse is not None:
+        _need(lse, torch.float32, "lse")
+        if lse.numel() < sum(queries) * p.n_q_heads:
+            raise ValueError("lse is smaller than its queries")
+    ws = workspace
+    if ws is None:
+        ws = torch.empty(max(accumulate_workspace_bytes(p, seqlens, queries), 256), dtype=torch.uint8, device=dev)
+    cp = p.c()
+    _check(_lib.audiokv_accumulate(C.byref(cp), _ptr(q), _ptr(k), _ptr(lse), _ptr(cu), _host_lens(seqlens), _ptr(cu_q),
+                                   _host_lens(queries), len(seqlens), _ptr(weights), int(pitch), _ptr(ws), ws.numel(), _stream()))
+    return weights
 
 
 PROFILE_STAGES = ("allocate", "score_sweep1", "score_sweep2", "pool_smooth", "select", "compact")

@@ -669,6 +669,63 @@ int32_t audiokv_decode_attend(const audiokv_params* params, const void* q_dev, c
     return AUDIOKV_OK;
 }
 
+// lengths and queries of a call that accumulates weights: window plays no part
+static int32_t check_queries(const audiokv_params* p, int32_t n_items, const int32_t* seqlens_host, const int32_t* queries_host,
+                             Geom* g, AccumPlan* plan)
+{
+    Batch b;
+    audiokv_params any_window = *p;
+    any_window.window = 0;
+    AUDIOKV_TRY(check_batch(&any_window, n_items, seqlens_host, &b));
+    if (!queries_host) return fail(AUDIOKV_E_INVALID_ARG, "queries_host is NULL");
+    for (int i = 0; i < n_items; ++i)
+        if (queries_host[i] < 0 || queries_host[i] > seqlens_host[i])
+            return fail(AUDIOKV_E_INVALID_ARG, "item %d: %d queries must lie in [0, length = %d]", i, queries_host[i], seqlens_host[i]);
+    *g = make_geom(p, n_items);
+    *plan = accumulate_plan(*g, seqlens_host, queries_host, n_items);
+    if (!accumulate_supported(*g, *plan))
+        return fail(AUDIOKV_E_UNSUPPORTED, "accumulate: too many (query, key) blocks for one call: split the batch");
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_accumulate_workspace_bytes(const audiokv_params* params, int32_t n_items, const int32_t* seqlens_host,
+                                           const int32_t* queries_host, size_t* out_bytes)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (!out_bytes) return fail(AUDIOKV_E_INVALID_ARG, "out_bytes is NULL");
+    if (n_items == 0) { *out_bytes = 0; return AUDIOKV_OK; }
+    Geom g;
+    AccumPlan plan;
+    AUDIOKV_TRY(check_queries(params, n_items, seqlens_host, queries_host, &g, &plan));
+    *out_bytes = accumulate_stats_bytes(plan) + accumulate_parts_bytes(g, plan);
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_accumulate(const audiokv_params* params, const void* q, const void* k, const float* lse_dev,
+                           const int32_t* cu_seqlens_dev, const int32_t* seqlens_host, const int32_t* cu_queries_dev,
+                           const int32_t* queries_host, int32_t n_items, float* weights, int64_t weights_pitch,
+                           void* workspace, size_t workspace_bytes, void* stream)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (n_items == 0) return AUDIOKV_OK;
+    Geom g;
+    AccumPlan plan;
+    AUDIOKV_TRY(check_queries(params, n_items, seqlens_host, queries_host, &g, &plan));
+    if (!q || !k || !cu_seqlens_dev || !cu_queries_dev || !weights || !workspace)
+        return fail(AUDIOKV_E_INVALID_ARG, "audiokv_accumulate: NULL pointer argument");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(workspace))
+        return fail(AUDIOKV_E_INVALID_ARG, "q, k and the workspace must be 16-byte aligned");
+    if (weights_pitch != 0 && weights_pitch < plan.max_L)
+        return fail(AUDIOKV_E_INVALID_ARG, "weights_pitch %lld < longest item %d", (long long)weights_pitch, plan.max_L);
+    const size_t need = (lse_dev ? 0 : accumulate_stats_bytes(plan)) + accumulate_parts_bytes(g, plan);
+    if (workspace_bytes < need)
+        return fail(AUDIOKV_E_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+    if (plan.max_Q == 0) return AUDIOKV_OK;           // no query anywhere: nothing to add
+    AUDIOKV_HIP(launch_accumulate(g, plan, q, k, cu_seqlens_dev, cu_queries_dev, lse_dev, weights, weights_pitch, workspace,
+                                  static_cast<hipStream_t>(stream)), "accumulate kernels");
+    return AUDIOKV_OK;
+}
+
 int32_t audiokv_profile_enable(int32_t enable)
 {
     if (enable && !g_prof.created) {

@@ -1,0 +1,254 @@
+"""Accumulated attention weight on the GPU against the float64 oracle, through the public entry point.
+
+Tolerance, relative to each weight (all its terms are positive), with u = 2^-24, the relative error of one fp32 rounding:
+a logit in base 2 is off by c (d/4) u A (at most d/4 roundings of partial sums that stay below A = max sum |q||k|) and by
+4 u X for the constants, the product and the difference (X: the largest logit or log-sum-exp); numerator and denominator
+both carry that. Sums add one rounding a term, at most L/16 + R/16 + 64 terms in a row (a lane takes every 32nd row or half
+of 32 keys); exp2 and log2 are good to 2^-21 together."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import audiokv_oracle as O
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def A():
+    import paper_2604_06694_amd as A
+    return A
+
+
+def bf16(x):
+    return torch.from_numpy(np.ascontiguousarray(x, dtype=np.float32)).to(torch.bfloat16)
+
+
+def f64(t):
+    return t.float().numpy().astype(np.float64)
+
+
+class Batch:
+    """Items of H_q / H_kv heads of d channels: bf16 values on the host (float64), tensors in the asked layout."""
+
+    def __init__(self, rng, H_q, H_kv, d, lens, queries, layout="head", k_scale=1.0, change=None):
+        self.H_q, self.H_kv, self.d, self.lens, self.queries, self.layout = H_q, H_kv, d, lens, queries, layout
+        self.k = [f64(bf16(k_scale * rng.standard_normal((H_kv, L, d)))) for L in lens]
+        self.q = [f64(bf16(rng.standard_normal((H_q, Q, d)))) for Q in queries]
+        if change:
+            change(self)
+            self.k, self.q = [f64(bf16(x)) for x in self.k], [f64(bf16(x)) for x in self.q]      # what the device is given
+
+    def tensors(self):
+        if self.layout == "slab":
+            T = max(self.lens) + 3
+            k = np.full((len(self.lens), self.H_kv, T, self.d), np.nan)          # rows past an item's end are never used
+            for i, x in enumerate(self.k):
+                k[i, :, :x.shape[1]] = x
+            q = [x.reshape(-1) for x in self.q]
+        elif self.layout == "token":
+            k = np.concatenate([x.transpose(1, 0, 2).reshape(-1) for x in self.k])
+            q = [x.transpose(1, 0, 2).reshape(-1) for x in self.q]
+        else:
+            k = np.concatenate([x.reshape(-1) for x in self.k])
+            q = [x.reshape(-1) for x in self.q]
+        q = np.concatenate(q + [np.zeros(8)])
+        return bf16(q).cuda(), bf16(k).reshape(-1).cuda()
+
+    def params(self, A, **more):
+        if self.layout == "slab":
+            T = max(self.lens) + 3
+            more |= dict(kv_stride_item=self.H_kv * T * self.d, kv_stride_head=T * self.d, kv_stride_tok=self.d)
+        return A.Params(self.H_q, self.H_kv, self.d, 0, kv_layout=1 if self.layout == "token" else 0, **more)
+
+    @property
+    def pitch(self):
+        return max(self.lens) + 3 if self.layout == "slab" else 0
+
+    def of(self, weights, i):
+        """Item i's weights [H_kv, L]."""
+        w, L = weights.cpu().numpy().astype(np.float64), self.lens[i]
+        if self.pitch:
+            return w.reshape(len(self.lens), self.H_kv, self.pitch)[i, :, :L]
+        at = sum(self.lens[:i]) * self.H_kv
+        return w[at:at + self.H_kv * L].reshape(self.H_kv, L)
+
+    def lse(self, causal=True, scale=None):
+        out = []
+        for q, k in zip(self.q, self.k):
+            for j in range(self.H_q):
+                for r in range(q.shape[1]):
+                    seen = k.shape[1] - q.shape[1] + r + 1 if causal else k.shape[1]
+                    z = (scale or self.d ** -0.5) * (k[j * self.H_kv // self.H_q, :seen] @ q[j, r])
+                    out.append(z.max() + np.log(np.exp(z - z.max()).sum()))
+        return torch.tensor(out + [0.0], dtype=torch.float32).cuda()
+
+    def bound(self, i, scale=None):
+        q, k, G = np.abs(self.q[i]), np.abs(self.k[i]), self.H_q // self.H_kv
+        q, k = np.where(np.isfinite(q), q, 0), np.where(np.isfinite(k), k, 0)
+        Q, L = q.shape[1], k.shape[1]
+        if Q == 0:
+            return 0.0
+        c = (scale or self.d ** -0.5) * 1.4426950408889634
+        a = max((q[j] @ k[j // G].T).max() for j in range(self.H_q))
+        x = c * max(np.abs(self.q[i][j] @ np.where(np.isfinite(self.k[i][j // G]), self.k[i][j // G], 0).T).max()
+                    for j in range(self.H_q)) + np.log2(L)
+        return 2 * 0.6932 * (c * self.d / 4 * U * a + 4 * U * x) + (L / 16 + G * Q / 16 + 64) * U + 2.0 ** -21
+
+    def check(self, A, weights, before=0.0, causal=True, scale=None):
+        for i in range(len(self.lens)):
+            want = O.accumulate(self.q[i], self.k[i], causal=causal, scale=scale) if self.queries[i] else 0 * self.k[i][..., 0]
+            got, tol = self.of(weights, i), self.bound(i, scale)
+            off = np.abs(got - before - want)
+            assert (off <= tol * want + 2 * U * (abs(before) + want) + 1e-30).all(), (i, off.max(), tol)
+
+
+def run(A, b, lse=None, weights=None, **params):
+    q, k = b.tensors()
+    out = A.accumulate(b.params(A, **params), q, k, b.lens, b.queries, pitch=b.pitch, lse=lse, weights=weights)
+    torch.cuda.synchronize()
+    return out
+
+
+@pytest.mark.parametrize("H_q,H_kv,d", [(28, 4, 128), (8, 2, 256), (8, 2, 64), (3, 3, 128), (32, 1, 64), (17, 1, 128)])
+@pytest.mark.parametrize("layout", ["head", "token", "slab"])
+def test_whole_prompts_and_chunks(A, H_q, H_kv, d, layout):
+    b = Batch(np.random.default_rng(d + H_q), H_q, H_kv, d, [1, 97, 260, 33], [1, 97, 5, 0], layout)
+    b.check(A, run(A, b))
+
+
+@pytest.mark.parametrize("L,Q", [(1, 1), (2, 1), (31, 31), (32, 32), (33, 33), (64, 63), (65, 1), (255, 2), (257, 257), (600, 600),
+                                 (1300, 1), (1300, 40), (5000, 3)])
+def test_lengths(A, L, Q):
+    b = Batch(np.random.default_rng(L * 7 + Q), 7, 1, 64, [L], [Q])
+    b.check(A, run(A, b))
+
+
+def test_many_ranges(A):
+    """Long enough that keys and rows are cut into several ranges each, and two row tiles a wave are not yet taken."""
+    b = Batch(np.random.default_rng(5), 14, 2, 64, [4500, 700], [150, 700])
+    b.check(A, run(A, b))
+
+
+def test_large_call_takes_two_row_tiles(A):
+    """The kernels of large calls, on sampled heads: 8 heads of 12000 x 12000 pairs."""
+    rng = np.random.default_rng(6)
+    L, d = 12000, 64
+    k, q = f64(bf16(rng.standard_normal((1, L, d)))), f64(bf16(rng.standard_normal((8, L, d))))
+    p = A.Params(8, 1, d, 0)
+    got = A.accumulate(p, bf16(q).reshape(-1).cuda(), bf16(k).reshape(-1).cuda(), [L], [L]).double().cpu()
+    kd, want = torch.from_numpy(k[0]).cuda(), torch.zeros(L, dtype=torch.float64, device="cuda")
+    for j in range(8):
+        z = (torch.from_numpy(q[j]).cuda() @ kd.T.contiguous()) * d ** -0.5
+        z.masked_fill_(torch.ones_like(z, dtype=torch.bool).triu_(1), -np.inf)
+        want += torch.softmax(z, dim=1).sum(0)
+    b = Batch.__new__(Batch)
+    b.H_q, b.H_kv, b.d, b.q, b.k = 8, 1, d, [q[:, ::97]], [k[:, ::89]]
+    tol = b.bound(0) + (L / 16 + 8 * L / 16) * U
+    off = (got - want.cpu()).abs()
+    assert (off <= tol * want.cpu()).all(), (off.max(), tol)
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("causal", [0, 1])
+def test_mask_scale_and_given_lse(A, given, causal):
+    b = Batch(np.random.default_rng(8), 6, 2, 128, [150, 90], [70, 90], "token")
+    scale = float(np.float32(0.21))
+    lse = b.lse(bool(causal), scale) if given else None
+    b.check(A, run(A, b, lse=lse, causal=causal, softmax_scale=scale), causal=bool(causal), scale=scale)
+
+
+def test_adds_to_what_is_there_and_leaves_the_padding(A):
+    b = Batch(np.random.default_rng(9), 4, 2, 64, [50, 40], [50, 0], "slab")
+    w = torch.full((2 * 2 * b.pitch,), 3.0, device="cuda")
+    assert run(A, b, weights=w) is w
+    b.check(A, w, before=3.0)
+    w = w.cpu().reshape(2, 2, b.pitch)
+    assert (w[0, :, 50:] == 3).all() and (w[1] == 3).all()
+
+
+def test_chunks_add_up_to_the_whole(A):
+    """A chunked prefill in a padded slab: the totals stay in place while the cache grows."""
+    b = Batch(np.random.default_rng(10), 8, 2, 128, [300], [300], "slab")
+    q, k = b.tensors()
+    p, w = b.params(A), torch.zeros(2 * b.pitch, device="cuda")
+    q = q[:8 * 300 * 128].view(8, 300, 128)
+    for begin, end in [(0, 100), (100, 101), (101, 300)]:
+        A.accumulate(p, q[:, begin:end].contiguous().view(-1), k, [end], [end - begin], weights=w, pitch=b.pitch)
+    b.check(A, w)
+
+
+def test_logits_far_from_the_first(A):
+    """Logits that rise by hundreds of octaves along the keys, and fall: the reference of a row has to follow."""
+    def steep(b):
+        for k in b.k:
+            k *= np.linspace(0.1, 12, k.shape[1])[None, :, None]
+        b.k[1] = b.k[1][:, ::-1].copy()
+        b.q = [4 * q for q in b.q]
+    b = Batch(np.random.default_rng(11), 2, 1, 64, [700, 700], [60, 60], change=steep)
+    b.check(A, run(A, b))
+
+
+def test_minus_infinity_gives_nothing(A):
+    """Tokens whose logits are -inf have no weight, wherever they stand; a query that sees nothing else adds nothing."""
+    def cut(b):
+        b.q[0][..., 0] = np.abs(b.q[0][..., 0]) + 1
+        b.k[0][:, :70, 0] = -np.inf                      # the first queries see only these
+        b.k[0][:, 130:140, 0] = -np.inf
+    b = Batch(np.random.default_rng(12), 4, 2, 64, [200], [200], change=cut)
+    w = run(A, b)
+    assert torch.isfinite(w).all()
+    b.check(A, w)
+    got = b.of(w, 0)
+    assert (got[:, :70] == 0).all() and (got[:, 130:140] == 0).all() and (got[:, 70:130] > 0).all()
+
+
+def test_a_given_lse_of_minus_infinity_gives_nothing(A):
+    b = Batch(np.random.default_rng(13), 2, 1, 64, [40], [40])
+    w = run(A, b, lse=torch.full((81,), -np.inf, device="cuda"))
+    assert (w == 0).all()
+
+
+def test_equal_calls_equal_bits_on_a_stream_and_in_a_graph(A):
+    b = Batch(np.random.default_rng(14), 14, 2, 128, [900, 333], [900, 20], "token")
+    q, k = b.tensors()
+    p = b.params(A)
+    cu, cu_q = (torch.tensor(np.concatenate([[0], np.cumsum(x)]), dtype=torch.int32, device="cuda") for x in (b.lens, b.queries))
+    first = A.accumulate(p, q, k, b.lens, b.queries)
+    ws = torch.empty(A.accumulate_workspace_bytes(p, b.lens, b.queries), dtype=torch.uint8, device="cuda")
+    other = torch.cuda.Stream()
+    w = torch.zeros_like(first)
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        A.accumulate(p, q, k, b.lens, b.queries, weights=w, cu_seqlens=cu, cu_queries=cu_q, workspace=ws)
+    torch.cuda.synchronize()
+    assert torch.equal(w, first)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        A.accumulate(p, q, k, b.lens, b.queries, weights=w, cu_seqlens=cu, cu_queries=cu_q, workspace=ws)
+    for _ in range(3):
+        w.zero_()
+        ws.fill_(255)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(w, first)
+
+
+def test_totals_feed_selection(A):
+    """Accumulated totals are laid out like scores: select and compact read them as they are."""
+    b = Batch(np.random.default_rng(15), 8, 2, 64, [120, 80], [120, 80])
+    q, k = b.tensors()
+    p = b.params(A)
+    w = A.accumulate(p, q, k, b.lens, b.queries)
+    budgets = torch.tensor([30, 40, 20, 10], dtype=torch.int32, device="cuda")
+    cu_b = torch.tensor([0, 30, 70, 90, 100], dtype=torch.int32, device="cuda")
+    p = A.Params(8, 2, 64, 8)
+    idx = A.select(p, w, budgets, cu_b, b.lens, 100)
+    kept, _ = A.compact(p, k, k, idx, cu_b, b.lens, 100)
+    idx, kept = idx.cpu().numpy(), kept.float().cpu().numpy()
+    for g in range(4):
+        i, h = divmod(g, 2)
+        rows = slice(int(cu_b[g]), int(cu_b[g + 1]))
+        assert np.array_equal(idx[rows], O.select(b.of(w, i)[h], int(budgets[g]), 8))
+        assert np.array_equal(kept[rows].astype(np.float64), b.k[i][h][idx[rows]])
