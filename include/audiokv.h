@@ -104,7 +104,8 @@ typedef struct audiokv_params {
      * moved as 16-byte vectors), kv_stride_tok >= head_dim, and kv_stride_item > 0 when n_items > 1. Rows of
      * different (item, head, token) must not overlap. This is how a padded prefill cache [B][H_kv][L_max][d]
      * (kv_stride_item = H_kv*L_max*d, kv_stride_head = L_max*d, kv_stride_tok = d) or a slice of a larger
-     * buffer is passed without a copy. Used by score, compact, evict (and their variants); q_win, the outputs
+     * buffer is passed without a copy. Used by score, compact, evict (and their variants), accumulate, and for the
+     * rows in audiokv_slots (a sequence is the item there); q_win, the outputs
      * and the compacted cache read by decode_attend are always packed. */
     int64_t  kv_stride_item;
     int64_t  kv_stride_head;
@@ -355,6 +356,61 @@ int32_t audiokv_accumulate(const audiokv_params* params,
                            const int32_t* cu_queries_dev, const int32_t* queries_host, int32_t n_items,
                            float* weights, int64_t weights_pitch,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows that sequences own and that grow: a cache of `capacity` slots per head
+ * (x, h), x a sequence and h a KV head, of which the first lengths[x * n_kv_heads
+ * + h] are in use. All pointers are device memory.
+ * k, v: bf16 [n_seqs][n_kv_heads][capacity][head_dim] (kv_layout 0),
+ * [n_seqs][capacity][n_kv_heads][head_dim] (kv_layout 1), or by the explicit
+ * strides of params with the sequence as the item. The order of the slots has no
+ * meaning beyond the tie-breaks below; positions say when a row was appended. */
+typedef struct audiokv_slots {
+    uint32_t size;           /* sizeof(audiokv_slots)                                        */
+    int32_t  capacity;       /* slots per head, >= 1                                         */
+    void    *k, *v;
+    int32_t *lengths;        /* [n_seqs * n_kv_heads]                                        */
+    float   *weights;        /* [n_seqs * n_kv_heads][capacity] accumulated weight, or NULL  */
+    int32_t *positions;      /* [n_seqs * n_kv_heads][capacity], or NULL                     */
+} audiokv_slots;
+
+/* One decoding step of n_seqs sequences that share compacted caches and own rows
+ * (paper Sec. 1 and Sec. 4.6: generation proceeds on the retained tokens; here for
+ * several continuations of one prompt, and for the rows that they add).
+ * Sequences cu_seqs[i] .. cu_seqs[i+1] - 1 continue item i (cu_seqs_dev: int32
+ * [n_items + 1], not falling, from 0); k_prompt / v_prompt / cu_budgets_dev /
+ * total_rows: the items' compacted cache, as for audiokv_decode_attend, read once
+ * for all sequences of an item. n_items = 0: no prompts (those pointers are not
+ * used), every sequence has its own rows only. slots NULL or max_own = 0: no own
+ * rows.
+ * In this order, for sequence x and KV head h:
+ *   append    (k_new, v_new not NULL; bf16 [n_seqs][n_kv_heads][head_dim]) the new
+ *             row goes to slot lengths[..], its weight starts at 0, its position
+ *             is pos_new_dev[x] (int32 [n_seqs]; needed where slots->positions is
+ *             given), and the length grows by one;
+ *   attend    out[x][q] = sum over the prompt's rows of h and the own rows of
+ *             softmax(scale * <q, K>) * V, for the queries q of h's group.
+ *             q_dev, out_dev: bf16 [n_seqs][n_q_heads][head_dim]. A query without
+ *             rows, or whose logits are all -infinity, gives zeros;
+ *   account   (slots->weights not NULL) every own row's weight grows by the sum of
+ *             what the group's queries gave it.
+ * max_own (host): no head has more own rows than this after the step, at most
+ * slots->capacity. Rows beyond it are not read, and a head that has max_own rows
+ * before the step appends none. max_seqs (host): no item has more sequences.
+ * Sequences from cu_seqs[n_items] on, and those of an item beyond max_seqs, take
+ * no part: their outputs, lengths and rows stay as they are, so that a batch of
+ * fixed size can be captured into a graph and filled by cu_seqs.
+ * Softmax statistics, weights and sums are fp32; each weight is rounded to bf16
+ * for its product with V, and out is bf16. n_q_heads / n_kv_heads <= 32.
+ * The workspace never shrinks as total_rows or max_own grow. */
+int32_t audiokv_decode_shared_workspace_bytes(const audiokv_params* params, int32_t n_items, int64_t total_rows,
+                                              int32_t n_seqs, int32_t max_seqs, int32_t max_own, size_t* out_bytes);
+int32_t audiokv_decode_shared(const audiokv_params* params, const void* q_dev,
+                              const void* k_prompt, const void* v_prompt, const int32_t* cu_budgets_dev,
+                              int32_t n_items, int64_t total_rows,
+                              const int32_t* cu_seqs_dev, int32_t n_seqs, int32_t max_seqs,
+                              const audiokv_slots* slots, int32_t max_own,
+                              const void* k_new, const void* v_new, const int32_t* pos_new_dev,
+                              void* out_dev, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Measurement aid, not part of the method (used by the benchmark to time the
  * kernels of audiokv_evict where they run). While enabled, audiokv_evict records

@@ -48,6 +48,18 @@ class _CParams(C.Structure):
     ]
 
 
+class _CSlots(C.Structure):
+    _fields_ = [
+        ("size", C.c_uint32),
+        ("capacity", C.c_int32),
+        ("k", C.c_void_p),
+        ("v", C.c_void_p),
+        ("lengths", C.c_void_p),
+        ("weights", C.c_void_p),
+        ("positions", C.c_void_p),
+    ]
+
+
 @dataclass
 class Params:
     n_q_heads: int
@@ -76,6 +88,33 @@ class Params:
                         self.pool_kernel, self.pool_mode, self.causal, self.kv_layout,
                         self.softmax_scale, self.floor_frac, self.cutoff_mode, self.taper_bins,
                         self.kv_stride_item, self.kv_stride_head, self.kv_stride_tok)
+
+
+@dataclass
+class Slots:
+    """Rows that sequences own: device tensors, see audiokv_slots. `weights` and `positions` may be missing."""
+    k: torch.Tensor                          # bf16, in the layout of Params with the sequence as the item
+    v: torch.Tensor
+    lengths: torch.Tensor                    # int32 [n_seqs * n_kv_heads]
+    capacity: int
+    weights: Optional[torch.Tensor] = None   # fp32 [n_seqs * n_kv_heads, capacity]
+    positions: Optional[torch.Tensor] = None # int32, the same
+
+    def c(self, p: Params, n_seqs: int) -> _CSlots:
+        """The C struct, after a look at types and sizes."""
+        heads = n_seqs * p.n_kv_heads
+        for name, t, dtype, n in (("lengths", self.lengths, torch.int32, heads),
+                                  ("weights", self.weights, torch.float32, heads * self.capacity),
+                                  ("positions", self.positions, torch.int32, heads * self.capacity)):
+            if t is not None and _need(t, dtype, "slots." + name).numel() < n:
+                raise ValueError(f"slots.{name} has {t.numel()} values, {n} needed")
+        for name, t in (("k", self.k), ("v", self.v)):
+            if not t.is_cuda or t.dtype != torch.bfloat16:
+                raise ValueError(f"slots.{name} must be a device tensor of dtype {torch.bfloat16}")
+            if p.kv_stride_tok == 0 and _need(t, torch.bfloat16, "slots." + name).numel() < heads * self.capacity * p.head_dim:
+                raise ValueError(f"slots.{name} has {t.numel()} values, {heads * self.capacity * p.head_dim} needed")
+        return _CSlots(C.sizeof(_CSlots), self.capacity, _ptr(self.k), _ptr(self.v), _ptr(self.lengths), _ptr(self.weights),
+                       _ptr(self.positions))
 
 
 def lib_path() -> str:
@@ -112,13 +151,16 @@ def _load() -> C.CDLL:
     lib.audiokv_decode_attend.argtypes = [pp, vp, vp, vp, vp, i32, i64, vp, vp, C.c_size_t, vp]
     lib.audiokv_accumulate_workspace_bytes.argtypes = [pp, i32, vp, vp, C.POINTER(C.c_size_t)]
     lib.audiokv_accumulate.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, i32, vp, i64, vp, C.c_size_t, vp]
+    lib.audiokv_decode_shared_workspace_bytes.argtypes = [pp, i32, i64, i32, i32, i32, C.POINTER(C.c_size_t)]
+    lib.audiokv_decode_shared.argtypes = [pp, vp, vp, vp, vp, i32, i64, vp, i32, i32, C.POINTER(_CSlots), i32, vp, vp, vp, vp, vp,
+                                          C.c_size_t, vp]
     lib.audiokv_profile_enable.argtypes = [i32]
     lib.audiokv_profile_enable.restype = i32
     lib.audiokv_profile_read.argtypes = [C.POINTER(C.c_float)]
     lib.audiokv_profile_read.restype = i32
     for name in ("total_kept", "workspace_bytes", "score", "allocate", "smooth", "smooth_cutoffs", "select", "compact", "evict",
                  "decode_workspace_bytes", "decode_attend", "score_lse", "evict_lse", "evict_noalloc",
-                 "accumulate_workspace_bytes", "accumulate"):
+                 "accumulate_workspace_bytes", "accumulate", "decode_shared_workspace_bytes", "decode_shared"):
         getattr(lib, "audiokv_" + name).restype = i32
     return lib
 
@@ -444,6 +486,55 @@ def accumulate(p: Params, q: torch.Tensor, k: torch.Tensor, seqlens: Sequence[in
     _check(_lib.audiokv_accumulate(C.byref(cp), _ptr(q), _ptr(k), _ptr(lse), _ptr(cu), _host_lens(seqlens), _ptr(cu_q),
                                    _host_lens(queries), len(seqlens), _ptr(weights), int(pitch), _ptr(ws), ws.numel(), _stream()))
     return weights
+
+
+def decode_shared_workspace_bytes(p: Params, n_items: int, total_rows: int, n_seqs: int, max_seqs: int, max_own: int) -> int:
+    out = C.c_size_t(0)
+    cp = p.c()
+    _check(_lib.audiokv_decode_shared_workspace_bytes(C.byref(cp), int(n_items), int(total_rows), int(n_seqs), int(max_seqs),
+                                                      int(max_own), C.byref(out)))
+    return out.value
+
+
+def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], v_prompt: Optional[torch.Tensor],
+                  cu_budgets: Optional[torch.Tensor], total_rows: int, cu_seqs: Optional[torch.Tensor], max_seqs: int, *,
+                  slots: Optional[Slots] = None, max_own: int = 0, k_new: Optional[torch.Tensor] = None,
+                  v_new: Optional[torch.Tensor] = None, pos_new: Optional[torch.Tensor] = None,
+                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One decoding step of q.shape[0] sequences (q: bf16 [n_seqs, n_q_heads, head_dim]) on the compacted caches that they
+    share (`k_prompt` None: on none) and the rows that they own; bf16 output of q's shape. Updates `slots` in place."""
+    _need(q, torch.bfloat16, "q")
+    dev, n_seqs = q.device, q.shape[0]
+    if q.numel() != n_seqs * p.n_q_heads * p.head_dim:
+        raise ValueError("q must be [n_seqs, n_q_heads, head_dim]")
+    n_items = 0
+    if k_prompt is not None:
+        _need(k_prompt, torch.bfloat16, "k_prompt"); _need(v_prompt, torch.bfloat16, "v_prompt")
+        _need(cu_budgets, torch.int32, "cu_budgets"); _need(cu_seqs, torch.int32, "cu_seqs")
+        n_items = cu_seqs.numel() - 1
+        if cu_budgets.numel() < n_items * p.n_kv_heads + 1:
+            raise ValueError(f"cu_budgets has {cu_budgets.numel()} values, {n_items * p.n_kv_heads + 1} needed")
+        if min(k_prompt.numel(), v_prompt.numel()) < total_rows * p.head_dim:
+            raise ValueError(f"k_prompt or v_prompt holds fewer than {total_rows} rows")
+    for name, t in (("k_new", k_new), ("v_new", v_new)):
+        if t is not None and _need(t, torch.bfloat16, name).numel() < n_seqs * p.n_kv_heads * p.head_dim:
+            raise ValueError(f"{name} must be [n_seqs, n_kv_heads, head_dim]")
+    if pos_new is not None and _need(pos_new, torch.int32, "pos_new").numel() < n_seqs:
+        raise ValueError("pos_new must have a value per sequence")
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
+    elif _need(out, torch.bfloat16, "out").numel() < q.numel():
+        raise ValueError("out is smaller than q")
+    ws = workspace
+    if ws is None:
+        ws = torch.empty(max(decode_shared_workspace_bytes(p, n_items, total_rows, n_seqs, max_seqs, max_own if slots else 0), 256),
+                         dtype=torch.uint8, device=dev)
+    cp = p.c()
+    cs = slots.c(p, n_seqs) if slots is not None else None
+    _check(_lib.audiokv_decode_shared(C.byref(cp), _ptr(q), _ptr(k_prompt), _ptr(v_prompt), _ptr(cu_budgets), n_items, int(total_rows),
+                                      _ptr(cu_seqs), n_seqs, int(max_seqs), C.byref(cs) if cs is not None else None, int(max_own),
+                                      _ptr(k_new), _ptr(v_new), _ptr(pos_new), _ptr(out), _ptr(ws), ws.numel(), _stream()))
+    return out
 
 
 PROFILE_STAGES = ("allocate", "score_sweep1", "score_sweep2", "pool_smooth", "select", "compact")

@@ -726,6 +726,103 @@ int32_t audiokv_accumulate(const audiokv_params* params, const void* q, const vo
     return AUDIOKV_OK;
 }
 
+// the rows that sequences own, as the entry points that read or write them take them
+static int32_t check_slots(const audiokv_params* p, const audiokv_slots* slots, int32_t n_seqs, int32_t max_own)
+{
+    if (slots->size != sizeof(audiokv_slots))
+        return fail(AUDIOKV_E_INVALID_ARG, "slots.size = %u, this library expects %zu", slots->size, sizeof(audiokv_slots));
+    if (!slots->k || !slots->v || !slots->lengths) return fail(AUDIOKV_E_INVALID_ARG, "slots: k, v or lengths is NULL");
+    if (!aligned16(slots->k) || !aligned16(slots->v)) return fail(AUDIOKV_E_INVALID_ARG, "slots: k and v must be 16-byte aligned");
+    if (slots->capacity < 1 || max_own < 0 || max_own > slots->capacity)
+        return fail(AUDIOKV_E_INVALID_ARG, "max_own %d must lie in [0, capacity = %d]", max_own, slots->capacity);
+    if (p->kv_stride_tok != 0 && n_seqs > 1 && p->kv_stride_item == 0)
+        return fail(AUDIOKV_E_INVALID_ARG, "explicit kv strides with %d sequences need kv_stride_item > 0", n_seqs);
+    return AUDIOKV_OK;
+}
+
+static int32_t plan_shared(const audiokv_params* p, int32_t n_items, int64_t total_rows, int32_t n_seqs, int32_t max_seqs,
+                           int32_t max_own, Geom* g, SharedPlan* plan)
+{
+    if (n_items < 0 || n_seqs < 1 || max_own < 0 || total_rows < 0 || total_rows > (int64_t)INT32_MAX)
+        return fail(AUDIOKV_E_INVALID_ARG, "n_items %d, n_seqs %d, max_own %d or total_rows %lld out of range", n_items, n_seqs, max_own,
+                    (long long)total_rows);
+    if (n_items > 0 && max_seqs < 1) return fail(AUDIOKV_E_INVALID_ARG, "max_seqs %d < 1", max_seqs);
+    if ((long long)n_items * p->n_kv_heads > (1 << 20) || (long long)n_seqs * p->n_q_heads > (1 << 22))
+        return fail(AUDIOKV_E_UNSUPPORTED, "too many heads in one call");
+    *g = make_geom(p, n_seqs);
+    *plan = shared_plan(*g, n_items, total_rows, n_seqs, max_seqs < n_seqs ? max_seqs : n_seqs, max_own);
+    if (!shared_supported(*g, *plan, n_seqs))
+        return fail(AUDIOKV_E_UNSUPPORTED, "decode_shared: %d query heads per KV head > 32, or more work than one launch holds", g->G);
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_decode_shared_workspace_bytes(const audiokv_params* params, int32_t n_items, int64_t total_rows, int32_t n_seqs,
+                                              int32_t max_seqs, int32_t max_own, size_t* out_bytes)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (!out_bytes) return fail(AUDIOKV_E_INVALID_ARG, "out_bytes is NULL");
+    if (n_seqs == 0) { *out_bytes = 0; return AUDIOKV_OK; }
+    Geom g;
+    SharedPlan plan;
+    AUDIOKV_TRY(plan_shared(params, n_items, total_rows, n_seqs, max_seqs, max_own, &g, &plan));
+    *out_bytes = plan.bytes;
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_decode_shared(const audiokv_params* params, const void* q_dev, const void* k_prompt, const void* v_prompt,
+                              const int32_t* cu_budgets_dev, int32_t n_items, int64_t total_rows, const int32_t* cu_seqs_dev,
+                              int32_t n_seqs, int32_t max_seqs, const audiokv_slots* slots, int32_t max_own, const void* k_new,
+                              const void* v_new, const int32_t* pos_new_dev, void* out_dev, void* workspace, size_t workspace_bytes,
+                              void* stream)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (n_seqs == 0) return AUDIOKV_OK;
+    if (!slots) max_own = 0;
+    Geom g;
+    SharedPlan plan;
+    AUDIOKV_TRY(plan_shared(params, n_items, total_rows, n_seqs, max_seqs, max_own, &g, &plan));
+    if (!q_dev || !out_dev || !workspace || (n_items > 0 && (!k_prompt || !v_prompt || !cu_budgets_dev || !cu_seqs_dev)))
+        return fail(AUDIOKV_E_INVALID_ARG, "audiokv_decode_shared: NULL pointer argument");
+    if (!aligned16(q_dev) || !aligned16(out_dev) || !aligned16(workspace) || (n_items > 0 && (!aligned16(k_prompt) || !aligned16(v_prompt))))
+        return fail(AUDIOKV_E_INVALID_ARG, "q, out, k_prompt, v_prompt and the workspace must be 16-byte aligned");
+    if (slots) AUDIOKV_TRY(check_slots(params, slots, n_seqs, max_own));
+    if ((k_new == nullptr) != (v_new == nullptr)) return fail(AUDIOKV_E_INVALID_ARG, "k_new and v_new come together");
+    if (k_new) {
+        if (!slots || max_own < 1) return fail(AUDIOKV_E_INVALID_ARG, "a new row needs slots and max_own >= 1");
+        if (!aligned16(k_new) || !aligned16(v_new)) return fail(AUDIOKV_E_INVALID_ARG, "k_new and v_new must be 16-byte aligned");
+        if (slots->positions && !pos_new_dev) return fail(AUDIOKV_E_INVALID_ARG, "slots have positions: pos_new is needed");
+    }
+    if (workspace_bytes < plan.bytes)
+        return fail(AUDIOKV_E_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", workspace_bytes, plan.bytes);
+    SharedCall c{};
+    c.q = q_dev;
+    if (n_items > 0) {
+        c.k_prompt = k_prompt;
+        c.v_prompt = v_prompt;
+        c.cu_budgets = cu_budgets_dev;
+        c.cu_seqs = cu_seqs_dev;
+        c.n_items = n_items;
+        c.total_rows = total_rows;
+    }
+    c.n_seqs = n_seqs;
+    c.max_seqs = max_seqs < n_seqs ? max_seqs : n_seqs;
+    if (slots && max_own > 0) {
+        c.k_own = slots->k;
+        c.v_own = slots->v;
+        c.lengths = slots->lengths;
+        c.positions = slots->positions;
+        c.weights = slots->weights;
+        c.capacity = slots->capacity;
+        c.max_own = max_own;
+        c.k_new = k_new;
+        c.v_new = v_new;
+        c.pos_new = pos_new_dev;
+    }
+    c.out = out_dev;
+    AUDIOKV_HIP(launch_shared(g, plan, c, workspace, static_cast<hipStream_t>(stream)), "decode_shared kernels");
+    return AUDIOKV_OK;
+}
+
 int32_t audiokv_profile_enable(int32_t enable)
 {
     if (enable && !g_prof.created) {

@@ -161,6 +161,34 @@ size_t accumulate_parts_bytes(const Geom& g, const AccumPlan& p);
 hipError_t launch_accumulate(const Geom& g, const AccumPlan& p, const void* q, const void* k, const int32_t* cu_seqlens,
                              const int32_t* cu_queries, const float* lse, float* weights, int64_t pitch, void* workspace, hipStream_t s);
 
+// one decoding step of sequences that share compacted caches (shared.hip)
+struct SharedPlan {
+    int log_r = 0, row_blocks = 0;             // prompts: rows of a chunk (a power of two), blocks of query rows
+    long long slots = 0;                       // of chunks: every head leaves at most one empty
+    int own_chunk = 0, own_chunks = 0;         // own rows: of a chunk, chunks of a head
+    int logit_pitch = 0;
+    size_t stats_p = 0, stats_o = 0, after = 0, part_p = 0, part_o = 0, logits = 0, bytes = 0;    // offsets in the workspace
+};
+struct SharedCall {
+    const void *q, *k_prompt, *v_prompt;
+    const int32_t* cu_budgets;
+    const int32_t* cu_seqs;
+    int n_items;
+    long long total_rows;
+    int n_seqs, max_seqs;
+    void *k_own, *v_own;
+    int32_t *lengths, *positions;
+    float* weights;
+    int capacity, max_own;
+    const void *k_new, *v_new;
+    const int32_t* pos_new;
+    void* out;
+};
+// n_items = 0: no prompts; max_own = 0: no own rows
+SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_seqs, int max_seqs, int max_own);
+bool shared_supported(const Geom& g, const SharedPlan& p, int n_seqs);
+hipError_t launch_shared(const Geom& g, const SharedPlan& p, const SharedCall& c, void* workspace, hipStream_t s);
+
 bool select_supported(int L);
 // whether launch_select can combine what smoothing left
 bool select_joins(int max_L);

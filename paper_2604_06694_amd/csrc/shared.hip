@@ -1,0 +1,558 @@
+// One decoding step of sequences that share compacted caches: sequence x continues item i, attends to the rows that the
+// eviction kept of i's prompt (packed, read once for all sequences of the item) and to rows of its own (slots of a growing
+// cache, to which the step appends one).
+//
+//   out[x, q] = softmax over both sets of rows (scale * <q, K>) V          weights[own row] += sum over the group's q of p
+//
+// The queries of an item's sequences that read one KV head, S * G of them, are the rows of a product with the prompt's keys; a
+// sequence's own rows meet its G queries only. Both are the same work for a workgroup of four waves: up to 128 query rows
+// against a chunk of rows of K and V. C = K Q^T on v_mfma_f32_32x32x16_bf16 leaves a lane with one query row (mfma_tile.h):
+// exponentials and their sum stay in the lane, and four keys at a time its weights, rounded to bf16, are already the operand
+// of O^T = V^T P^T, whose other operand the transposing LDS read fetches from V as it lies. Weights are rounded to bf16 (half a
+// step is 2^-8 of each at most) because V and the result are bf16; the sums that divide them are of the unrounded fp32 values.
+// 32 query rows a wave. Up to 64 rows the tile's keys are split over two (groups of) waves, joined at the end through LDS.
+// A row's exponentials are taken against a reference, the maximum of the first tile: where a later sum leaves the safe range,
+// accumulators and sum are rescaled (see score_impl.h; here the two halves of a wave share their row's reference, since the
+// product joins their keys).
+//
+// Up to a few dozen query rows the bound is HBM, above it the matrix pipe. What a workgroup costs beside that is latency: the
+// next tile is in flight, in registers, while one is worked on.
+//
+// Budgets, lengths and the sequences of an item are known on the device only. A chunk of prompt rows finds its head as in
+// decode.hip: chunk c of head g has slot floor(cu_b[g] / R) + g + c. A second kernel joins the chunks of a query in fixed order
+// and adds the own rows' weights from the logits that the first one left. No atomics.
+#include "mfma_tile.h"
+
+namespace audiokv {
+
+namespace {
+
+using namespace mfma_tile;
+
+constexpr int kTile = 64;                     // keys of a tile
+constexpr int kRowBlock = 32 * kWaves;        // query rows of a workgroup
+
+struct Shared {
+    Geom g;
+    const __bf16* q;
+    const __bf16 *kp, *vp;                    // prompts' rows
+    const int32_t* cu_b;
+    const int32_t* cu_seqs;
+    int n_items, total_rows, n_seqs, max_seqs;
+    int log_r, slots, slots_pad, row_blocks;  // prompt chunks; slots_pad: a multiple of 8, so that a chunk stays on one XCD
+    __bf16 *ko, *vo;                          // own rows
+    int32_t* lengths;
+    int32_t* positions;
+    float* weights;
+    int capacity, max_own, own_chunk, own_chunks;
+    const __bf16 *k_new, *v_new;
+    const int32_t* pos_new;
+    float *part_p, *part_o;                   // [slot][max_seqs * G][D], [own head][chunk][G][D]
+    float2 *stats_p, *stats_o;                // (reference, sum) of the same
+    float* logits;                            // [own head][G][logit_pitch], base 2
+    int logit_pitch;
+    int32_t* after;                           // [own head]: 2 * rows after the step + whether one was appended
+    __bf16* out;
+};
+
+__device__ __forceinline__ int head_start(const Shared& a, int g) { return min(a.cu_b[g], a.total_rows); }
+__device__ __forceinline__ int first_slot(const Shared& a, int g) { return (head_start(a, g) >> a.log_r) + g; }
+
+// The last of n entries of a rising table whose value is not past v (64 entries probed at a time, one per lane); the first is not.
+template <typename Value>
+__device__ __forceinline__ int last_at_or_before(int n, int v, Value value) {
+    int at = 0;
+    for (int span = n; span > 1;) {
+        const int step = (span + 63) >> 6, probe = at + (int)(threadIdx.x & 63) * step;
+        const bool before = probe < at + span && value(min(probe, n - 1)) <= v;
+        const int found = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
+        const int skip = found > 0 ? (found - 1) * step : 0;
+        at += skip;
+        span = min(step, span - skip);
+    }
+    return __builtin_amdgcn_readfirstlane(at);
+}
+
+// The item that sequence x continues, or -1: it takes no part. (Without prompts all take part, as item 0.)
+__device__ __forceinline__ int item_of(const Shared& a, int x) {
+    if (!a.cu_seqs) return 0;
+    if (x < a.cu_seqs[0] || x >= a.cu_seqs[a.n_items]) return -1;
+    const int i = last_at_or_before(a.n_items, x, [&](int e) { return a.cu_seqs[e]; });
+    return x - a.cu_seqs[i] < a.max_seqs ? i : -1;
+}
+
+// What a workgroup attends to
+struct Rows {
+    const __bf16 *k, *v;       // first row of the chunk
+    int64_t stride;            // elements between rows
+    int n;                     // rows of the chunk
+    int fresh;                 // row that is read from k_new / v_new and stored into k_dst / v_dst (-1: none)
+    const __bf16 *k_new, *v_new;
+    __bf16 *k_dst, *v_dst;
+    float* logits;             // of the chunk's first row and the group's first query, or nullptr
+};
+
+template <int D>
+__device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int first_seq, int h, int M, int r_first, float* part, float2* stats)
+{
+    constexpr int KK = D / 16, CT = D / 32, N = kPieces<D, kTile>;
+    __shared__ __attribute__((aligned(16))) __bf16 tile[2][2][kTile * D];     // [buffer][K, V]
+    __shared__ float2 joint[2][64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5, col = lane & 31;
+    const int G = a.g.G;
+    // waves over query rows, and over the two halves of a tile's keys
+    const int left = M - r_first, wq_n = left <= 32 ? 1 : left <= 64 ? 2 : 4;
+    const int wq = wave % wq_n, wk = wave / wq_n;
+    const bool works = wk < 2;
+    const int sub0 = wq_n == 4 ? 0 : wk, sub1 = wq_n == 4 ? kTile / 32 : wk + 1;
+
+    const int r = r_first + wq * 32 + col, rc = min(r, M - 1);
+    const __bf16* qsrc = a.q + ((int64_t)(first_seq + rc / G) * a.g.H_q + h * G + rc % G) * D + hf * 8;
+    bf16x8 qf[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qsrc + kk * 16);
+
+    const int chunk = piece_chunk<D>() * 8;
+    u32x4 kpiece[N], vpiece[N];
+    auto fetch = [&](int t) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int j = t + piece_row<D>(u);
+            const int64_t at = (int64_t)min(j, rows.n - 1) * rows.stride + chunk;
+            kpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.k_new + chunk : rows.k + at);
+            vpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.v_new + chunk : rows.v + at);
+        }
+    };
+    auto put = [&](int t, int buffer) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            const int j = t + piece_row<D>(u);
+            if (j == rows.fresh) {
+                *reinterpret_cast<u32x4*>(rows.k_dst + chunk) = kpiece[u];
+                *reinterpret_cast<u32x4*>(rows.v_dst + chunk) = vpiece[u];
+            }
+            // rows past the end have weight 0, but 0 times an infinity is NaN
+            vpiece[u] = j < rows.n ? vpiece[u] : u32x4{0, 0, 0, 0};
+        }
+        put_tile<D>(tile[buffer][0], kpiece);
+        put_tile<D>(tile[buffer][1], vpiece);
+    };
+
+    f32x16 acc[CT] = {};
+    float m = -INFINITY, l = 0.f;
+    // the transposing read: sixteen lanes take four keys x sixteen channels, each lane then holds a channel's four keys
+    const int tr_key = 4 * hf + ((lane & 15) >> 2), tr_chunk = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), tr_low = (lane & 1) * 4;
+    auto values = [&](const __bf16* v, int key0, int ct) {
+        const int row = key0 + tr_key;
+        const __bf16* at = v + row * D + slot_of(ct * 4 + tr_chunk, row) * 8 + tr_low;
+        typedef __attribute__((ext_vector_type(4))) short s16x4;
+        typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)const_cast<__bf16*>(at));
+    };
+
+    fetch(0);
+    put(0, 0);
+    __syncthreads();
+    for (int t = 0, at = 0; t < rows.n; t += kTile, at ^= 1) {
+        if (t + kTile < rows.n) fetch(t + kTile);
+        __builtin_amdgcn_sched_barrier(0);
+        if (works) {
+            for (int s = sub0; s < sub1; ++s) {
+                const int key0 = t + s * 32;
+                if (key0 >= rows.n) break;
+                f32x16 z = {};
+#pragma unroll
+                for (int kk = 0; kk < KK; ++kk)
+                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<D>(tile[at][0], s * 32 + col, kk, hf), qf[kk], z, 0, 0, 0);
+                if (key0 + 32 > rows.n) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) z[i] = key0 + key_of(i, hf) < rows.n ? z[i] : -INFINITY;
+                }
+                if (rows.logits && col < G) {
+                    float* dst = rows.logits + (int64_t)col * a.logit_pitch + key0 + 4 * hf;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *reinterpret_cast<f32x4*>(dst + 2 * i) =
+                            f32x4{z[i] * a.g.c_log2, z[i + 1] * a.g.c_log2, z[i + 2] * a.g.c_log2, z[i + 3] * a.g.c_log2};
+                }
+                float p[16], sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    p[i] = fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -m));
+                    sum += p[i];
+                }
+                const bool far = !(sum < 0x1p10f);
+                if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
+                    float top = z[0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
+                    top = fmaxf(top, __shfl_xor(top, 32, 64));
+                    const int theirs = __shfl_xor((int)far, 32, 64);       // (in front of the test: all lanes take part)
+                    const bool redo = far | (theirs != 0);
+                    const float ref = redo ? fmaxf(m, top * a.g.c_log2) : m, ref0 = ref == -INFINITY ? 0.f : ref;
+                    const float by = redo ? fast_exp2(m - ref0) : 1.f;
+                    sum = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        p[i] = fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -ref0));
+                        sum += p[i];
+                    }
+                    l *= by;
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[ct][i] *= by;
+                    m = ref;
+                }
+                l += sum;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) {
+                    bf16x8 pf;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) pf[e] = (__bf16)p[kb * 8 + e];
+#pragma unroll
+                    for (int ct = 0; ct < CT; ++ct) {
+                        typedef __attribute__((ext_vector_type(4))) short s16x4;
+                        typedef __attribute__((ext_vector_type(8))) short s16x8;
+                        const s16x4 lo = values(tile[at][1], s * 32 + kb * 16, ct), hi = values(tile[at][1], s * 32 + kb * 16 + 8, ct);
+                        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                        acc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), pf, acc[ct], 0, 0, 0);
+                    }
+                }
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + kTile < rows.n) put(t + kTile, at ^ 1);
+        __syncthreads();
+    }
+
+    l += __shfl_xor(l, 32, 64);
+    if (wq_n < 4) {                                           // uniform: the second half of the keys joins the first
+        f32x4* xch = reinterpret_cast<f32x4*>(&tile[0][0][0]) + wq * (CT * 4 * 64) + lane;
+        if (wk == 1) {
+            joint[wq][lane] = make_float2(m, l);
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    xch[(ct * 4 + i / 4) * 64] = f32x4{acc[ct][i], acc[ct][i + 1], acc[ct][i + 2], acc[ct][i + 3]};
+        }
+        __syncthreads();
+        if (wk == 0) {
+            const float2 o = joint[wq][lane];
+            const float M2 = fmaxf(m, o.x), ref = M2 == -INFINITY ? 0.f : M2;
+            const float mine = fast_exp2(m - ref), other = fast_exp2(o.x - ref);
+            l = l * mine + o.y * other;
+            m = M2;
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const f32x4 v = xch[(ct * 4 + i / 4) * 64];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[ct][i + e] = acc[ct][i + e] * mine + v[e] * other;
+                }
+        }
+    }
+    if (wk == 0 && r < M) {
+        float* dst = part + (int64_t)r * D + 4 * hf;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                *reinterpret_cast<f32x4*>(dst + ct * 32 + 2 * i) = f32x4{acc[ct][i], acc[ct][i + 1], acc[ct][i + 2], acc[ct][i + 3]};
+        if (hf == 0) stats[r] = make_float2(m, l);
+    }
+}
+
+template <int D>
+__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void shared_partial_kernel(Shared a)
+{
+    const int prompt_blocks = a.slots_pad * a.row_blocks;
+    Rows rows{};
+    rows.fresh = -1;
+    int first_seq, h, M, r_first = 0;
+    float* part;
+    float2* stats;
+    if ((int)blockIdx.x < prompt_blocks) {
+        const int block = blockIdx.x / a.slots_pad, slot = blockIdx.x - block * a.slots_pad;
+        if (slot >= a.slots) return;
+        const int head = last_at_or_before(a.n_items * a.g.H_kv, slot, [&](int e) { return first_slot(a, e); });
+        const int item = head / a.g.H_kv;
+        h = head - item * a.g.H_kv;
+        const int c = slot - first_slot(a, head);
+        const int64_t row0 = head_start(a, head) + ((int64_t)c << a.log_r);
+        rows.n = (int)min((int64_t)1 << a.log_r, head_start(a, head + 1) - row0);
+        first_seq = max(0, a.cu_seqs[item]);
+        M = min(min(a.cu_seqs[item + 1], a.n_seqs) - first_seq, a.max_seqs) * a.g.G;
+        r_first = block * kRowBlock;
+        if (c < 0 || rows.n <= 0 || r_first >= M) return;
+        rows.k = a.kp + row0 * D;
+        rows.v = a.vp + row0 * D;
+        rows.stride = D;
+        const int64_t base = (int64_t)slot * a.max_seqs * a.g.G;
+        part = a.part_p + base * D;
+        stats = a.stats_p + base;
+    } else {
+        const int id = blockIdx.x - prompt_blocks, own = id / a.own_chunks, c = id - own * a.own_chunks;
+        const int x = own / a.g.H_kv;
+        h = own - x * a.g.H_kv;
+        if (item_of(a, x) < 0) return;
+        const int before = max(0, min(a.lengths[own], a.max_own));
+        const bool appends = a.k_new != nullptr && before < a.max_own;
+        const int n = before + appends, j0 = c * a.own_chunk;
+        if (c == 0 && threadIdx.x == 0) a.after[own] = 2 * n + appends;
+        rows.n = min(a.own_chunk, n - j0);
+        if (rows.n <= 0) return;
+        first_seq = x;
+        M = a.g.G;
+        const int64_t at = kv_row_offset(a.g, x, (int64_t)x * a.capacity, a.capacity, h, j0);
+        rows.k = a.ko + at;
+        rows.v = a.vo + at;
+        rows.stride = kv_tok_stride(a.g);
+        if (appends && before >= j0 && before < j0 + a.own_chunk) {
+            rows.fresh = before - j0;
+            rows.k_new = a.k_new + (int64_t)own * D;
+            rows.v_new = a.v_new + (int64_t)own * D;
+            rows.k_dst = a.ko + at + rows.fresh * rows.stride;
+            rows.v_dst = a.vo + at + rows.fresh * rows.stride;
+        }
+        const int64_t base = ((int64_t)own * a.own_chunks + c) * a.g.G;
+        part = a.part_o + base * D;
+        stats = a.stats_o + base;
+        if (a.weights) rows.logits = a.logits + (int64_t)own * a.g.G * a.logit_pitch + j0;
+    }
+    attend<D>(a, rows, first_seq, h, M, r_first, part, stats);
+}
+
+// The chunks that a query of sequence x has rows in: first those of the prompt, then its own
+struct Chunks {
+    const float2 *sp, *so;     // statistics of the first of each, and the distance from chunk to chunk
+    int64_t step_p, step_o;
+    int np, no;
+    __device__ __forceinline__ float2 stat(int c) const { return c < np ? sp[c * step_p] : so[(c - np) * step_o]; }
+};
+__device__ __forceinline__ Chunks chunks_of(const Shared& a, int x, int item, int h, int gq) {
+    Chunks t{a.stats_p, a.stats_o, 0, 0, 0, 0};
+    if (a.cu_seqs) {
+        const int head = item * a.g.H_kv + h, n = head_start(a, head + 1) - head_start(a, head);
+        t.np = n > 0 ? (n + (1 << a.log_r) - 1) >> a.log_r : 0;
+        t.step_p = (int64_t)a.max_seqs * a.g.G;
+        t.sp = a.stats_p + first_slot(a, head) * t.step_p + (int64_t)(x - a.cu_seqs[item]) * a.g.G + gq;
+    }
+    if (a.own_chunks > 0) {
+        const int own = x * a.g.H_kv + h, n = a.after[own] >> 1;
+        t.no = (n + a.own_chunk - 1) / a.own_chunk;
+        t.step_o = a.g.G;
+        t.so = a.stats_o + (int64_t)own * a.own_chunks * a.g.G + gq;
+    }
+    return t;
+}
+
+// A workgroup per query: its chunks joined. Behind those, workgroups of 256 own rows each add the rows' weights.
+constexpr int kJoinLds = 1024;                // chunks whose factors fit the LDS array (more: recomputed where used)
+
+__global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int weight_blocks)
+{
+    __shared__ float factor[kJoinLds];
+    __shared__ float wave_m[kWaves], wave_l[kWaves];
+    __shared__ __attribute__((aligned(16))) f32x4 red[kThreads];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, G = a.g.G, D = a.g.D;
+    const int queries = a.n_seqs * a.g.H_q;
+    if ((int)blockIdx.x >= queries) {
+        const int id = blockIdx.x - queries, own = id / weight_blocks, j = (id - own * weight_blocks) * kThreads + tid;
+        const int x = own / a.g.H_kv, h = own - x * a.g.H_kv, item = item_of(a, x);
+        if (item < 0) return;
+        const int after = a.after[own], n = after >> 1;
+        if (j - tid >= n) return;
+        // max + log2(sum) of the group's queries, a wave on every fourth
+        for (int gq = wave; gq < G; gq += kWaves) {
+            const Chunks t = chunks_of(a, x, item, h, gq);
+            float m = -INFINITY, l = 0.f;
+            for (int c = lane; c < t.np + t.no; c += 64) {
+                const float2 s = t.stat(c);
+                const float m2 = fmaxf(m, s.x), ref = m2 == -INFINITY ? 0.f : m2;
+                l = l * fast_exp2(m - ref) + s.y * fast_exp2(s.x - ref);
+                m = m2;
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) {
+                const float mo = __shfl_xor(m, o, 64), lo = __shfl_xor(l, o, 64);
+                const float m2 = fmaxf(m, mo), ref = m2 == -INFINITY ? 0.f : m2;
+                // (the same order in both lanes: the sum of a pair is theirs alike)
+                const float a0 = l * fast_exp2(m - ref), a1 = lo * fast_exp2(mo - ref);
+                l = a0 + a1;
+                m = m2;
+            }
+            if (lane == 0) factor[gq] = l == 0.f ? INFINITY : m + __log2f(l);
+        }
+        __syncthreads();
+        if (j >= n) return;
+        const float* z = a.logits + (int64_t)own * G * a.logit_pitch + j;
+        float w = 0.f;
+#pragma unroll 8
+        for (int gq = 0; gq < G; ++gq) w += fast_exp2(z[(int64_t)gq * a.logit_pitch] - factor[gq]);
+        float* dst = a.weights + (int64_t)own * a.capacity + j;
+        *dst = (after & 1) && j == n - 1 ? w : *dst + w;      // the appended row begins at nothing
+        return;
+    }
+    const int x = blockIdx.x / a.g.H_q, hq = blockIdx.x - x * a.g.H_q, h = hq / G, gq = hq - h * G, item = item_of(a, x);
+    if (item < 0) return;
+    const Chunks t = chunks_of(a, x, item, h, gq);
+    if (gq == 0 && a.own_chunks > 0 && tid == 0) {
+        const int own = x * a.g.H_kv + h, after = a.after[own];
+        if (after & 1) {
+            a.lengths[own] = after >> 1;
+            if (a.positions) a.positions[(int64_t)own * a.capacity + (after >> 1) - 1] = a.pos_new[x];
+        }
+    }
+    const int nc = t.np + t.no;
+    float m = -INFINITY, l = 0.f;
+    for (int c = tid; c < nc; c += kThreads) {
+        const float2 s = t.stat(c);
+        if (c < kJoinLds) factor[c] = s.x;
+        const float m2 = fmaxf(m, s.x), ref = m2 == -INFINITY ? 0.f : m2;
+        l = l * fast_exp2(m - ref) + s.y * fast_exp2(s.x - ref);
+        m = m2;
+    }
+    float M = m;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+    if (lane == 0) wave_m[wave] = M;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, wave_m[w]);
+    const float ref = M == -INFINITY ? 0.f : M;
+    l *= fast_exp2(m - ref);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+    if (lane == 0) wave_l[wave] = l;
+    for (int c = tid; c < min(nc, kJoinLds); c += kThreads) factor[c] = fast_exp2(factor[c] - ref);
+    __syncthreads();
+    const float den = ((wave_l[0] + wave_l[1]) + wave_l[2]) + wave_l[3];
+
+    const int quads = D >> 2, groups = kThreads / quads, ch = tid % quads, grp = tid / quads;
+    const f32x4* pp = reinterpret_cast<const f32x4*>(a.part_p + (t.sp - a.stats_p) * D) + ch;
+    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + (t.so - a.stats_o) * D) + ch;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int c = grp; c < nc; c += groups) {
+        const float f = c < kJoinLds ? factor[c] : fast_exp2(t.stat(c).x - ref);
+        acc += (c < t.np ? pp[c * t.step_p * quads] : po[(c - t.np) * t.step_o * quads]) * f;
+    }
+    red[tid] = acc;
+    __syncthreads();
+    if (grp == 0) {
+        f32x4 num = acc;
+        for (int k = 1; k < groups; ++k) num += red[k * quads + ch];
+        bf16x4 o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);     // no row, or nothing but -inf: zeros
+        *reinterpret_cast<bf16x4*>(a.out + ((int64_t)x * a.g.H_q + hq) * D + ch * 4) = o;
+    }
+}
+
+inline size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+
+}  // namespace
+
+// How a call is cut. Pure function of its sizes, so that the workspace query and the launch agree. The workspace never shrinks as
+// total_rows or max_own grow: one that is sized for the largest step serves the smaller ones.
+SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_seqs, int max_seqs, int max_own)
+{
+    SharedPlan p;
+    long long slots = 0, chunks = 0;            // what the workspace is charged
+    if (n_items > 0) {
+        p.row_blocks = (int)(((long long)max_seqs * g.G + kRowBlock - 1) / kRowBlock);
+        const long long wanted = (512 + p.row_blocks - 1) / p.row_blocks;     // chunks: two workgroups per CU
+        p.log_r = 7;
+        while (p.log_r < 16 && (total_rows >> (p.log_r + 1)) >= wanted) ++p.log_r;
+        p.slots = (total_rows >> p.log_r) + (long long)n_items * g.H_kv;
+        slots = p.slots;                        // where the chunks double, the slots halve
+        if (p.log_r > 7 && (total_rows >> p.log_r) < 2 * wanted - 1) slots = 2 * wanted - 1 + (long long)n_items * g.H_kv;
+    }
+    if (max_own > 0) {
+        const long long heads = (long long)n_seqs * g.H_kv;
+        chunks = (max_own + 127) / 128;
+        const long long most = (1024 + heads - 1) / heads;
+        if (chunks > most) chunks = most;
+        p.own_chunk = (int)(((max_own + chunks - 1) / chunks + kTile - 1) / kTile * kTile);
+        p.own_chunks = (max_own + p.own_chunk - 1) / p.own_chunk;
+        p.logit_pitch = (max_own + kTile - 1) / kTile * kTile;
+    }
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
+    const size_t prompt = (size_t)slots * max_seqs * g.G, own = (size_t)n_seqs * g.H_kv * chunks * g.G;
+    p.stats_p = take(prompt * sizeof(float2));
+    p.stats_o = take(own * sizeof(float2));
+    p.after = take((size_t)n_seqs * g.H_kv * sizeof(int32_t));
+    p.part_p = take(prompt * g.D * sizeof(float));
+    p.part_o = take(own * g.D * sizeof(float));
+    p.logits = take((size_t)n_seqs * g.H_q * p.logit_pitch * sizeof(float));
+    p.bytes = at;
+    return p;
+}
+bool shared_supported(const Geom& g, const SharedPlan& p, int n_seqs)
+{
+    const double most = 8388608.;               // launches stay below 2^32 threads
+    return g.G <= 32 && (double)(p.slots + 8) * p.row_blocks + (double)n_seqs * g.H_kv * p.own_chunks < most &&
+           (double)n_seqs * g.H_q + (double)n_seqs * g.H_kv * (p.logit_pitch / kThreads + 1) < most;
+}
+
+hipError_t launch_shared(const Geom& g, const SharedPlan& p, const SharedCall& c, void* workspace, hipStream_t s)
+{
+    Shared a{};
+    char* ws = static_cast<char*>(workspace);
+    a.g = g;
+    a.q = static_cast<const __bf16*>(c.q);
+    a.kp = static_cast<const __bf16*>(c.k_prompt);
+    a.vp = static_cast<const __bf16*>(c.v_prompt);
+    a.cu_b = c.cu_budgets;
+    a.cu_seqs = c.cu_seqs;
+    a.n_items = c.n_items;
+    a.total_rows = (int)c.total_rows;
+    a.n_seqs = c.n_seqs;
+    a.max_seqs = c.max_seqs;
+    a.log_r = p.log_r;
+    a.slots = (int)p.slots;
+    a.slots_pad = (int)((p.slots + 7) / 8 * 8);
+    a.row_blocks = p.row_blocks;
+    a.ko = static_cast<__bf16*>(c.k_own);
+    a.vo = static_cast<__bf16*>(c.v_own);
+    a.lengths = c.lengths;
+    a.positions = c.positions;
+    a.weights = c.weights;
+    a.capacity = c.capacity;
+    a.max_own = c.max_own;
+    a.own_chunk = p.own_chunk;
+    a.own_chunks = p.own_chunks;
+    a.k_new = static_cast<const __bf16*>(c.k_new);
+    a.v_new = static_cast<const __bf16*>(c.v_new);
+    a.pos_new = c.pos_new;
+    a.stats_p = reinterpret_cast<float2*>(ws + p.stats_p);
+    a.stats_o = reinterpret_cast<float2*>(ws + p.stats_o);
+    a.after = reinterpret_cast<int32_t*>(ws + p.after);
+    a.part_p = reinterpret_cast<float*>(ws + p.part_p);
+    a.part_o = reinterpret_cast<float*>(ws + p.part_o);
+    a.logits = reinterpret_cast<float*>(ws + p.logits);
+    a.logit_pitch = p.logit_pitch;
+    a.out = static_cast<__bf16*>(c.out);
+    const dim3 threads(kThreads);
+    const unsigned blocks = (unsigned)(a.slots_pad * a.row_blocks + c.n_seqs * g.H_kv * p.own_chunks);
+    if (blocks > 0) {
+        switch (g.D) {
+            case 64:  hipLaunchKernelGGL(shared_partial_kernel<64>, dim3(blocks), threads, 0, s, a); break;
+            case 128: hipLaunchKernelGGL(shared_partial_kernel<128>, dim3(blocks), threads, 0, s, a); break;
+            case 256: hipLaunchKernelGGL(shared_partial_kernel<256>, dim3(blocks), threads, 0, s, a); break;
+            default: return hipErrorInvalidValue;
+        }
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    const int weight_blocks = c.weights ? (c.max_own + kThreads - 1) / kThreads : 0;
+    hipLaunchKernelGGL(shared_join_kernel, dim3((unsigned)(c.n_seqs * g.H_q + c.n_seqs * g.H_kv * weight_blocks)), threads, 0, s, a,
+                       weight_blocks);
+    return hipGetLastError();
+}
+
+}  // namespace audiokv
