@@ -412,6 +412,27 @@ int32_t audiokv_decode_shared(const audiokv_params* params, const void* q_dev,
                               const void* k_new, const void* v_new, const int32_t* pos_new_dev,
                               void* out_dev, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Cuts the rows that sequences own to a budget, by recency and accumulated weight
+ * (paper Sec. 4: one of the compared evictions; here for the rows of
+ * audiokv_slots, in place). A head with more rows than its budget keeps, in this
+ * order, until the budget is full:
+ *   1. rows at positions > newest - recent, newest being the head's largest;
+ *   2. rows by slots->weights, the largest first, NaN last (-0 equals +0);
+ * equal ones by slot, the lower first. Kept rows stay where they are, but those in
+ * slots from the budget on move, in order, into the lower slots that became free:
+ * K, V, weight and position; the length becomes the budget. Slots from the budget
+ * on keep their contents. The next audiokv_decode_shared appends behind.
+ * The budget of head (x, h) is `budget`, or the larger of it and
+ * budgets_dev[x * n_kv_heads + h] where budgets_dev (int32, device) is not NULL.
+ * recent >= 0; slots->weights is needed, slots->positions where recent > 0.
+ * max_own (host): no head has more rows, at most capacity; a head that has more is
+ * left as it is. Exact: no arithmetic but comparisons. */
+int32_t audiokv_evict_accumulated_workspace_bytes(const audiokv_params* params, int32_t n_seqs, int32_t max_own,
+                                                  int32_t budget, size_t* out_bytes);
+int32_t audiokv_evict_accumulated(const audiokv_params* params, const audiokv_slots* slots, int32_t n_seqs,
+                                  int32_t budget, const int32_t* budgets_dev, int32_t recent, int32_t max_own,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
 /* Measurement aid, not part of the method (used by the benchmark to time the
  * kernels of audiokv_evict where they run). While enabled, audiokv_evict records
  * HIP events on the caller's stream between its kernels; audiokv_profile_read

@@ -154,13 +154,16 @@ def _load() -> C.CDLL:
     lib.audiokv_decode_shared_workspace_bytes.argtypes = [pp, i32, i64, i32, i32, i32, C.POINTER(C.c_size_t)]
     lib.audiokv_decode_shared.argtypes = [pp, vp, vp, vp, vp, i32, i64, vp, i32, i32, C.POINTER(_CSlots), i32, vp, vp, vp, vp, vp,
                                           C.c_size_t, vp]
+    lib.audiokv_evict_accumulated_workspace_bytes.argtypes = [pp, i32, i32, i32, C.POINTER(C.c_size_t)]
+    lib.audiokv_evict_accumulated.argtypes = [pp, C.POINTER(_CSlots), i32, i32, vp, i32, i32, vp, C.c_size_t, vp]
     lib.audiokv_profile_enable.argtypes = [i32]
     lib.audiokv_profile_enable.restype = i32
     lib.audiokv_profile_read.argtypes = [C.POINTER(C.c_float)]
     lib.audiokv_profile_read.restype = i32
     for name in ("total_kept", "workspace_bytes", "score", "allocate", "smooth", "smooth_cutoffs", "select", "compact", "evict",
                  "decode_workspace_bytes", "decode_attend", "score_lse", "evict_lse", "evict_noalloc",
-                 "accumulate_workspace_bytes", "accumulate", "decode_shared_workspace_bytes", "decode_shared"):
+                 "accumulate_workspace_bytes", "accumulate", "decode_shared_workspace_bytes", "decode_shared",
+                 "evict_accumulated_workspace_bytes", "evict_accumulated"):
         getattr(lib, "audiokv_" + name).restype = i32
     return lib
 
@@ -535,6 +538,28 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
                                       _ptr(cu_seqs), n_seqs, int(max_seqs), C.byref(cs) if cs is not None else None, int(max_own),
                                       _ptr(k_new), _ptr(v_new), _ptr(pos_new), _ptr(out), _ptr(ws), ws.numel(), _stream()))
     return out
+
+
+def evict_accumulated_workspace_bytes(p: Params, n_seqs: int, max_own: int, budget: int) -> int:
+    out = C.c_size_t(0)
+    cp = p.c()
+    _check(_lib.audiokv_evict_accumulated_workspace_bytes(C.byref(cp), int(n_seqs), int(max_own), int(budget), C.byref(out)))
+    return out.value
+
+
+def evict_accumulated(p: Params, slots: Slots, n_seqs: int, budget: int, recent: int, max_own: int, *,
+                      budgets: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """Cuts the rows of every head of `slots` to its budget (`budget`, or the larger of it and budgets[head]) in place, by
+    recency and accumulated weight."""
+    if budgets is not None and _need(budgets, torch.int32, "budgets").numel() < n_seqs * p.n_kv_heads:
+        raise ValueError(f"budgets has {budgets.numel()} values, {n_seqs * p.n_kv_heads} needed")
+    ws = workspace
+    if ws is None:
+        ws = torch.empty(max(evict_accumulated_workspace_bytes(p, n_seqs, max_own, budget), 256), dtype=torch.uint8,
+                         device=slots.lengths.device)
+    cp, cs = p.c(), slots.c(p, n_seqs)
+    _check(_lib.audiokv_evict_accumulated(C.byref(cp), C.byref(cs), int(n_seqs), int(budget), _ptr(budgets), int(recent), int(max_own),
+                                          _ptr(ws), ws.numel(), _stream()))
 
 
 PROFILE_STAGES = ("allocate", "score_sweep1", "score_sweep2", "pool_smooth", "select", "compact")

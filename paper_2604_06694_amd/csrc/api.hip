@@ -823,6 +823,58 @@ int32_t audiokv_decode_shared(const audiokv_params* params, const void* q_dev, c
     return AUDIOKV_OK;
 }
 
+static int32_t check_evict_accumulated(const audiokv_params* p, int32_t n_seqs, int32_t max_own, int32_t budget)
+{
+    if (n_seqs < 1 || max_own < 0 || budget < 0)
+        return fail(AUDIOKV_E_INVALID_ARG, "n_seqs %d, max_own %d or budget %d out of range", n_seqs, max_own, budget);
+    if ((long long)n_seqs * p->n_kv_heads > (1 << 20)) return fail(AUDIOKV_E_UNSUPPORTED, "too many heads in one call");
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_evict_accumulated_workspace_bytes(const audiokv_params* params, int32_t n_seqs, int32_t max_own, int32_t budget,
+                                                  size_t* out_bytes)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (!out_bytes) return fail(AUDIOKV_E_INVALID_ARG, "out_bytes is NULL");
+    if (n_seqs == 0) { *out_bytes = 0; return AUDIOKV_OK; }
+    AUDIOKV_TRY(check_evict_accumulated(params, n_seqs, max_own, budget));
+    *out_bytes = max_own > budget ? evict_accumulated_bytes(make_geom(params, n_seqs), max_own, budget) : 0;
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_evict_accumulated(const audiokv_params* params, const audiokv_slots* slots, int32_t n_seqs, int32_t budget,
+                                  const int32_t* budgets_dev, int32_t recent, int32_t max_own, void* workspace, size_t workspace_bytes,
+                                  void* stream)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (n_seqs == 0) return AUDIOKV_OK;
+    AUDIOKV_TRY(check_evict_accumulated(params, n_seqs, max_own, budget));
+    if (!slots) return fail(AUDIOKV_E_INVALID_ARG, "audiokv_evict_accumulated: slots is NULL");
+    AUDIOKV_TRY(check_slots(params, slots, n_seqs, max_own));
+    if (!slots->weights) return fail(AUDIOKV_E_INVALID_ARG, "audiokv_evict_accumulated: slots have no weights");
+    if (recent < 0 || (recent > 0 && !slots->positions))
+        return fail(AUDIOKV_E_INVALID_ARG, "recent %d must be >= 0, and slots need positions where it is not 0", recent);
+    if (max_own <= budget) return AUDIOKV_OK;                  // nobody has too many
+    const Geom g = make_geom(params, n_seqs);
+    const size_t need = evict_accumulated_bytes(g, max_own, budget);
+    if (need > 0 && !workspace) return fail(AUDIOKV_E_INVALID_ARG, "audiokv_evict_accumulated: workspace is NULL");
+    if (workspace_bytes < need)
+        return fail(AUDIOKV_E_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+    EvictAccumCall c{};
+    c.k = slots->k;
+    c.v = slots->v;
+    c.lengths = slots->lengths;
+    c.weights = slots->weights;
+    c.positions = slots->positions;
+    c.budgets = budgets_dev;
+    c.capacity = slots->capacity;
+    c.max_own = max_own;
+    c.budget = budget;
+    c.recent = recent;
+    AUDIOKV_HIP(launch_evict_accumulated(g, c, workspace, static_cast<hipStream_t>(stream)), "evict_accumulated kernels");
+    return AUDIOKV_OK;
+}
+
 int32_t audiokv_profile_enable(int32_t enable)
 {
     if (enable && !g_prof.created) {

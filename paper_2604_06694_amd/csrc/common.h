@@ -189,6 +189,18 @@ SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_s
 bool shared_supported(const Geom& g, const SharedPlan& p, int n_seqs);
 hipError_t launch_shared(const Geom& g, const SharedPlan& p, const SharedCall& c, void* workspace, hipStream_t s);
 
+// rows of growing caches cut to a budget by accumulated weight (evict_accumulated.hip); Geom's items are the sequences
+struct EvictAccumCall {
+    void *k, *v;
+    int32_t* lengths;
+    float* weights;
+    int32_t* positions;
+    const int32_t* budgets;            // may be nullptr
+    int capacity, max_own, budget, recent;
+};
+size_t evict_accumulated_bytes(const Geom& g, int max_own, int budget);
+hipError_t launch_evict_accumulated(const Geom& g, const EvictAccumCall& c, void* workspace, hipStream_t s);
+
 bool select_supported(int L);
 // whether launch_select can combine what smoothing left
 bool select_joins(int max_L);

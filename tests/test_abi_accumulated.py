@@ -109,3 +109,31 @@ def test_decode_shared_workspace_never_shrinks(A):
         assert sizes == sorted(sizes)
         sizes = [A.decode_shared_workspace_bytes(p, 0, 0, n, 0, r) for r in range(0, 9000, 31)]
         assert sizes == sorted(sizes)
+
+
+def evict(A, p, s, n=2, budget=4, budgets=None, recent=2, own=16, ws=PTR, size=1 << 40):
+    cp = p.c()
+    return A.binding._lib.audiokv_evict_accumulated(C.byref(cp), s and C.byref(s), n, budget, budgets, recent, own, ws, C.c_size_t(size), None)
+
+
+def test_evict_accumulated_refusals(A):
+    p = A.Params(8, 2, 64, 0)
+    assert evict(A, A.Params(8, 3, 64, 0), slots(A)) == -1
+    assert evict(A, p, None) == -1
+    for bad in (dict(size=8), dict(k=None), dict(v=ODD), dict(lengths=None), dict(capacity=15), dict(weights=None), dict(positions=None)):
+        assert evict(A, p, slots(A, **bad)) == -1, bad
+    for bad in (dict(n=-1), dict(budget=-1), dict(recent=-1), dict(own=-1)):
+        assert evict(A, p, slots(A), **bad) == -1, bad
+    assert evict(A, p, slots(A), n=2**20) == -2
+    big = slots(A, capacity=4096)
+    assert evict(A, p, big, own=4096, budget=2000, size=64) == -3
+    assert evict(A, p, big, own=4096, budget=2000, ws=None) == -1
+
+
+def test_evict_accumulated_of_nothing(A):
+    p = A.Params(8, 2, 64, 0)
+    assert evict(A, p, None, n=0) == 0
+    assert evict(A, p, slots(A), budget=16) == 0                  # nobody can have too many: nothing is enqueued
+    assert A.evict_accumulated_workspace_bytes(p, 2, 16, 16) == 0
+    assert A.evict_accumulated_workspace_bytes(p, 2, 5000, 2000) > 0
+    assert A.evict_accumulated_workspace_bytes(p, 2, 5000, 4900) == 0     # few moves: the ranking workgroup makes them
