@@ -12,22 +12,22 @@
 // all row tiles and the lanes are joined once, at the end, so that a logit costs fma, exp2 and add in both.
 // Rows are numbered r = i * G + (head of the group): what a key block sees is then a contiguous tail of the rows, whatever G.
 //
-// The long side is cut into ranges of equal size (rows: of keys, cols: of rows), a workgroup per (block, range) that has a
-// visible pair: all workgroups cost the same but those on the diagonal. Column sums of several ranges are joined by a third
-// kernel in fixed order; row statistics by the workgroups of cols, for their rows, before they start. No atomics.
+// Work is cut into spans of equal numbers of tiles, one workgroup per CU, across blocks and heads (accumulate_plan.h): the
+// triangle leaves blocks of very different lengths, and a workgroup costs as much to start as three tiles. A grid of (block,
+// range of 13 to 32 tiles) took 350 + 340 us for one layer of 8192 tokens where this takes 262 + 274. What the parts of a block that several
+// workgroups share have found is joined by two small kernels in fixed order (row statistics; column sums). No atomics.
 //
 // References of a row are not maxima (see score_impl.h): the first logits set one, and only a tile whose sum leaves the safe
 // range is redone against a new one. Everything is in base-2 units: z = <q,k> * scale * log2(e).
+#include "accumulate_plan.h"
 #include "mfma_tile.h"
+#include "score_ring.h"
 
 namespace audiokv {
 
 namespace {
 
 using namespace mfma_tile;
-
-constexpr int kStream = 64;               // rows of a tile that streams through LDS
-constexpr int kMaxRowsPerRange = 2048;    // cols: rows whose log-sum-exp a workgroup keeps in LDS
 
 struct Accum {
     Geom g;
@@ -36,20 +36,23 @@ struct Accum {
     const int32_t* cu_seq;
     const int32_t* cu_q;
     const float* lse;          // given, or nullptr
-    float2* stats;             // [key range][row of all items] (reference, sum)
-    float* parts;              // [row range][head][longest item, padded]
+    float* norms;              // [row of all items]: log2 of the row's sum of exp2
+    float2* stats;             // [part][row of all items] (reference, sum), of rows whose block has several parts
+    float* parts;              // [part][head][part_pitch] column sums, of keys whose block has several
     float* weights;
     int64_t pitch;             // between heads of weights; 0: packed like scores
     int64_t rows_total;        // of all items
     unsigned div_g;            // r / G = umulhi(r, div_g), G > 1
-    int key_range, row_range;  // keys, rows of a range
-    int n_key_ranges, n_row_ranges, n_row_blocks, n_key_blocks;
+    int block;                 // rows (keys) of a block of the sweep
     int part_pitch;
+    AccumSpans spans;          // of the sweep (a kernel's arguments hold no more than 4 KB)
 };
+static_assert(sizeof(Accum) < 4000);
 
 struct Place {
     int item, h, L, Q, R;
     int64_t tok0, q0;          // first token and first query of the item
+    AccumItem item_of;
 };
 __device__ __forceinline__ Place place_of(const Accum& a, int head) {
     Place p;
@@ -60,6 +63,7 @@ __device__ __forceinline__ Place place_of(const Accum& a, int head) {
     p.q0 = a.cu_q[p.item];
     p.Q = min(a.cu_q[p.item + 1] - (int)p.q0, p.L);
     p.R = p.Q * a.g.G;
+    p.item_of = AccumItem{p.L, p.Q, a.g.G, a.g.causal};
     return p;
 }
 __device__ __forceinline__ int query_of(const Accum& a, int r) { return a.g.G == 1 ? r : (int)__umulhi((unsigned)r, a.div_g); }
@@ -73,249 +77,504 @@ __device__ __forceinline__ int64_t q_offset(const Accum& a, const Place& p, int 
 __device__ __forceinline__ int last_key(const Accum& a, const Place& p, int r) {
     return r >= p.R ? -1 : a.g.causal ? p.L - p.Q + query_of(a, r) : p.L - 1;
 }
-// first row that sees key j
-__device__ __forceinline__ int first_row(const Accum& a, const Place& p, int j) {
-    return a.g.causal ? max(0, j - (p.L - p.Q)) * a.g.G : 0;
-}
+// what a row's exponents are taken against: log2 of its sum of exp2. Nothing but -inf: the row gives nothing.
+__device__ __forceinline__ float norm_from(float M, float Z) { return Z == 0.f ? INFINITY : M + __log2f(Z); }
 __device__ __forceinline__ int64_t stat_row(const Accum& a, const Place& p, int r) { return p.q0 * a.g.H_q + (int64_t)p.h * p.R + r; }
 
-// ---- rows: statistics of NB * 128 rows over a range of keys ----
-template <int D, int NB>
-__global__ __launch_bounds__(kThreads, 2) void accumulate_rows_kernel(Accum a)
-{
-    constexpr int KK = D / 16, N = kPieces<D, kStream>;
-    __shared__ __attribute__((aligned(16))) __bf16 tile[2][kStream * D];
-    const int range = blockIdx.x % a.n_key_ranges, rest = blockIdx.x / a.n_key_ranges;
-    const int block = rest % a.n_row_blocks;
-    const Place p = place_of(a, rest / a.n_row_blocks);
-    const int r_first = block * (NB * 32 * kWaves);
-    if (r_first >= p.R) return;
-    const int j0 = range * a.key_range;
-    const int seen = last_key(a, p, min(r_first + NB * 32 * kWaves, p.R) - 1);       // by the last row of the block
-    const int j1 = min(j0 + a.key_range, seen + 1);
-    if (j0 >= j1) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5, col = lane & 31;
+// Compute waves of a workgroup; one more wave loads. The waves of a workgroup hold kComputeWaves * NB tiles of 32 rows (or keys) as
+// stationary operands, tiles of kStream keys (or rows) come through a ring of LDS buffers that the loader fills straight from HBM
+// or L2 (score_ring.h), one barrier per tile.
+constexpr int kLeastTiles = 2;           // fewer are not worth a workgroup
+constexpr int kComputeWaves = 7, kSweepThreads = 64 * (kComputeWaves + 1), kStages = 4;
+constexpr int stationary(int NB) { return kComputeWaves * NB * 32; }
 
-    bf16x8 qf[NB][KK];
-    int vis[NB], least[NB];            // last key that the lane's row sees, and the first row of the tile
-    float m[NB], l[NB];
+typedef __attribute__((address_space(3))) void* lds_void_ptr;
+typedef const __attribute__((address_space(1))) void* global_void_ptr;
+
+// LDS traffic only: the waves exchange nothing else
+__device__ __forceinline__ void sweep_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// The loader wave: begin(r) sets out at row r of the stream (the lane's first), next() is where the row that it has come to begins,
+// and goes on by the rows of an instruction. Rows past the end read the last one.
+// more(t): what else a tile brings.
+template <int D, class Walk, class More>
+__device__ __forceinline__ void load_stream(unsigned char* ring, int n_tiles, Walk walk, More more)
+{
+    constexpr int CPR = D / 8, RPI = 64 / CPR, CH = kStream / RPI;       // chunks of a row, rows and instructions of a tile
+    const int lane = threadIdx.x & 63, row = lane / CPR, slot = lane % CPR;
+    int from[8 / RPI];                                                   // the slots' rotation repeats after eight rows
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const int r = r_first + (wave * NB + b) * 32 + col;
-        const __bf16* src = a.q + q_offset(a, p, min(r, p.R - 1)) + hf * 8;
+    for (int v = 0; v < 8 / RPI; ++v) from[v] = ((slot & ~7) | ((slot - (v * RPI + row)) & 7)) * 8;
+    walk.begin(row, RPI);
+    score_detail::fill_ring<kStages>(
+        n_tiles,
+        [&](int t) {
+            unsigned char* dst = ring + (t % kStages) * (kStream * D * 2);
 #pragma unroll
-        for (int kk = 0; kk < KK; ++kk) qf[b][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
-        vis[b] = last_key(a, p, r);
-        least[b] = __builtin_amdgcn_readfirstlane(min(last_key(a, p, r_first + (wave * NB + b) * 32),
-                                                      last_key(a, p, r_first + (wave * NB + b) * 32 + 31)));   // -1: some are no rows
-        m[b] = -INFINITY;
-        l[b] = 0.f;
+            for (int it = 0; it < CH; ++it)
+                // a wave-wide instruction fills consecutive LDS: the lane fetches the chunk that belongs in its slot (slot_of)
+                __builtin_amdgcn_global_load_lds((global_void_ptr)(walk.next() + from[it % (8 / RPI)]), (lds_void_ptr)(dst + it * 1024), 16, 0, 0);
+            more(t);
+        },
+        [&]() {
+            __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));         // vmcnt(0): all that was requested is there
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+            __builtin_amdgcn_s_barrier();
+        });
+}
+// Keys of a head from j0 on
+struct KeyWalk {
+    const __bf16 *at, *last;
+    int64_t stride;
+    int left;                  // rows up to the last
+    int step;
+    int64_t on;
+    __device__ __forceinline__ KeyWalk(const Accum& a, const Place& p, int j0) {
+        stride = kv_tok_stride(a.g);
+        at = a.k + kv_row_offset(a.g, p.item, p.tok0, p.L, p.h, j0);
+        left = p.L - 1 - j0;
+        last = at + left * stride;
     }
-    const int chunk = piece_chunk<D>() * 8;
-    u32x4 piece[N];
-    auto fetch = [&](int j) {
+    __device__ __forceinline__ void begin(int row, int rows) {
+        at += row * stride;
+        left -= row;
+        step = rows;
+        on = rows * stride;
+    }
+    __device__ __forceinline__ const __bf16* next() {
+        const __bf16* here = left >= 0 ? at : last;
+        at += on;
+        left -= step;
+        return here;
+    }
+};
+// Query rows of a KV head from r0 on: a step is some queries and some heads, with a carry
+struct RowWalk {
+    const __bf16 *at, *last;
+    const Accum& a;
+    int64_t per_query, per_head, on, carry;
+    int left, step, heads_on, in_group, r0;
+    __device__ __forceinline__ RowWalk(const Accum& accum, const Place& p, int r) : a(accum) {
+        const bool head_major = a.g.layout == AUDIOKV_LAYOUT_HEAD_MAJOR;
+        per_query = head_major ? a.g.D : (int64_t)a.g.H_q * a.g.D;
+        per_head = head_major ? (int64_t)p.Q * a.g.D : a.g.D;
+        at = a.q + q_offset(a, p, 0);
+        last = a.q + q_offset(a, p, p.R - 1);
+        r0 = r;
+        left = p.R - 1;
+    }
+    __device__ __forceinline__ void begin(int row, int rows) {
+        const int r = r0 + row, i = query_of(a, r);
+        in_group = r - i * a.g.G;
+        at += i * per_query + in_group * per_head;
+        left -= r;
+        step = rows;
+        const int queries = query_of(a, rows);
+        heads_on = rows - queries * a.g.G;
+        on = queries * per_query + heads_on * per_head;
+        carry = per_query - a.g.G * per_head;
+    }
+    __device__ __forceinline__ const __bf16* next() {
+        const __bf16* here = left >= 0 ? at : last;
+        left -= step;
+        in_group += heads_on;
+        const bool wraps = in_group >= a.g.G;
+        in_group -= wraps ? a.g.G : 0;
+        at += on + (wraps ? carry : 0);
+        return here;
+    }
+};
+
+// A compute wave's blocks: its NB stationary tiles times 32 rows of the stream, NB * KK MFMAs, then per logit fma, exp2, add.
+// Both take about as long, so (score_impl.h) while the MFMAs of one block accumulate into one register set the logits of the block
+// before are reduced from the other, a slice after each MFMA; an empty asm statement that takes accumulator, sums and scale in and
+// out keeps the compiler from gathering the MFMAs. PIPE false: one register set, a block after the other.
+template <int D, int NB, bool COLS, bool PIPE>
+struct Wave {
+    static constexpr int KK = D / 16, SLICE = 16 / KK, PF = 2, RING = 4;
+    static_assert(KK % RING == 0 && SLICE * KK == 16);
+    bf16x8 still[NB][KK];
+    f32x16 acc[PIPE ? 2 : 1][NB];
+    bf16x8 frag[RING];
+    int frag_at[4];
+    float c;                                  // scale * log2(e)
+    float m[NB], l[NB], red[NB];              // rows: reference, sum, and the sum of a block
+    float sum[NB][16];                        // cols: a lane's share of its sixteen keys' sums
+    float norm;                               // cols: of the lane's row of the block that is reduced
+    const unsigned char* ring;
+    int hf, col;
+
+    __device__ __forceinline__ void begin(const unsigned char* r, float scale) {
+        const int lane = threadIdx.x & 63;
+        hf = lane >> 5;
+        col = lane & 31;
+        ring = r;
+        c = scale;
 #pragma unroll
-        for (int u = 0; u < N; ++u)
-            piece[u] = *reinterpret_cast<const u32x4*>(
-                a.k + kv_row_offset(a.g, p.item, p.tok0, p.L, p.h, min(j + piece_row<D>(u), p.L - 1)) + chunk);
-    };
-    fetch(j0);
-    put_tile<D>(tile[0], piece);
-    __syncthreads();
-    for (int j = j0, at = 0; j < j1; j += kStream, at ^= 1) {
-        if (j + kStream < j1) fetch(j + kStream);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int v = 0; v < 4; ++v) frag_at[v] = (col * D + slot_of((2 * v) | hf, col) * 8) * 2;
 #pragma unroll
-        for (int s = 0; s < kStream / 32; ++s) {
-            const int key0 = j + s * 32;
+        for (int b = 0; b < NB; ++b) {
+            m[b] = -INFINITY;
+            l[b] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[b][i] = 0.f;
+        }
+    }
+    // (a block is numbered from the first tile, two to a tile)
+    __device__ __forceinline__ void load(int block, int kk, int to) {
+        frag[to] = *reinterpret_cast<const bf16x8*>(ring + ((block >> 1) % kStages) * (kStream * D * 2) + (block & 1) * (32 * D * 2) +
+                                                    frag_at[kk & 3] + (kk >> 2) * 128);
+    }
+    __device__ __forceinline__ void reduce_part(f32x16 (&z)[NB], int kk, int b) {
+#pragma unroll
+        for (int e = 0; e < SLICE; ++e) {
+            const int i = kk * SLICE + e;
+            if (COLS) sum[b][i] += fast_exp2(__builtin_fmaf(z[b][i], c, -norm));
+            else red[b] += fast_exp2(__builtin_fmaf(z[b][i], c, -m[b]));
+        }
+    }
+    // MFMAs of block `next` into zm (the first PF fragments are in the ring already if STREAM, and those of the block after it are
+    // fetched at the end), reduction of zr
+    template <bool MFMA, bool REDUCE, bool STREAM>
+    __device__ __forceinline__ void run(f32x16 (&zm)[NB], int next, f32x16 (&zr)[NB]) {
+        if (MFMA && !STREAM) {
+#pragma unroll
+            for (int kk = 0; kk < PF; ++kk) load(next, kk, kk);
+        }
+        if (REDUCE && !COLS) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) red[b] = 0.f;
+        }
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) {
+            if (MFMA) {
+                if (kk + PF < KK) load(next, kk + PF, (kk + PF) % RING);
+                else if (STREAM) load(next + 1, kk + PF - KK, (kk + PF) % RING);
+            }
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                f32x16 z = {};
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk)
-                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<D>(tile[at], s * 32 + col, kk, hf), qf[b][kk], z, 0, 0, 0);
-                // keys past the range belong to another workgroup's
-                const int most = min(vis[b], j1 - 1);
-                if (key0 + 31 > min(least[b], j1 - 1)) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = key0 + key_of(i, hf) <= most ? z[i] : -INFINITY;
+                if (MFMA) {
+                    const f32x16 zero = {};
+                    const f32x16 in = kk == 0 ? zero : zm[b];
+                    // C[key][row]
+                    zm[b] = COLS ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(still[b][kk], frag[kk % RING], in, 0, 0, 0)
+                                 : __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag[kk % RING], still[b][kk], in, 0, 0, 0);
                 }
-                float sum = 0.f;
-                const float mc = m[b];
+                if (REDUCE) reduce_part(zr, kk, b);
+#if defined(__HIP_DEVICE_COMPILE__)
+                if (MFMA && REDUCE) {
+                    if constexpr (!COLS) asm volatile("" : "+v"(c), "+v"(zm[b]), "+v"(red[b]));
+                    else if constexpr (SLICE == 1) asm volatile("" : "+v"(c), "+v"(zm[b]), "+v"(sum[b][kk]));
+                    else if constexpr (SLICE == 2) asm volatile("" : "+v"(c), "+v"(zm[b]), "+v"(sum[b][2 * kk]), "+v"(sum[b][2 * kk + 1]));
+                    else asm volatile("" : "+v"(c), "+v"(zm[b]), "+v"(sum[b][4 * kk]), "+v"(sum[b][4 * kk + 1]), "+v"(sum[b][4 * kk + 2]), "+v"(sum[b][4 * kk + 3]));
+                }
+#endif
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    // rows: a block's sums join the rows'; where one has left the safe range (the first logits of a lane, whose reference is -inf;
+    // logits far above the reference; NaN), the block is summed again against a new reference
+    __device__ __forceinline__ void finish(f32x16 (&z)[NB]) {
+        if constexpr (!COLS) {
+            float worst = red[0];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) sum += fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -mc));
-                if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum < 0x1p64f)) != 0, 0)) {
-                    // the first logits of a lane (its reference is -inf), or far above its reference, or NaN
-                    float top = z[0];
+            for (int b = 1; b < NB; ++b) worst = red[b] < 0x1p64f ? worst : red[b];
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(worst < 0x1p64f)) != 0, 0)) {
 #pragma unroll
-                    for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
-                    const bool redo = !(sum < 0x1p64f);
-                    const float ref = redo ? fmaxf(mc, top * a.g.c_log2) : mc, ref0 = ref == -INFINITY ? 0.f : ref;
+                for (int b = 0; b < NB; ++b) {
+                    float top = z[b][0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) top = fmaxf(top, z[b][i]);
+                    const bool redo = !(red[b] < 0x1p64f);
+                    const float ref = redo ? fmaxf(m[b], top * c) : m[b], ref0 = ref == -INFINITY ? 0.f : ref;
                     float again = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) again += fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -ref0));
-                    l[b] = redo ? l[b] * fast_exp2(mc - ref0) : l[b];
-                    sum = redo ? again : sum;
+                    for (int i = 0; i < 16; ++i) again += fast_exp2(__builtin_fmaf(z[b][i], c, -ref0));
+                    l[b] = redo ? l[b] * fast_exp2(m[b] - ref0) : l[b];
+                    red[b] = redo ? again : red[b];
                     m[b] = ref;
                 }
-                l[b] += sum;
             }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) l[b] += red[b];
         }
-        __builtin_amdgcn_sched_barrier(0);
-        if (j + kStream < j1) put_tile<D>(tile[at ^ 1], piece);
-        __syncthreads();
     }
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        // the two halves of the wave hold different keys of the same row
-        const float m2 = __shfl_xor(m[b], 32, 64), l2 = __shfl_xor(l[b], 32, 64);
-        const float M = fmaxf(m[b], m2), ref = M == -INFINITY ? 0.f : M;
-        const float sum = l[b] * fast_exp2(m[b] - ref) + l2 * fast_exp2(m2 - ref);
-        const int r = r_first + (wave * NB + b) * 32 + col;
-        if (hf == 0 && r < p.R) a.stats[(int64_t)range * a.rows_total + stat_row(a, p, r)] = make_float2(M, sum);
-    }
-}
-
-// ---- cols: column sums of 256 keys over a range of rows ----
-constexpr int kKeyTiles = 2, kKeyBlock = kKeyTiles * 32 * kWaves;
-
-template <int D>
-__global__ __launch_bounds__(kThreads, 2) void accumulate_cols_kernel(Accum a)
-{
-    constexpr int KK = D / 16, N = kPieces<D, kStream>;
-    __shared__ __attribute__((aligned(16))) __bf16 tile[2][kStream * D];
-    __shared__ float norm[kMaxRowsPerRange + kStream];        // log2 of a row's sum of exp2, by row of the range
-    const int range = blockIdx.x % a.n_row_ranges, rest = blockIdx.x / a.n_row_ranges;
-    const int block = rest % a.n_key_blocks, head = rest / a.n_key_blocks;
-    const Place p = place_of(a, head);
-    const int k_first = block * kKeyBlock;
-    if (k_first >= p.L) return;
-    const int r1 = min((range + 1) * a.row_range, p.R);
-    const int r0 = max(range * a.row_range, first_row(a, p, k_first) & ~31);
-    if (r0 >= r1) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5, col = lane & 31;
-
-    // key tiles, the stationary operand
-    bf16x8 kf[kKeyTiles][KK];
-    const int key0 = k_first + wave * (kKeyTiles * 32);
-#pragma unroll
-    for (int b = 0; b < kKeyTiles; ++b) {
-        const __bf16* src = a.k + kv_row_offset(a.g, p.item, p.tok0, p.L, p.h, min(key0 + b * 32 + col, p.L - 1)) + hf * 8;
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) kf[b][kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
-    }
-    const int chunk = piece_chunk<D>() * 8;
-    u32x4 piece[N];
-    auto fetch = [&](int r) {
-#pragma unroll
-        for (int u = 0; u < N; ++u)
-            piece[u] = *reinterpret_cast<const u32x4*>(a.q + q_offset(a, p, min(r + piece_row<D>(u), p.R - 1)) + chunk);
-    };
-    fetch(r0);
-    for (int r = r0 + tid; r < r1 + kStream; r += kThreads) {
-        float v = INFINITY;                                   // no such row: exp2(z - inf) = 0
-        if (r < r1) {
-            if (a.lse) {
-                const int i = query_of(a, r), hq = p.h * a.g.G + (r - i * a.g.G);
-                const float given = a.lse[p.q0 * a.g.H_q + (int64_t)hq * p.Q + i];
-                v = given == -INFINITY ? INFINITY : given * 1.44269504088896340736f;
-            } else {
-                const int n = last_key(a, p, r) / a.key_range + 1;
-                const float2* st = a.stats + stat_row(a, p, r);
-                float M = -INFINITY, Z = 0.f;
-                for (int c = 0; c < n; ++c) {
-                    const float2 s = st[(int64_t)c * a.rows_total];
-                    const float M2 = fmaxf(M, s.x), ref = M2 == -INFINITY ? 0.f : M2;
-                    Z = Z * fast_exp2(M - ref) + s.y * fast_exp2(s.x - ref);
-                    M = M2;
-                }
-                v = Z == 0.f ? INFINITY : M + __log2f(Z);     // nothing but -inf: the row gives nothing
-            }
-        }
-        norm[r - r0] = v;
-    }
-    put_tile<D>(tile[0], piece);
-    __syncthreads();
-
-    float sum[kKeyTiles][16];
-#pragma unroll
-    for (int b = 0; b < kKeyTiles; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum[b][i] = 0.f;
-    for (int r = r0, at = 0; r < r1; r += kStream, at ^= 1) {
-        if (r + kStream < r1) fetch(r + kStream);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int s = 0; s < kStream / 32; ++s) {
-            const int row0 = r + s * 32;
-            const float c = norm[row0 + col - r0];
-            const int vis = row0 + col < r1 ? last_key(a, p, row0 + col) : -1;
-            const int least = __builtin_amdgcn_readfirstlane(row0 + 31 < r1 ? last_key(a, p, row0) : -1);
-#pragma unroll
-            for (int b = 0; b < kKeyTiles; ++b) {
-                f32x16 z = {};
-#pragma unroll
-                for (int kk = 0; kk < KK; ++kk)
-                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[b][kk], fragment<D>(tile[at], s * 32 + col, kk, hf), z, 0, 0, 0);
-                if (key0 + b * 32 + 31 <= least) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) sum[b][i] += fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -c));
+    // Tiles t0 to t1, all of whose pairs count. norm_of(block): the lane's row's norm in that block.
+    template <class Norm>
+    __device__ __forceinline__ void plain(int t0, int t1, Norm norm_of) {
+        if (t0 >= t1) return;
+        if constexpr (PIPE) {
+            float next_norm = COLS ? norm_of(2 * t0) : 0.f;
+            run<true, false, false>(acc[0], 2 * t0, acc[1]);
+            load(2 * t0 + 1, 0, 0);
+            load(2 * t0 + 1, 1, 1);
+            for (int t = t0; t < t1; ++t) {
+                norm = next_norm;
+                if (COLS) next_norm = norm_of(2 * t + 1);
+                run<true, true, true>(acc[1], 2 * t + 1, acc[0]);
+                finish(acc[0]);
+                norm = next_norm;
+                if (t + 1 < t1) {
+                    if (COLS) next_norm = norm_of(2 * t + 2);
+                    run<true, true, true>(acc[0], 2 * t + 2, acc[1]);
                 } else {
+                    run<false, true, false>(acc[0], 0, acc[1]);
+                }
+                finish(acc[1]);
+                sweep_barrier();
+            }
+        } else {
+            for (int t = t0; t < t1; ++t) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if (COLS) norm = norm_of(2 * t + s);
+                    run<true, false, false>(acc[0], 2 * t + s, acc[0]);
+                    run<false, true, false>(acc[0], 0, acc[0]);
+                    finish(acc[0]);
+                }
+                sweep_barrier();
+            }
+        }
+    }
+    // Tiles t0 to t1 with pairs that do not: most_of(block, b) is the last key of the block's 32, as the lane's half counts them,
+    // that counts for the lane's row and stationary tile b.
+    template <class Norm, class Most>
+    __device__ __forceinline__ void masked(int t0, int t1, Norm norm_of, Most most_of) {
+        for (int t = t0; t < t1; ++t) {
+#pragma unroll 1
+            for (int s = 0; s < 2; ++s) {
+                run<true, false, false>(acc[0], 2 * t + s, acc[0]);
+                if (COLS) norm = norm_of(2 * t + s);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    const int most = most_of(2 * t + s, b) - 4 * hf;
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const float e = fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -c));
-                        sum[b][i] += key0 + b * 32 + key_of(i, hf) <= vis ? e : 0.f;
+                        if (COLS) {                           // (a row's NaN is none of the keys' that it does not see)
+                            const float e = fast_exp2(__builtin_fmaf(acc[0][b][i], c, -norm));
+                            sum[b][i] += key_of(i, 0) <= most ? e : 0.f;
+                        } else {
+                            acc[0][b][i] = key_of(i, 0) <= most ? acc[0][b][i] : -INFINITY;
+                        }
                     }
                 }
+                if (!COLS) {
+                    run<false, true, false>(acc[0], 0, acc[0]);
+                    finish(acc[0]);
+                }
             }
+            sweep_barrier();
         }
-        __builtin_amdgcn_sched_barrier(0);
-        if (r + kStream < r1) put_tile<D>(tile[at ^ 1], piece);
-        __syncthreads();
     }
-    // the lanes of a half hold the same keys of different rows
-#pragma unroll
-    for (int b = 0; b < kKeyTiles; ++b) {
-        float mine = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float v = sum[b][i];
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-            mine = (lane & 15) == i ? v : mine;
+};
+
+// The parts of blocks in a workgroup's span: body(place, head, block, first tile, tiles, part, whether the block has others).
+// Neighbouring spans go to one XCD, whose L2 then holds the head that they are about.
+template <bool COLS, class Body>
+__device__ __forceinline__ void for_parts(const Accum& a, Body body)
+{
+    const AccumSpans& s = a.spans;
+    const int w = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
+    if (w >= s.n) return;
+    const SpanStart end = s.at[w + 1];
+    int head = s.at[w].head, block = s.at[w].block, tile = s.at[w].tile;
+    while (head < end.head || (head == end.head && (block < end.block || (block == end.block && tile < end.tile)))) {
+        const Place p = place_of(a, head);
+        if (block >= p.item_of.blocks(COLS, a.block)) {
+            ++head;
+            block = tile = 0;
+            continue;
         }
-        const int j = key0 + b * 32 + key_of(lane & 15, hf);
-        if (col < 16 && j < p.L) {
-            if (a.n_row_ranges > 1) {
-                a.parts[((int64_t)range * a.g.n_items * a.g.H_kv + head) * a.part_pitch + j] = mine;
-            } else {
-                float* w = a.weights + (a.pitch ? head * a.pitch : p.tok0 * a.g.H_kv + (int64_t)p.h * p.L);
-                w[j] += mine;
-            }
-        }
+        const int tiles = p.item_of.tiles(COLS, block, a.block), stop = head == end.head && block == end.block ? min(tiles, end.tile) : tiles;
+        if (tile < stop) body(p, head, block, tile, stop - tile, tile > 0 ? w - s.first_of(head, block, w) : 0, stop - tile < tiles);
+        ++block;
+        tile = 0;
     }
 }
 
-// weights += the column sums of the row ranges that see the key's block
-__global__ __launch_bounds__(kThreads) void accumulate_join_kernel(Accum a, int blocks)
+// ---- rows: statistics of blocks of stationary(NB) rows ----
+template <int D, int NB>
+__global__ __launch_bounds__(kSweepThreads, 2) void accumulate_rows_kernel(Accum a)
 {
-    const int head = blockIdx.x / blocks;
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    for_parts<false>(a, [&](const Place& p, int, int block, int tile0, int n_tiles, int part, bool shared) {
+        const int j0 = tile0 * kStream;
+        if (wave == kComputeWaves) {
+            load_stream<D>(lds, n_tiles, KeyWalk(a, p, j0), [](int) {});
+            return;
+        }
+        Wave<D, NB, false, true> w;
+        w.begin(lds, a.g.c_log2);
+        const int r_wave = block * stationary(NB) + wave * NB * 32;
+        int vis[NB];                           // last key that the lane's row sees, from the part's first
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            load_fragments<D, NB>(w.still[b], [&](int i) { return a.q + q_offset(a, p, min(r_wave + b * 32 + i, p.R - 1)); });
+            vis[b] = last_key(a, p, min(r_wave + b * 32 + w.col, p.R - 1)) - j0;
+        }
+        // tiles that every row of the wave sees, and that some row does
+        int all = 0, some = 0;
+        if (r_wave < p.R) {
+            all = min(max(0, last_key(a, p, r_wave) + 1 - j0) / kStream, n_tiles);
+            some = min((max(0, last_key(a, p, min(r_wave + NB * 32, p.R) - 1) + 1 - j0) + kStream - 1) / kStream, n_tiles);
+        }
+        all = __builtin_amdgcn_readfirstlane(all);
+        some = __builtin_amdgcn_readfirstlane(some);
+        auto none = [](int) { return 0.f; };
+        sweep_barrier();                       // the first tiles are in the ring
+        w.plain(0, all, none);
+        w.masked(all, some, none, [&](int blk, int b) { return vis[b] - blk * 32; });
+        for (int t = some; t < n_tiles; ++t) sweep_barrier();
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            // the two halves of the wave hold different keys of the same row
+            const float m2 = __shfl_xor(w.m[b], 32, 64), l2 = __shfl_xor(w.l[b], 32, 64);
+            const float M = fmaxf(w.m[b], m2), ref = M == -INFINITY ? 0.f : M;
+            const float sum = w.l[b] * fast_exp2(w.m[b] - ref) + l2 * fast_exp2(m2 - ref);
+            const int r = r_wave + b * 32 + w.col;
+            if (w.hf == 0 && r < p.R) {
+                if (shared) a.stats[part * a.rows_total + stat_row(a, p, r)] = make_float2(M, sum);
+                else a.norms[stat_row(a, p, r)] = norm_from(M, sum);
+            }
+        }
+    });
+}
+
+// The statistics of rows whose block has several parts, joined to one norm each. A workgroup per block.
+__global__ __launch_bounds__(kThreads) void accumulate_norm_kernel(Accum a, int max_blocks)
+{
+    const int head = blockIdx.x / max_blocks, block = blockIdx.x - head * max_blocks;
     const Place p = place_of(a, head);
-    const int j = (blockIdx.x - head * blocks) * kThreads + threadIdx.x;
-    if (j >= p.L) return;
-    const int first = (first_row(a, p, j / kKeyBlock * kKeyBlock) & ~31) / a.row_range, n = (p.R + a.row_range - 1) / a.row_range;
-    if (first >= n) return;
+    if (block >= p.item_of.row_blocks(a.block)) return;
+    int first, n;
+    parts_of(a.spans, head, block, &first, &n);
+    if (n == 1) return;
+    const int end = min((block + 1) * a.block, p.R);
+    for (int r = block * a.block + threadIdx.x; r < end; r += kThreads) {
+        const float2* st = a.stats + stat_row(a, p, r);
+        float M = -INFINITY, Z = 0.f;
+        for (int c0 = 0; c0 < n; c0 += 8) {
+            float2 s[8];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) s[c] = st[min(c0 + c, n - 1) * a.rows_total];
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                if (c0 + c >= n) continue;
+                const float M2 = fmaxf(M, s[c].x), ref = M2 == -INFINITY ? 0.f : M2;
+                Z = Z * fast_exp2(M - ref) + s[c].y * fast_exp2(s[c].x - ref);
+                M = M2;
+            }
+        }
+        a.norms[stat_row(a, p, r)] = norm_from(M, Z);
+    }
+}
+
+// ---- cols: column sums of blocks of stationary(NB) keys ----
+template <int D, int NB, bool PIPE>
+__global__ __launch_bounds__(kSweepThreads, 2) void accumulate_cols_kernel(Accum a)
+{
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    float* norm = reinterpret_cast<float*>(lds + kStages * kStream * D * 2);      // of a tile's rows, beside the tile in the ring
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    for_parts<true>(a, [&](const Place& p, int head, int block, int tile0, int n_tiles, int part, bool shared) {
+        const int r0 = p.item_of.key_tiles_from(block, a.block) + tile0 * kStream;
+        if (wave == kComputeWaves) {
+            load_stream<D>(lds, n_tiles, RowWalk(a, p, r0), [&](int t) {
+                const int r = min(r0 + t * kStream + lane, p.R - 1);
+                const float* src;
+                if (a.lse) {
+                    const int i = query_of(a, r), hq = p.h * a.g.G + (r - i * a.g.G);
+                    src = a.lse + p.q0 * a.g.H_q + (int64_t)hq * p.Q + i;
+                } else {
+                    src = a.norms + stat_row(a, p, r);
+                }
+                __builtin_amdgcn_global_load_lds((global_void_ptr)src, (lds_void_ptr)(norm + (t % kStages) * kStream), 4, 0, 0);
+            });
+            return;
+        }
+        Wave<D, NB, true, PIPE> w;
+        w.begin(lds, a.g.c_log2);
+        const int key0 = block * stationary(NB) + wave * NB * 32;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            load_fragments<D, NB>(w.still[b], [&](int i) {
+                return a.k + kv_row_offset(a.g, p.item, p.tok0, p.L, p.h, min(key0 + b * 32 + i, p.L - 1));
+            });
+        // tiles that see none of the wave's keys, and the first that sees them all
+        int none = n_tiles, all = n_tiles;
+        if (key0 < p.L) {
+            none = min(max(0, p.item_of.first_row(key0) - r0) / kStream, n_tiles);
+            all = min((max(0, p.item_of.first_row(min(key0 + NB * 32, p.L) - 1) - r0) + kStream - 1) / kStream, n_tiles);
+        }
+        none = __builtin_amdgcn_readfirstlane(none);
+        all = __builtin_amdgcn_readfirstlane(all);
+        const bool given = a.lse != nullptr;
+        const int end = p.R - r0 - w.col;      // the lane's row of a block 32 * blk rows on is there below it
+        auto norm_of = [&](int blk) {
+            float v = norm[((blk >> 1) % kStages) * kStream + (blk & 1) * 32 + w.col];
+            if (given) v = v == -INFINITY ? INFINITY : v * 1.44269504088896340736f;      // (-inf: the row saw nothing, and gives nothing)
+            return blk * 32 < end ? v : INFINITY;                                        // no such row: exp2(z - inf) = 0
+        };
+        sweep_barrier();                       // the first tiles are in the ring
+        for (int t = 0; t < none; ++t) sweep_barrier();
+        w.masked(none, all, norm_of, [&](int blk, int b) { return last_key(a, p, min(r0 + blk * 32 + w.col, p.R - 1)) - key0 - b * 32; });
+        w.plain(all, n_tiles, norm_of);
+        // The lanes of a half hold the same sixteen keys of different rows: with every exchange a lane keeps half of its keys, until
+        // it has one, that of its number mod 16, and so has the lane sixteen on.
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int o = 8, n = 16; o > 0; o >>= 1, n >>= 1) {
+                const bool upper = lane & o;
+#pragma unroll
+                for (int i = 0; i < n / 2; ++i) {
+                    const float keep = upper ? w.sum[b][i + n / 2] : w.sum[b][i], give = upper ? w.sum[b][i] : w.sum[b][i + n / 2];
+                    w.sum[b][i] = keep + __shfl_xor(give, o, 64);
+                }
+            }
+            const float mine = w.sum[b][0] + __shfl_xor(w.sum[b][0], 16, 64);
+            const int j = key0 + b * 32 + key_of(lane & 15, w.hf);
+            if (w.col < 16 && j < p.L) {
+                if (shared) {
+                    a.parts[((int64_t)part * a.g.n_items * a.g.H_kv + head) * a.part_pitch + j] = mine;
+                } else {
+                    float* to = a.weights + (a.pitch ? head * a.pitch : p.tok0 * a.g.H_kv + (int64_t)p.h * p.L);
+                    to[j] += mine;
+                }
+            }
+        }
+    });
+}
+
+// weights += the column sums of keys whose block has several parts. A workgroup per block.
+__global__ __launch_bounds__(kThreads) void accumulate_join_kernel(Accum a, int max_blocks)
+{
+    const int head = blockIdx.x / max_blocks, block = blockIdx.x - head * max_blocks;
+    const Place p = place_of(a, head);
+    if (block >= p.item_of.key_blocks(a.block)) return;
+    int first, n;
+    parts_of(a.spans, head, block, &first, &n);
+    if (n == 1) return;
     const int64_t step = (int64_t)a.g.n_items * a.g.H_kv * a.part_pitch;
-    const float* src = a.parts + (int64_t)head * a.part_pitch + j;
-    float v = 0.f;
+    const int end = min((block + 1) * a.block, p.L);
+    for (int j = block * a.block + threadIdx.x; j < end; j += kThreads) {
+        const float* src = a.parts + (int64_t)head * a.part_pitch + j;
+        float v = 0.f;
 #pragma unroll 8
-    for (int c = first; c < n; ++c) v += src[c * step];
-    a.weights[(a.pitch ? head * a.pitch : p.tok0 * a.g.H_kv + (int64_t)p.h * p.L) + j] += v;
+        for (int c = 0; c < n; ++c) v += src[c * step];
+        a.weights[(a.pitch ? head * a.pitch : p.tok0 * a.g.H_kv + (int64_t)p.h * p.L) + j] += v;
+    }
 }
 
 }  // namespace
 
-// How a call is cut. Pure function of the batch, so that the workspace query and the launch agree.
+// Pure function of the batch, so that the workspace query and the launch agree.
 AccumPlan accumulate_plan(const Geom& g, const int32_t* seqlens, const int32_t* queries, int n_items)
 {
     AccumPlan p;
@@ -327,85 +586,92 @@ AccumPlan accumulate_plan(const Geom& g, const int32_t* seqlens, const int32_t* 
         p.rows_total += (long long)queries[i] * g.H_q;
         pairs += (g.causal ? Q * (L - Q) + Q * (Q + 1.) / 2. : Q * L) * g.H_q;
     }
-    const long long R = (long long)p.max_Q * g.G;
-    constexpr double kWorkgroups = 1024.;                 // two rounds of two per CU
-    auto round_up = [](double x, int to, long long least, long long most) {
-        long long v = ((long long)x / to + 1) * to;
-        return v < least ? least : v > most ? most : v;
-    };
-    p.row_tiles = pairs / (256. * 64.) >= 65536. ? 2 : 1;
-    const int row_block = p.row_tiles * 32 * kWaves;
-    const long long least = ((long long)p.max_L + 15) / 16;               // sixteen key ranges at most
-    p.key_range = (int)round_up(pairs / (kWorkgroups * row_block), kStream, (least + kStream - 1) / kStream * kStream, 1LL << 30);
-    if (p.key_range < 256) p.key_range = 256;
-    p.n_key_ranges = (p.max_L + p.key_range - 1) / p.key_range;
-    p.row_range = (int)round_up(pairs / (kWorkgroups * kKeyBlock), kStream, 256, kMaxRowsPerRange);
-    p.n_row_ranges = (int)((R + p.row_range - 1) / p.row_range);
-    p.n_row_blocks = (int)((R + row_block - 1) / row_block);
-    p.n_key_blocks = (p.max_L + kKeyBlock - 1) / kKeyBlock;
-    p.part_pitch = p.n_key_blocks * kKeyBlock;
+    // two tiles per wave where they still make eight tiles of work for every CU
+    p.tiles_per_wave = pairs / (stationary(2) * (double)kStream) >= 8. * kSpans ? 2 : 1;
+    // launches stay below 2^32 threads, tiles below 2^31, and a row's number below what query_of divides exactly
+    const double rows = (double)p.max_Q * g.G, blocks = (rows > p.max_L ? rows : p.max_L) / stationary(1) + 1.;
+    p.too_large = (double)n_items * g.H_kv * blocks >= 8388608. || rows * g.G >= 2147483648. ||
+                  pairs / (stationary(1) * (double)kStream) + (double)n_items * g.H_kv * blocks * (g.G + 2.) >= 2e9;
+    if (p.too_large) return p;
+    auto item = [&](int i) { return AccumItem{seqlens[i], queries[i], g.G, g.causal}; };
+    p.rows = plan_sweep(false, stationary(p.tiles_per_wave), n_items, g.H_kv, kLeastTiles, item);
+    p.cols = plan_sweep(true, stationary(p.tiles_per_wave), n_items, g.H_kv, kLeastTiles, item);
     return p;
 }
 
+namespace {
+inline size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+inline int part_pitch(const AccumPlan& p) { return p.cols.max_blocks * p.cols.size; }
+}  // namespace
+
 size_t accumulate_stats_bytes(const AccumPlan& p) {
-    return ((size_t)p.n_key_ranges * (size_t)p.rows_total * sizeof(float2) + 255) & ~(size_t)255;
+    return up((size_t)p.rows_total * sizeof(float)) + (p.rows.max_parts > 1 ? up((size_t)p.rows.max_parts * (size_t)p.rows_total * sizeof(float2)) : 0);
 }
 size_t accumulate_parts_bytes(const Geom& g, const AccumPlan& p) {
-    return p.n_row_ranges > 1 ? (size_t)p.n_row_ranges * g.n_items * g.H_kv * p.part_pitch * sizeof(float) : 0;
+    return p.cols.max_parts > 1 ? (size_t)p.cols.max_parts * g.n_items * g.H_kv * part_pitch(p) * sizeof(float) : 0;
 }
-// launches stay below 2^32 threads, and a row's number below what query_of divides exactly
-bool accumulate_supported(const Geom& g, const AccumPlan& p) {
-    const double heads = (double)g.n_items * g.H_kv, most = 8388608.;
-    return heads * p.n_key_ranges * p.n_row_blocks < most && heads * p.n_row_ranges * p.n_key_blocks < most &&
-           (double)p.max_Q * g.G * g.G < 4294967296.;
+namespace {
+// more than 64 KB of LDS have to be asked for, once per device and kernel
+template <class Kernel>
+hipError_t launch_sweep(Kernel kernel, unsigned lds, const AccumSweep& sweep, Accum& a, hipStream_t s)
+{
+    a.spans = sweep.spans;
+    a.block = sweep.size;
+    if (sweep.spans.n == 0) return hipSuccess;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((sweep.spans.n + 7) / 8 * 8)), dim3(kSweepThreads), lds, s, a);
+    return hipGetLastError();
 }
+template <int D>
+hipError_t launch_sweeps(const Geom& g, const AccumPlan& p, Accum& a, hipStream_t s)
+{
+    constexpr unsigned ring = kStages * kStream * D * 2;
+    const int heads = g.n_items * g.H_kv;
+    const bool two = p.tiles_per_wave == 2;
+    hipError_t e = hipSuccess;
+    if (!a.lse) {
+        e = two ? launch_sweep(accumulate_rows_kernel<D, 2>, ring, p.rows, a, s) : launch_sweep(accumulate_rows_kernel<D, 1>, ring, p.rows, a, s);
+        if (e == hipSuccess && p.rows.max_parts > 1) {
+            hipLaunchKernelGGL(accumulate_norm_kernel, dim3((unsigned)(heads * p.rows.max_blocks)), dim3(kThreads), 0, s, a, p.rows.max_blocks);
+            e = hipGetLastError();
+        }
+        if (e != hipSuccess) return e;
+    }
+    constexpr unsigned norms = kStages * kStream * sizeof(float);
+    e = two ? launch_sweep(accumulate_cols_kernel<D, 2, D != 256>, ring + norms, p.cols, a, s)
+            : launch_sweep(accumulate_cols_kernel<D, 1, true>, ring + norms, p.cols, a, s);
+    if (e != hipSuccess || p.cols.max_parts == 1) return e;
+    hipLaunchKernelGGL(accumulate_join_kernel, dim3((unsigned)(heads * p.cols.max_blocks)), dim3(kThreads), 0, s, a, p.cols.max_blocks);
+    return hipGetLastError();
+}
+}  // namespace
 
 hipError_t launch_accumulate(const Geom& g, const AccumPlan& p, const void* q, const void* k, const int32_t* cu_seqlens,
                              const int32_t* cu_queries, const float* lse, float* weights, int64_t pitch, void* workspace, hipStream_t s)
 {
     Accum a{};
+    char* ws = static_cast<char*>(workspace);
     a.g = g;
     a.q = static_cast<const __bf16*>(q);
     a.k = static_cast<const __bf16*>(k);
     a.cu_seq = cu_seqlens;
     a.cu_q = cu_queries;
     a.lse = lse;
-    a.stats = static_cast<float2*>(workspace);
-    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + (lse ? 0 : accumulate_stats_bytes(p)));
+    a.norms = reinterpret_cast<float*>(ws);
+    a.stats = reinterpret_cast<float2*>(ws + up((size_t)p.rows_total * sizeof(float)));
+    a.parts = reinterpret_cast<float*>(ws + (lse ? 0 : accumulate_stats_bytes(p)));
     a.weights = weights;
     a.pitch = pitch;
     a.rows_total = p.rows_total;
     a.div_g = g.G > 1 ? (unsigned)((0x100000000ULL + g.G - 1) / g.G) : 0;
-    a.key_range = p.key_range;
-    a.row_range = p.row_range;
-    a.n_key_ranges = p.n_key_ranges;
-    a.n_row_ranges = p.n_row_ranges;
-    a.n_row_blocks = p.n_row_blocks;
-    a.n_key_blocks = p.n_key_blocks;
-    a.part_pitch = p.part_pitch;
-    const int heads = g.n_items * g.H_kv;
-    const dim3 rows((unsigned)(heads * p.n_row_blocks * p.n_key_ranges)), cols((unsigned)(heads * p.n_key_blocks * p.n_row_ranges));
-    const dim3 threads(kThreads);
-#define AUDIOKV_ACCUMULATE(DD)                                                                                       \
-    do {                                                                                                             \
-        if (!lse) {                                                                                                  \
-            if (p.row_tiles == 2) hipLaunchKernelGGL((accumulate_rows_kernel<DD, 2>), rows, threads, 0, s, a);       \
-            else hipLaunchKernelGGL((accumulate_rows_kernel<DD, 1>), rows, threads, 0, s, a);                        \
-        }                                                                                                            \
-        hipLaunchKernelGGL((accumulate_cols_kernel<DD>), cols, threads, 0, s, a);                                    \
-    } while (0)
+    a.part_pitch = part_pitch(p);
     switch (g.D) {
-        case 64:  AUDIOKV_ACCUMULATE(64);  break;
-        case 128: AUDIOKV_ACCUMULATE(128); break;
-        case 256: AUDIOKV_ACCUMULATE(256); break;
+        case 64:  return launch_sweeps<64>(g, p, a, s);
+        case 128: return launch_sweeps<128>(g, p, a, s);
+        case 256: return launch_sweeps<256>(g, p, a, s);
         default: return hipErrorInvalidValue;
     }
-#undef AUDIOKV_ACCUMULATE
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.n_row_ranges == 1) return e;
-    const int blocks = (p.max_L + kThreads - 1) / kThreads;
-    hipLaunchKernelGGL(accumulate_join_kernel, dim3((unsigned)(heads * blocks)), threads, 0, s, a, blocks);
-    return hipGetLastError();
 }
 
 }  // namespace audiokv

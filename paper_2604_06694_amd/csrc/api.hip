@@ -6,6 +6,7 @@
 #include <cstring>
 #include <mutex>
 
+#include "accumulate_plan.h"
 #include "common.h"
 #include "conv.h"
 #include "select_head.h"
@@ -683,7 +684,7 @@ static int32_t check_queries(const audiokv_params* p, int32_t n_items, const int
             return fail(AUDIOKV_E_INVALID_ARG, "item %d: %d queries must lie in [0, length = %d]", i, queries_host[i], seqlens_host[i]);
     *g = make_geom(p, n_items);
     *plan = accumulate_plan(*g, seqlens_host, queries_host, n_items);
-    if (!accumulate_supported(*g, *plan))
+    if (plan->too_large)
         return fail(AUDIOKV_E_UNSUPPORTED, "accumulate: too many (query, key) blocks for one call: split the batch");
     return AUDIOKV_OK;
 }

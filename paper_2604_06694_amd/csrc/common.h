@@ -145,17 +145,8 @@ hipError_t launch_decode(const Geom& g, const void* q, const void* k_cache, cons
                          const int32_t* cu_budgets, long long total_rows, float* out, void* workspace, hipStream_t s);
 
 // accumulated attention weight of all queries (accumulate.hip)
-struct AccumPlan {
-    int max_L = 0, max_Q = 0;
-    long long rows_total = 0;                  // query rows of all items
-    int row_tiles = 1;                         // tiles of 32 rows per wave where rows are stationary
-    int key_range = 0, n_key_ranges = 0;       // keys of a range of the row statistics
-    int row_range = 0, n_row_ranges = 0;       // rows of a range of the column sums
-    int n_row_blocks = 0, n_key_blocks = 0;
-    int part_pitch = 0;
-};
+struct AccumPlan;                          // accumulate_plan.h
 AccumPlan accumulate_plan(const Geom& g, const int32_t* seqlens_host, const int32_t* queries_host, int n_items);
-bool accumulate_supported(const Geom& g, const AccumPlan& p);
 size_t accumulate_stats_bytes(const AccumPlan& p);       // none of it is used where the log-sum-exp is given
 size_t accumulate_parts_bytes(const Geom& g, const AccumPlan& p);
 hipError_t launch_accumulate(const Geom& g, const AccumPlan& p, const void* q, const void* k, const int32_t* cu_seqlens,

@@ -5,10 +5,10 @@
 #pragma once
 
 #include "common.h"
+#include "quad_transpose.h"
 
 namespace audiokv {
 
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
@@ -48,6 +48,29 @@ __device__ __forceinline__ void put_tile(__bf16* tile, const u32x4 (&piece)[N]) 
 template <int D>
 __device__ __forceinline__ bf16x8 fragment(const __bf16* tile, int row, int kk, int hf) {
     return *reinterpret_cast<const bf16x8*>(tile + row * D + slot_of(2 * kk + hf, row) * 8);
+}
+
+// The fragments of the lane's row of 32 (lane & 31), kk as above, straight from global memory: row(i) is where row i begins. Load
+// i of a quad of lanes takes row i of its four rows, lane q of the quad the pieces of k-steps q, q + 4, ...: whole cache lines,
+// where lanes that load their own rows touch a line for every 32 bytes. The quad then exchanges its pieces.
+// (The exchange needs registers beside the fragments: where these are 128, NB = 2 sets of d = 256, lanes load their own rows.)
+template <int D, int NB, class Row>
+__device__ __forceinline__ void load_fragments(bf16x8 (&f)[D / 16], Row row) {
+    const int lane = threadIdx.x & 63, hf = lane >> 5;
+    if constexpr (D * NB > 256) {
+        const __bf16* src = row(lane & 31) + hf * 8;
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) f[kk] = *reinterpret_cast<const bf16x8*>(src + kk * 16);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __bf16* src = row((lane & 28) + i) + (lane & 3) * 16 + hf * 8;
+#pragma unroll
+        for (int kq = 0; kq < D / 16; kq += 4) f[kq + i] = *reinterpret_cast<const bf16x8*>(src + kq * 16);
+    }
+#pragma unroll
+    for (int kq = 0; kq < D / 16; kq += 4) quad_transpose(f[kq], f[kq + 1], f[kq + 2], f[kq + 3], lane);
 }
 
 }  // namespace mfma_tile
