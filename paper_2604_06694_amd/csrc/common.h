@@ -154,7 +154,8 @@ hipError_t launch_accumulate(const Geom& g, const AccumPlan& p, const void* q, c
 
 // one decoding step of sequences that share compacted caches (shared.hip)
 struct SharedPlan {
-    int log_r = 0, row_blocks = 0;             // prompts: rows of a chunk (a power of two), blocks of query rows
+    int log_r = 0;                             // prompts: rows of a chunk (a power of two)
+    int row_block = 0, row_blocks = 0;         // query rows of a workgroup, blocks of them
     long long slots = 0;                       // of chunks: every head leaves at most one empty
     int own_chunk = 0, own_chunks = 0;         // own rows: of a chunk, chunks of a head
     int logit_pitch = 0;

@@ -29,8 +29,14 @@ namespace {
 
 using namespace mfma_tile;
 
-constexpr int kTile = 64;                     // keys of a tile
-constexpr int kRowBlock = 32 * kWaves;        // query rows of a workgroup
+// At d = 256 tiles are half as long and a wave's accumulators half the channels (two waves then share their rows): so that two
+// workgroups share a CU there, too.
+template <int D> struct Shape {
+    static constexpr int kTile = D == 256 ? 32 : 64;              // keys of a tile
+    static constexpr int kSplit = D == 256 ? 2 : 1;               // waves that share 32 rows, each its part of the channels
+    static constexpr int kRowWaves = kWaves / kSplit;             // 32 rows each
+};
+int max_row_block(int D) { return D == 256 ? 64 : 128; }          // query rows of a workgroup
 
 struct Shared {
     Geom g;
@@ -39,7 +45,7 @@ struct Shared {
     const int32_t* cu_b;
     const int32_t* cu_seqs;
     int n_items, total_rows, n_seqs, max_seqs;
-    int log_r, slots, slots_pad, row_blocks;  // prompt chunks; slots_pad: a multiple of 8, so that a chunk stays on one XCD
+    int log_r, slots, slots_pad, row_block, row_blocks;  // prompt chunks; slots_pad: a multiple of 8, so that a chunk stays on one XCD
     __bf16 *ko, *vo;                          // own rows
     int32_t* lengths;
     int32_t* positions;
@@ -58,27 +64,41 @@ struct Shared {
 __device__ __forceinline__ int head_start(const Shared& a, int g) { return min(a.cu_b[g], a.total_rows); }
 __device__ __forceinline__ int first_slot(const Shared& a, int g) { return (head_start(a, g) >> a.log_r) + g; }
 
-// The last of n entries of a rising table whose value is not past v (64 entries probed at a time, one per lane); the first is not.
+// The last of n entries of a rising table of n + 1 whose value is not past v; the first is not. Tables of up to 63 entries are
+// loaded at once, an entry per lane, and what follows is read from the lanes: one latency. Of longer ones 64 entries are probed at
+// a time.
+struct Entry {
+    int at, value, next;       // the entry, its value and that of the one behind
+};
 template <typename Value>
-__device__ __forceinline__ int last_at_or_before(int n, int v, Value value) {
+__device__ __forceinline__ Entry last_at_or_before(int n, int v, Value value) {
+    const int lane = threadIdx.x & 63;
+    if (n < 64) {
+        const int mine = value(min(lane, n));
+        const int at = max(__builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < n && mine <= v)) - 1, 0);
+        return Entry{at, __builtin_amdgcn_readlane(mine, at), __builtin_amdgcn_readlane(mine, at + 1)};
+    }
     int at = 0;
     for (int span = n; span > 1;) {
-        const int step = (span + 63) >> 6, probe = at + (int)(threadIdx.x & 63) * step;
+        const int step = (span + 63) >> 6, probe = at + lane * step;
         const bool before = probe < at + span && value(min(probe, n - 1)) <= v;
         const int found = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
         const int skip = found > 0 ? (found - 1) * step : 0;
         at += skip;
         span = min(step, span - skip);
     }
-    return __builtin_amdgcn_readfirstlane(at);
+    at = __builtin_amdgcn_readfirstlane(at);
+    return Entry{at, value(at), value(at + 1)};
 }
 
-// The item that sequence x continues, or -1: it takes no part. (Without prompts all take part, as item 0.)
-__device__ __forceinline__ int item_of(const Shared& a, int x) {
-    if (!a.cu_seqs) return 0;
-    if (x < a.cu_seqs[0] || x >= a.cu_seqs[a.n_items]) return -1;
-    const int i = last_at_or_before(a.n_items, x, [&](int e) { return a.cu_seqs[e]; });
-    return x - a.cu_seqs[i] < a.max_seqs ? i : -1;
+// The item that sequence x continues and its first sequence; item -1: x takes no part. (Without prompts all take part, as item 0.)
+struct ItemOf {
+    int item, first;
+};
+__device__ __forceinline__ ItemOf item_of(const Shared& a, int x) {
+    if (!a.cu_seqs) return ItemOf{0, 0};
+    const Entry e = last_at_or_before(a.n_items, x, [&](int i) { return a.cu_seqs[i]; });
+    return ItemOf{x >= e.value && x < e.next && x - e.value < a.max_seqs ? e.at : -1, e.value};
 }
 
 // What a workgroup attends to
@@ -93,131 +113,162 @@ struct Rows {
 };
 
 template <int D>
-__device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int first_seq, int h, int M, int r_first, float* part, float2* stats)
+__device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int first_seq, int h, int r_first, int r_end, float* part, float2* stats)
 {
-    constexpr int KK = D / 16, CT = D / 32, N = kPieces<D, kTile>;
+    typedef Shape<D> W;
+    constexpr int KK = D / 16, CT = D / 32 / W::kSplit, kTile = W::kTile, N = kPieces<D, kTile>;
     __shared__ __attribute__((aligned(16))) __bf16 tile[2][2][kTile * D];     // [buffer][K, V]
-    __shared__ float2 joint[2][64];
+    __shared__ float2 joint[kWaves][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5, col = lane & 31;
     const int G = a.g.G;
-    // waves over query rows, and over the two halves of a tile's keys
-    const int left = M - r_first, wq_n = left <= 32 ? 1 : left <= 64 ? 2 : 4;
-    const int wq = wave % wq_n, wk = wave / wq_n;
-    const bool works = wk < 2;
-    const int sub0 = wq_n == 4 ? 0 : wk, sub1 = wq_n == 4 ? kTile / 32 : wk + 1;
+    // waves over query rows, and, where these leave some and a tile has two, over its halves
+    const int left = r_end - r_first, wq_n = left <= 32 ? 1 : left <= 64 || W::kRowWaves == 2 ? 2 : 4;
+    const int part_of = wave % W::kSplit, wq = wave / W::kSplit % wq_n, wk = wave / W::kSplit / wq_n;
+    const bool halves = kTile > 32 && wq_n < 4, works = wk < (halves ? 2 : 1);
+    const int sub0 = halves ? wk : 0, sub1 = halves ? wk + 1 : kTile / 32;
+    const int r_wave = r_first + wq * 32;
 
-    const int r = r_first + wq * 32 + col, rc = min(r, M - 1);
-    const __bf16* qsrc = a.q + ((int64_t)(first_seq + rc / G) * a.g.H_q + h * G + rc % G) * D + hf * 8;
-    bf16x8 qf[KK];
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qsrc + kk * 16);
-
+    // A tile's first row is uniform, and so is the distance to the rows of a thread's next piece.
     const int chunk = piece_chunk<D>() * 8;
+    const int64_t apart = piece_row<D>(0) * rows.stride + chunk;
+    constexpr int kStep = kThreads / (D / 8);
     u32x4 kpiece[N], vpiece[N];
+    auto plain = [&](int t) { return t + kTile <= rows.n && (rows.fresh < t || rows.fresh >= t + kTile); };
     auto fetch = [&](int t) {
+        if (plain(t)) {
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            const int j = t + piece_row<D>(u);
-            const int64_t at = (int64_t)min(j, rows.n - 1) * rows.stride + chunk;
-            kpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.k_new + chunk : rows.k + at);
-            vpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.v_new + chunk : rows.v + at);
+            for (int u = 0; u < N; ++u) {
+                const int64_t first = (t + u * kStep) * rows.stride;
+                kpiece[u] = *reinterpret_cast<const u32x4*>(rows.k + first + apart);
+                vpiece[u] = *reinterpret_cast<const u32x4*>(rows.v + first + apart);
+            }
+        } else {
+#pragma unroll
+            for (int u = 0; u < N; ++u) {
+                const int j = t + piece_row<D>(u);
+                const int64_t at = min(j, rows.n - 1) * rows.stride + chunk;
+                kpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.k_new + chunk : rows.k + at);
+                vpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.v_new + chunk : rows.v + at);
+            }
         }
     };
     auto put = [&](int t, int buffer) {
+        if (!plain(t)) {
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
-            const int j = t + piece_row<D>(u);
-            if (j == rows.fresh) {
-                *reinterpret_cast<u32x4*>(rows.k_dst + chunk) = kpiece[u];
-                *reinterpret_cast<u32x4*>(rows.v_dst + chunk) = vpiece[u];
+            for (int u = 0; u < N; ++u) {
+                const int j = t + piece_row<D>(u);
+                if (j == rows.fresh) {                        // the new row takes its slot
+                    *reinterpret_cast<u32x4*>(rows.k_dst + chunk) = kpiece[u];
+                    *reinterpret_cast<u32x4*>(rows.v_dst + chunk) = vpiece[u];
+                }
+                // rows past the end have weight 0, but 0 times an infinity is NaN
+                vpiece[u] = j < rows.n ? vpiece[u] : u32x4{0, 0, 0, 0};
             }
-            // rows past the end have weight 0, but 0 times an infinity is NaN
-            vpiece[u] = j < rows.n ? vpiece[u] : u32x4{0, 0, 0, 0};
         }
         put_tile<D>(tile[buffer][0], kpiece);
         put_tile<D>(tile[buffer][1], vpiece);
     };
 
+    fetch(0);
+    bf16x8 qf[KK];
+    load_fragments<D, 1>(qf, [&](int i) {
+        const int rc = min(r_wave + i, r_end - 1);
+        return a.q + ((int64_t)(first_seq + rc / G) * a.g.H_q + h * G + rc % G) * D;
+    });
     f32x16 acc[CT] = {};
     float m = -INFINITY, l = 0.f;
     // the transposing read: sixteen lanes take four keys x sixteen channels, each lane then holds a channel's four keys
     const int tr_key = 4 * hf + ((lane & 15) >> 2), tr_chunk = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), tr_low = (lane & 1) * 4;
-    auto values = [&](const __bf16* v, int key0, int ct) {
-        const int row = key0 + tr_key;
-        const __bf16* at = v + row * D + slot_of(ct * 4 + tr_chunk, row) * 8 + tr_low;
-        typedef __attribute__((ext_vector_type(4))) short s16x4;
-        typedef __attribute__((address_space(3))) s16x4* lds_ptr;
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)const_cast<__bf16*>(at));
+    typedef __attribute__((ext_vector_type(4))) short s16x4;
+    auto values = [&](const __bf16* v, int key0, int ct) {       // sixteen keys of 32 channels
+        s16x4 four[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int row = key0 + e * 8 + tr_key;
+            const __bf16* at = v + row * D + slot_of((part_of * CT + ct) * 4 + tr_chunk, row) * 8 + tr_low;
+            typedef __attribute__((address_space(3))) s16x4* lds_ptr;
+            four[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)const_cast<__bf16*>(at));
+        }
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(four[0], four[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
 
-    fetch(0);
     put(0, 0);
     __syncthreads();
     for (int t = 0, at = 0; t < rows.n; t += kTile, at ^= 1) {
         if (t + kTile < rows.n) fetch(t + kTile);
         __builtin_amdgcn_sched_barrier(0);
-        if (works) {
-            for (int s = sub0; s < sub1; ++s) {
-                const int key0 = t + s * 32;
-                if (key0 >= rows.n) break;
-                f32x16 z = {};
+        for (int s = sub0; works && s < sub1 && t + s * 32 < rows.n; ++s) {
+            const int key0 = t + s * 32;
+            // Fragments are requested four k-steps ahead of their MFMA, those of V for the first sixteen keys in front of the
+            // exponentials: left alone the compiler waits for each in turn.
+            const __bf16 *kt = tile[at][0] + s * 32 * D, *vt = tile[at][1] + s * 32 * D;
+            f32x16 z = {};
+            bf16x8 kf[4];
 #pragma unroll
-                for (int kk = 0; kk < KK; ++kk)
-                    z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fragment<D>(tile[at][0], s * 32 + col, kk, hf), qf[kk], z, 0, 0, 0);
-                if (key0 + 32 > rows.n) {
+            for (int kk = 0; kk < 4; ++kk) kf[kk] = fragment<D>(kt, col, kk, hf);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) z[i] = key0 + key_of(i, hf) < rows.n ? z[i] : -INFINITY;
-                }
-                if (rows.logits && col < G) {
-                    float* dst = rows.logits + (int64_t)col * a.logit_pitch + key0 + 4 * hf;
+            for (int kk = 0; kk < KK; ++kk) {
+                z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk % 4], qf[kk], z, 0, 0, 0);
+                if (kk + 4 < KK) kf[kk % 4] = fragment<D>(kt, col, kk + 4, hf);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            bf16x8 vf[CT];
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4)
-                        *reinterpret_cast<f32x4*>(dst + 2 * i) =
-                            f32x4{z[i] * a.g.c_log2, z[i + 1] * a.g.c_log2, z[i + 2] * a.g.c_log2, z[i + 3] * a.g.c_log2};
-                }
-                float p[16], sum = 0.f;
+            for (int ct = 0; ct < CT; ++ct) vf[ct] = values(vt, 0, ct);
+            __builtin_amdgcn_sched_barrier(0);
+            if (key0 + 32 > rows.n) {
+                const int most = rows.n - key0 - 4 * hf;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = key_of(i, 0) < most ? z[i] : -INFINITY;
+            }
+            if (rows.logits && col < G && part_of == 0) {
+                float* dst = rows.logits + (int64_t)col * a.logit_pitch + key0 + 4 * hf;
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    *reinterpret_cast<f32x4*>(dst + 2 * i) =
+                        f32x4{z[i] * a.g.c_log2, z[i + 1] * a.g.c_log2, z[i + 2] * a.g.c_log2, z[i + 3] * a.g.c_log2};
+            }
+            float p[16], sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                p[i] = fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -m));
+                sum += p[i];
+            }
+            const bool far = !(sum < 0x1p10f);
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
+                float top = z[0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
+                top = fmaxf(top, __shfl_xor(top, 32, 64));
+                const int theirs = __shfl_xor((int)far, 32, 64);       // (in front of the test: all lanes take part)
+                const bool redo = far | (theirs != 0);
+                const float ref = redo ? fmaxf(m, top * a.g.c_log2) : m, ref0 = ref == -INFINITY ? 0.f : ref;
+                const float by = redo ? fast_exp2(m - ref0) : 1.f;
+                sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    p[i] = fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -m));
+                    p[i] = fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -ref0));
                     sum += p[i];
                 }
-                const bool far = !(sum < 0x1p10f);
-                if (__builtin_expect(__builtin_amdgcn_ballot_w64(far) != 0, 0)) {
-                    float top = z[0];
+                l *= by;
 #pragma unroll
-                    for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
-                    top = fmaxf(top, __shfl_xor(top, 32, 64));
-                    const int theirs = __shfl_xor((int)far, 32, 64);       // (in front of the test: all lanes take part)
-                    const bool redo = far | (theirs != 0);
-                    const float ref = redo ? fmaxf(m, top * a.g.c_log2) : m, ref0 = ref == -INFINITY ? 0.f : ref;
-                    const float by = redo ? fast_exp2(m - ref0) : 1.f;
-                    sum = 0.f;
+                for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        p[i] = fast_exp2(__builtin_fmaf(z[i], a.g.c_log2, -ref0));
-                        sum += p[i];
-                    }
-                    l *= by;
+                    for (int i = 0; i < 16; ++i) acc[ct][i] *= by;
+                m = ref;
+            }
+            l += sum;
 #pragma unroll
-                    for (int ct = 0; ct < CT; ++ct)
+            for (int kb = 0; kb < 2; ++kb) {
+                bf16x8 pf;
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[ct][i] *= by;
-                    m = ref;
-                }
-                l += sum;
+                for (int e = 0; e < 8; ++e) pf[e] = (__bf16)p[kb * 8 + e];
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    bf16x8 pf;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) pf[e] = (__bf16)p[kb * 8 + e];
-#pragma unroll
-                    for (int ct = 0; ct < CT; ++ct) {
-                        typedef __attribute__((ext_vector_type(4))) short s16x4;
-                        typedef __attribute__((ext_vector_type(8))) short s16x8;
-                        const s16x4 lo = values(tile[at][1], s * 32 + kb * 16, ct), hi = values(tile[at][1], s * 32 + kb * 16 + 8, ct);
-                        const s16x8 both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                        acc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, both), pf, acc[ct], 0, 0, 0);
-                    }
+                for (int ct = 0; ct < CT; ++ct) {
+                    acc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ct], pf, acc[ct], 0, 0, 0);
+                    if (kb == 0) vf[ct] = values(vt, 16, ct);
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
@@ -226,66 +277,78 @@ __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int fi
         __syncthreads();
     }
 
+    // A lane has every second group of four channels of one row: rows are put together in LDS (where the tiles were), so that whole
+    // ones are stored, and where a second wave had the other half of the keys it hands its share over there. Groups of four are
+    // rotated by the row.
+    constexpr int kGroups = CT * 8;
+    f32x4* mine = reinterpret_cast<f32x4*>(&tile[0][0][0]) + (wq * W::kSplit + part_of) * (32 * kGroups);
+    auto group = [&](int ct, int i) { return col * kGroups + ((ct * 8 + i / 2 + hf) ^ (col & 15)); };
     l += __shfl_xor(l, 32, 64);
-    if (wq_n < 4) {                                           // uniform: the second half of the keys joins the first
-        f32x4* xch = reinterpret_cast<f32x4*>(&tile[0][0][0]) + wq * (CT * 4 * 64) + lane;
+    if (halves) {                                             // uniform
         if (wk == 1) {
             joint[wq][lane] = make_float2(m, l);
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    xch[(ct * 4 + i / 4) * 64] = f32x4{acc[ct][i], acc[ct][i + 1], acc[ct][i + 2], acc[ct][i + 3]};
+                for (int i = 0; i < 16; i += 4) mine[group(ct, i)] = f32x4{acc[ct][i], acc[ct][i + 1], acc[ct][i + 2], acc[ct][i + 3]};
         }
         __syncthreads();
-        if (wk == 0) {
-            const float2 o = joint[wq][lane];
-            const float M2 = fmaxf(m, o.x), ref = M2 == -INFINITY ? 0.f : M2;
-            const float mine = fast_exp2(m - ref), other = fast_exp2(o.x - ref);
-            l = l * mine + o.y * other;
-            m = M2;
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const f32x4 v = xch[(ct * 4 + i / 4) * 64];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[ct][i + e] = acc[ct][i + e] * mine + v[e] * other;
-                }
-        }
     }
-    if (wk == 0 && r < M) {
-        float* dst = part + (int64_t)r * D + 4 * hf;
+    if (wk != 0) return;
+    float by = 1.f;
+    if (halves) {
+        const float2 o = joint[wq][lane];
+        const float M2 = fmaxf(m, o.x), ref = M2 == -INFINITY ? 0.f : M2;
+        by = fast_exp2(m - ref);
+        const float other = fast_exp2(o.x - ref);
+        l = l * by + o.y * other;
+        m = M2;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                *reinterpret_cast<f32x4*>(dst + ct * 32 + 2 * i) = f32x4{acc[ct][i], acc[ct][i + 1], acc[ct][i + 2], acc[ct][i + 3]};
-        if (hf == 0) stats[r] = make_float2(m, l);
+            for (int i = 0; i < 16; i += 4) {
+                const f32x4 v = mine[group(ct, i)];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[ct][i + e] = acc[ct][i + e] * by + v[e] * other;
+            }
+    }
+    if (hf == 0 && part_of == 0 && r_wave + col < r_end) stats[r_wave + col] = make_float2(m, l);
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) mine[group(ct, i)] = f32x4{acc[ct][i], acc[ct][i + 1], acc[ct][i + 2], acc[ct][i + 3]};
+    f32x4* dst = reinterpret_cast<f32x4*>(part + (int64_t)r_wave * D) + part_of * kGroups;
+    const int n_rows = min(32, r_end - r_wave);
+#pragma unroll
+    for (int e = 0; e < 32 * kGroups; e += 64) {
+        const int row = (e + lane) / kGroups, c = (e + lane) % kGroups;
+        if (row < n_rows) dst[row * (D / 4) + c] = mine[row * kGroups + (c ^ (row & 15))];
     }
 }
 
 template <int D>
-__global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void shared_partial_kernel(Shared a)
+__global__ __launch_bounds__(kThreads, 2) void shared_partial_kernel(Shared a)
 {
     const int prompt_blocks = a.slots_pad * a.row_blocks;
     Rows rows{};
     rows.fresh = -1;
-    int first_seq, h, M, r_first = 0;
+    int first_seq, h, M, r_first = 0, r_end;
     float* part;
     float2* stats;
     if ((int)blockIdx.x < prompt_blocks) {
         const int block = blockIdx.x / a.slots_pad, slot = blockIdx.x - block * a.slots_pad;
         if (slot >= a.slots) return;
-        const int head = last_at_or_before(a.n_items * a.g.H_kv, slot, [&](int e) { return first_slot(a, e); });
-        const int item = head / a.g.H_kv;
+        const int n_heads = a.n_items * a.g.H_kv;
+        const Entry e = last_at_or_before(n_heads, slot, [&](int g) { return first_slot(a, g); });
+        const int head = e.at, item = head / a.g.H_kv;
         h = head - item * a.g.H_kv;
-        const int c = slot - first_slot(a, head);
-        const int64_t row0 = head_start(a, head) + ((int64_t)c << a.log_r);
+        const int c = slot - e.value, begin = head_start(a, head);
+        const int64_t row0 = begin + ((int64_t)c << a.log_r);
         rows.n = (int)min((int64_t)1 << a.log_r, head_start(a, head + 1) - row0);
         first_seq = max(0, a.cu_seqs[item]);
         M = min(min(a.cu_seqs[item + 1], a.n_seqs) - first_seq, a.max_seqs) * a.g.G;
-        r_first = block * kRowBlock;
+        r_first = block * a.row_block;
+        r_end = min(M, r_first + a.row_block);
         if (c < 0 || rows.n <= 0 || r_first >= M) return;
         rows.k = a.kp + row0 * D;
         rows.v = a.vp + row0 * D;
@@ -297,15 +360,16 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void shared_partial_ker
         const int id = blockIdx.x - prompt_blocks, own = id / a.own_chunks, c = id - own * a.own_chunks;
         const int x = own / a.g.H_kv;
         h = own - x * a.g.H_kv;
-        if (item_of(a, x) < 0) return;
-        const int before = max(0, min(a.lengths[own], a.max_own));
+        const int length = a.lengths[own];
+        if (item_of(a, x).item < 0) return;
+        const int before = max(0, min(length, a.max_own));
         const bool appends = a.k_new != nullptr && before < a.max_own;
         const int n = before + appends, j0 = c * a.own_chunk;
         if (c == 0 && threadIdx.x == 0) a.after[own] = 2 * n + appends;
         rows.n = min(a.own_chunk, n - j0);
         if (rows.n <= 0) return;
         first_seq = x;
-        M = a.g.G;
+        M = r_end = a.g.G;
         const int64_t at = kv_row_offset(a.g, x, (int64_t)x * a.capacity, a.capacity, h, j0);
         rows.k = a.ko + at;
         rows.v = a.vo + at;
@@ -322,7 +386,7 @@ __global__ __launch_bounds__(kThreads, D == 256 ? 1 : 2) void shared_partial_ker
         stats = a.stats_o + base;
         if (a.weights) rows.logits = a.logits + (int64_t)own * a.g.G * a.logit_pitch + j0;
     }
-    attend<D>(a, rows, first_seq, h, M, r_first, part, stats);
+    attend<D>(a, rows, first_seq, h, r_first, r_end, part, stats);
 }
 
 // The chunks that a query of sequence x has rows in: first those of the prompt, then its own
@@ -332,25 +396,26 @@ struct Chunks {
     int np, no;
     __device__ __forceinline__ float2 stat(int c) const { return c < np ? sp[c * step_p] : so[(c - np) * step_o]; }
 };
-__device__ __forceinline__ Chunks chunks_of(const Shared& a, int x, int item, int h, int gq) {
+// after: of the sequence's own head h
+__device__ __forceinline__ Chunks chunks_of(const Shared& a, int x, ItemOf it, int h, int gq, int after) {
     Chunks t{a.stats_p, a.stats_o, 0, 0, 0, 0};
     if (a.cu_seqs) {
-        const int head = item * a.g.H_kv + h, n = head_start(a, head + 1) - head_start(a, head);
+        const int head = it.item * a.g.H_kv + h, begin = head_start(a, head), n = head_start(a, head + 1) - begin;
         t.np = n > 0 ? (n + (1 << a.log_r) - 1) >> a.log_r : 0;
         t.step_p = (int64_t)a.max_seqs * a.g.G;
-        t.sp = a.stats_p + first_slot(a, head) * t.step_p + (int64_t)(x - a.cu_seqs[item]) * a.g.G + gq;
+        t.sp = a.stats_p + ((begin >> a.log_r) + head) * t.step_p + (int64_t)(x - it.first) * a.g.G + gq;
     }
     if (a.own_chunks > 0) {
-        const int own = x * a.g.H_kv + h, n = a.after[own] >> 1;
-        t.no = (n + a.own_chunk - 1) / a.own_chunk;
+        t.no = ((after >> 1) + a.own_chunk - 1) / a.own_chunk;
         t.step_o = a.g.G;
-        t.so = a.stats_o + (int64_t)own * a.own_chunks * a.g.G + gq;
+        t.so = a.stats_o + (int64_t)(x * a.g.H_kv + h) * a.own_chunks * a.g.G + gq;
     }
     return t;
 }
 
-// A workgroup per query: its chunks joined. Behind those, workgroups of 256 own rows each add the rows' weights.
+// A workgroup per query: its chunks joined. Behind those, workgroups of kWeightRows own rows each add the rows' weights.
 constexpr int kJoinLds = 1024;                // chunks whose factors fit the LDS array (more: recomputed where used)
+constexpr int kWeightRows = 4 * kThreads;
 
 __global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int weight_blocks)
 {
@@ -360,14 +425,21 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int wei
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, G = a.g.G, D = a.g.D;
     const int queries = a.n_seqs * a.g.H_q;
     if ((int)blockIdx.x >= queries) {
-        const int id = blockIdx.x - queries, own = id / weight_blocks, j = (id - own * weight_blocks) * kThreads + tid;
-        const int x = own / a.g.H_kv, h = own - x * a.g.H_kv, item = item_of(a, x);
-        if (item < 0) return;
-        const int after = a.after[own], n = after >> 1;
-        if (j - tid >= n) return;
+        const int id = blockIdx.x - queries, own = id / weight_blocks, j0 = (id - own * weight_blocks) * kWeightRows;
+        const int x = own / a.g.H_kv, h = own - x * a.g.H_kv, after = a.after[own], n = after >> 1;
+        const ItemOf it = item_of(a, x);
+        if (it.item < 0 || j0 >= n) return;
+        // the logits of the first heads are on their way while the statistics are joined
+        constexpr int kRows = kWeightRows / kThreads, kEarly = 8;
+        const float* z = a.logits + (int64_t)own * G * a.logit_pitch;
+        float early[kEarly][kRows];
+#pragma unroll
+        for (int gq = 0; gq < kEarly; ++gq)
+#pragma unroll
+            for (int u = 0; u < kRows; ++u) early[gq][u] = z[(int64_t)min(gq, G - 1) * a.logit_pitch + min(j0 + u * kThreads + tid, n - 1)];
         // max + log2(sum) of the group's queries, a wave on every fourth
         for (int gq = wave; gq < G; gq += kWaves) {
-            const Chunks t = chunks_of(a, x, item, h, gq);
+            const Chunks t = chunks_of(a, x, it, h, gq, after);
             float m = -INFINITY, l = 0.f;
             for (int c = lane; c < t.np + t.no; c += 64) {
                 const float2 s = t.stat(c);
@@ -379,28 +451,33 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int wei
             for (int o = 32; o > 0; o >>= 1) {
                 const float mo = __shfl_xor(m, o, 64), lo = __shfl_xor(l, o, 64);
                 const float m2 = fmaxf(m, mo), ref = m2 == -INFINITY ? 0.f : m2;
-                // (the same order in both lanes: the sum of a pair is theirs alike)
-                const float a0 = l * fast_exp2(m - ref), a1 = lo * fast_exp2(mo - ref);
-                l = a0 + a1;
+                l = l * fast_exp2(m - ref) + lo * fast_exp2(mo - ref);
                 m = m2;
             }
             if (lane == 0) factor[gq] = l == 0.f ? INFINITY : m + __log2f(l);
         }
         __syncthreads();
-        if (j >= n) return;
-        const float* z = a.logits + (int64_t)own * G * a.logit_pitch + j;
-        float w = 0.f;
-#pragma unroll 8
-        for (int gq = 0; gq < G; ++gq) w += fast_exp2(z[(int64_t)gq * a.logit_pitch] - factor[gq]);
-        float* dst = a.weights + (int64_t)own * a.capacity + j;
-        *dst = (after & 1) && j == n - 1 ? w : *dst + w;      // the appended row begins at nothing
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) {
+            const int j = j0 + u * kThreads + tid;
+            if (j >= n) break;
+            float w = 0.f;
+#pragma unroll
+            for (int gq = 0; gq < kEarly; ++gq)
+                if (gq < G) w += fast_exp2(early[gq][u] - factor[gq]);
+            for (int gq = kEarly; gq < G; ++gq) w += fast_exp2(z[(int64_t)gq * a.logit_pitch + j] - factor[gq]);
+            float* dst = a.weights + (int64_t)own * a.capacity + j;
+            *dst = (after & 1) && j == n - 1 ? w : *dst + w;  // the appended row begins at nothing
+        }
         return;
     }
-    const int x = blockIdx.x / a.g.H_q, hq = blockIdx.x - x * a.g.H_q, h = hq / G, gq = hq - h * G, item = item_of(a, x);
-    if (item < 0) return;
-    const Chunks t = chunks_of(a, x, item, h, gq);
-    if (gq == 0 && a.own_chunks > 0 && tid == 0) {
-        const int own = x * a.g.H_kv + h, after = a.after[own];
+    const int x = blockIdx.x / a.g.H_q, hq = blockIdx.x - x * a.g.H_q, h = hq / G, gq = hq - h * G;
+    const int after = a.own_chunks > 0 ? a.after[x * a.g.H_kv + h] : 0;      // (of a sequence that takes no part: anything)
+    const ItemOf it = item_of(a, x);
+    if (it.item < 0) return;
+    const Chunks t = chunks_of(a, x, it, h, gq, after);
+    if (gq == 0 && tid == 0) {
+        const int own = x * a.g.H_kv + h;
         if (after & 1) {
             a.lengths[own] = after >> 1;
             if (a.positions) a.positions[(int64_t)own * a.capacity + (after >> 1) - 1] = a.pos_new[x];
@@ -456,6 +533,11 @@ inline size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
 }  // namespace
 
+// Workgroups that a call's prompts, and own rows, are cut for at least, where they are long enough. A prompt's chunk costs a result per
+// query, 512 bytes written and read at d = 128: few, long ones (32 sequences on 13107 rows, 4 heads: chunks of 128, 256 and 512 rows
+// 32 + 13, 24 + 10 and 23 + 8 us). Own rows: 48 caches of up to 4096 rows, 4 heads, 1024 workgroups 43 us, 2048 39.
+constexpr int kPromptBlocks = 192, kOwnBlocks = 2048;
+
 // How a call is cut. Pure function of its sizes, so that the workspace query and the launch agree. The workspace never shrinks as
 // total_rows or max_own grow: one that is sized for the largest step serves the smaller ones.
 SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_seqs, int max_seqs, int max_own)
@@ -463,8 +545,9 @@ SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_s
     SharedPlan p;
     long long slots = 0, chunks = 0;            // what the workspace is charged
     if (n_items > 0) {
-        p.row_blocks = (int)(((long long)max_seqs * g.G + kRowBlock - 1) / kRowBlock);
-        const long long wanted = (512 + p.row_blocks - 1) / p.row_blocks;     // chunks: two workgroups per CU
+        p.row_block = max_row_block(g.D);
+        p.row_blocks = (int)(((long long)max_seqs * g.G + p.row_block - 1) / p.row_block);
+        const long long wanted = (kPromptBlocks + p.row_blocks - 1) / p.row_blocks;
         p.log_r = 7;
         while (p.log_r < 16 && (total_rows >> (p.log_r + 1)) >= wanted) ++p.log_r;
         p.slots = (total_rows >> p.log_r) + (long long)n_items * g.H_kv;
@@ -474,11 +557,11 @@ SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_s
     if (max_own > 0) {
         const long long heads = (long long)n_seqs * g.H_kv;
         chunks = (max_own + 127) / 128;
-        const long long most = (1024 + heads - 1) / heads;
+        const long long most = (kOwnBlocks + heads - 1) / heads;
         if (chunks > most) chunks = most;
-        p.own_chunk = (int)(((max_own + chunks - 1) / chunks + kTile - 1) / kTile * kTile);
+        p.own_chunk = (int)(((max_own + chunks - 1) / chunks + 63) / 64 * 64);
         p.own_chunks = (max_own + p.own_chunk - 1) / p.own_chunk;
-        p.logit_pitch = (max_own + kTile - 1) / kTile * kTile;
+        p.logit_pitch = (max_own + 63) / 64 * 64;
     }
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
@@ -516,6 +599,7 @@ hipError_t launch_shared(const Geom& g, const SharedPlan& p, const SharedCall& c
     a.log_r = p.log_r;
     a.slots = (int)p.slots;
     a.slots_pad = (int)((p.slots + 7) / 8 * 8);
+    a.row_block = p.row_block;
     a.row_blocks = p.row_blocks;
     a.ko = static_cast<__bf16*>(c.k_own);
     a.vo = static_cast<__bf16*>(c.v_own);
@@ -549,7 +633,7 @@ hipError_t launch_shared(const Geom& g, const SharedPlan& p, const SharedCall& c
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const int weight_blocks = c.weights ? (c.max_own + kThreads - 1) / kThreads : 0;
+    const int weight_blocks = c.weights ? (c.max_own + kWeightRows - 1) / kWeightRows : 0;
     hipLaunchKernelGGL(shared_join_kernel, dim3((unsigned)(c.n_seqs * g.H_q + c.n_seqs * g.H_kv * weight_blocks)), threads, 0, s, a,
                        weight_blocks);
     return hipGetLastError();
