@@ -78,6 +78,17 @@ class Params:
     kv_stride_head: int = 0
     kv_stride_tok: int = 0
 
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_kept", None)
+
+    def _c(self) -> _CParams:
+        """c(), kept until a field is set: the struct is only read."""
+        kept = self.__dict__.get("_kept")
+        if kept is None:
+            kept = self.__dict__["_kept"] = self.c()
+        return kept
+
     def key(self) -> tuple:
         return (self.n_q_heads, self.n_kv_heads, self.head_dim, self.window, self.pool_kernel, self.pool_mode,
                 self.causal, self.kv_layout, self.softmax_scale, self.floor_frac, self.cutoff_mode, self.taper_bins,
@@ -100,12 +111,22 @@ class Slots:
     weights: Optional[torch.Tensor] = None   # fp32 [n_seqs * n_kv_heads, capacity]
     positions: Optional[torch.Tensor] = None # int32, the same
 
-    def c(self, p: Params, n_seqs: int) -> _CSlots:
-        """The C struct, after a look at types and sizes."""
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        self.__dict__.pop("_kept", None)
+
+    def _c(self, p: Params, n_seqs: int) -> _CSlots:
+        """The C struct. Types and sizes are looked at once for the same tensors and heads (a step is a few microseconds of
+        the host's, and this look three)."""
+        w, pos = self.weights, self.positions
+        where = (self.k.data_ptr(), self.v.data_ptr(), self.lengths.data_ptr(), None if w is None else w.data_ptr(),
+                 None if pos is None else pos.data_ptr(), n_seqs, p.n_kv_heads, p.head_dim, p.kv_stride_tok)
+        kept = self.__dict__.get("_kept")
+        if kept is not None and kept[0] == where:
+            return kept[1]
         heads = n_seqs * p.n_kv_heads
-        for name, t, dtype, n in (("lengths", self.lengths, torch.int32, heads),
-                                  ("weights", self.weights, torch.float32, heads * self.capacity),
-                                  ("positions", self.positions, torch.int32, heads * self.capacity)):
+        for name, t, dtype, n in (("lengths", self.lengths, torch.int32, heads), ("weights", w, torch.float32, heads * self.capacity),
+                                  ("positions", pos, torch.int32, heads * self.capacity)):
             if t is not None and _need(t, dtype, "slots." + name).numel() < n:
                 raise ValueError(f"slots.{name} has {t.numel()} values, {n} needed")
         for name, t in (("k", self.k), ("v", self.v)):
@@ -113,8 +134,9 @@ class Slots:
                 raise ValueError(f"slots.{name} must be a device tensor of dtype {torch.bfloat16}")
             if p.kv_stride_tok == 0 and _need(t, torch.bfloat16, "slots." + name).numel() < heads * self.capacity * p.head_dim:
                 raise ValueError(f"slots.{name} has {t.numel()} values, {heads * self.capacity * p.head_dim} needed")
-        return _CSlots(C.sizeof(_CSlots), self.capacity, _ptr(self.k), _ptr(self.v), _ptr(self.lengths), _ptr(self.weights),
-                       _ptr(self.positions))
+        c = _CSlots(C.sizeof(_CSlots), self.capacity, *where[:5])
+        self.__dict__["_kept"] = (where, c)
+        return c
 
 
 def lib_path() -> str:
@@ -532,10 +554,9 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
     if ws is None:
         ws = torch.empty(max(decode_shared_workspace_bytes(p, n_items, total_rows, n_seqs, max_seqs, max_own if slots else 0), 256),
                          dtype=torch.uint8, device=dev)
-    cp = p.c()
-    cs = slots.c(p, n_seqs) if slots is not None else None
-    _check(_lib.audiokv_decode_shared(C.byref(cp), _ptr(q), _ptr(k_prompt), _ptr(v_prompt), _ptr(cu_budgets), n_items, int(total_rows),
-                                      _ptr(cu_seqs), n_seqs, int(max_seqs), C.byref(cs) if cs is not None else None, int(max_own),
+    cs = C.byref(slots._c(p, n_seqs)) if slots is not None else None
+    _check(_lib.audiokv_decode_shared(C.byref(p._c()), _ptr(q), _ptr(k_prompt), _ptr(v_prompt), _ptr(cu_budgets), n_items, int(total_rows),
+                                      _ptr(cu_seqs), n_seqs, int(max_seqs), cs, int(max_own),
                                       _ptr(k_new), _ptr(v_new), _ptr(pos_new), _ptr(out), _ptr(ws), ws.numel(), _stream()))
     return out
 
@@ -557,8 +578,7 @@ def evict_accumulated(p: Params, slots: Slots, n_seqs: int, budget: int, recent:
     if ws is None:
         ws = torch.empty(max(evict_accumulated_workspace_bytes(p, n_seqs, max_own, budget), 256), dtype=torch.uint8,
                          device=slots.lengths.device)
-    cp, cs = p.c(), slots.c(p, n_seqs)
-    _check(_lib.audiokv_evict_accumulated(C.byref(cp), C.byref(cs), int(n_seqs), int(budget), _ptr(budgets), int(recent), int(max_own),
+    _check(_lib.audiokv_evict_accumulated(C.byref(p._c()), C.byref(slots._c(p, n_seqs)), int(n_seqs), int(budget), _ptr(budgets), int(recent), int(max_own),
                                           _ptr(ws), ws.numel(), _stream()))
 
 

@@ -16,7 +16,8 @@ namespace audiokv {
 
 namespace {
 
-constexpr int kLdsRanks = 8192;       // rows whose ranks are kept in LDS (of more, they are worked out again where needed)
+constexpr int kRun = 8;               // slots that a thread keeps in registers
+constexpr int kLdsMoves = 1024 * kRun / 2;    // moves that are paired up in LDS: all of a head's whose slots are in registers
 constexpr int kOneByOne = 8;          // rows too many that are found one by one
 constexpr int kFewMoves = 256;        // moves that the ranking workgroup makes itself
 constexpr int kDigit = 11, kBins = 1 << kDigit;
@@ -77,33 +78,50 @@ __device__ __forceinline__ void move_piece(const EvictAccum& a, int x, int h, in
     *reinterpret_cast<u32x4*>(cache + to) = *reinterpret_cast<const u32x4*>(cache + from);
 }
 
-template <int THREADS>
+// REGS: max_own <= THREADS * kRun, slots in registers; otherwise they are read again where needed
+template <int THREADS, bool REGS>
 __global__ __launch_bounds__(THREADS) void evict_rank_kernel(EvictAccum a)
 {
-    constexpr int WAVES = THREADS / 64;
-    __shared__ unsigned ranks[kLdsRanks];
-    __shared__ int bins[kBins];
-    __shared__ int2 few[kFewMoves];
+    constexpr int WAVES = THREADS / 64, MOVES = REGS ? THREADS * kRun / 2 : kFewMoves;
+    static_assert(MOVES <= kLdsMoves);
+    __shared__ int bins[2][kBins];
+    __shared__ int digit_total[2][WAVES], wave_count[2][REGS ? kRun * WAVES : 1];
+    __shared__ int holes_at[MOVES], movers_at[MOVES];
     __shared__ Scan<THREADS> scan;
     __shared__ int wave_top[WAVES];
     __shared__ unsigned long long wave_min[2][WAVES];
     __shared__ int found[2];
     const int head = blockIdx.x, x = head / a.g.H_kv, h = head - x * a.g.H_kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    float* w = a.weights + (int64_t)head * a.capacity;
+    int32_t* pos = a.positions ? a.positions + (int64_t)head * a.capacity : nullptr;
     const int n = a.lengths[head], b = a.budgets ? max(a.budget, a.budgets[head]) : a.budget;
+    float wv[REGS ? kRun : 1];
+    int pv[REGS ? kRun : 1];
+    if constexpr (REGS) {                                         // (slots up to max_own, whatever the length turns out to be)
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) wv[e] = w[min(e * THREADS + tid, a.max_own - 1)];
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) pv[e] = a.recent > 0 ? pos[min(e * THREADS + tid, a.max_own - 1)] : 0;
+    }
     int32_t* listed = a.moves ? a.moves + (int64_t)head * (1 + 2 * a.max_moves) : nullptr;
     if (n <= b || n > a.max_own) {
         if (listed && tid == 0) listed[0] = 0;
         return;
     }
-    float* w = a.weights + (int64_t)head * a.capacity;
-    int32_t* pos = a.positions ? a.positions + (int64_t)head * a.capacity : nullptr;
+    // slots in registers: every THREADS-th; otherwise a run of them
+    const int run = (n + THREADS - 1) / THREADS, t0 = min(tid * run, n), t1 = min(t0 + run, n);
 
     // positions above `old` are recent (64 bits: newest - recent may pass the smallest int)
     int64_t old = INT64_MAX;
     if (a.recent > 0) {
         int top = INT_MIN;
-        for (int t = tid; t < n; t += THREADS) top = max(top, pos[t]);
+        if constexpr (REGS) {
+#pragma unroll
+            for (int e = 0; e < kRun; ++e) top = e * THREADS + tid < n ? max(top, pv[e]) : top;
+        } else {
+            for (int t = t0; t < t1; ++t) top = max(top, pos[t]);
+        }
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) top = max(top, __shfl_xor(top, o, 64));
         if (lane == 0) wave_top[wave] = top;
@@ -112,26 +130,34 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(EvictAccum a)
         for (int i = 0; i < WAVES; ++i) top = max(top, wave_top[i]);
         old = (int64_t)top - a.recent;
     }
-    const bool kept_ranks = n <= kLdsRanks;
-    auto fresh_rank = [&](int t) { return a.recent > 0 && (int64_t)pos[t] > old ? 0xffffffffu : rank_of(w[t]); };
-    if (kept_ranks) {
-        for (int t = tid; t < n; t += THREADS) ranks[t] = fresh_rank(t);
-        __syncthreads();
+    unsigned ranks[REGS ? kRun : 1];
+    if constexpr (REGS) {
+#pragma unroll
+        for (int e = 0; e < kRun; ++e) ranks[e] = a.recent > 0 && (int64_t)pv[e] > old ? 0xffffffffu : rank_of(wv[e]);
     }
-    auto rank = [&](int t) { return kept_ranks ? ranks[t] : fresh_rank(t); };
+    // f(slot, rank) for the thread's slots in order
+    auto each = [&](auto f) {
+        if constexpr (REGS) {
+#pragma unroll
+            for (int e = 0; e < kRun; ++e)
+                if (e * THREADS + tid < n) f(e * THREADS + tid, ranks[e]);
+        } else {
+            for (int t = t0; t < t1; ++t) f(t, a.recent > 0 && (int64_t)pos[t] > old ? 0xffffffffu : rank_of(w[t]));
+        }
+    };
 
     const int gone = n - b;
     int moves = 0;
     if (gone <= kOneByOne) {
         // the next one to go: the smallest (rank, slots from the end) above the one before
         unsigned long long last = 0;
-        unsigned out[kOneByOne];
+        int out[kOneByOne];
         for (int e = 0; e < gone; ++e) {
             unsigned long long least = ~0ull;
-            for (int t = tid; t < n; t += THREADS) {
-                const unsigned long long v = ((unsigned long long)rank(t) << 32) | (unsigned)(INT_MAX - t);
+            each([&](int t, unsigned r) {
+                const unsigned long long v = ((unsigned long long)r << 32) | (unsigned)(INT_MAX - t);
                 least = (e == 0 || v > last) && v < least ? v : least;
-            }
+            });
 #pragma unroll
             for (int o = 32; o > 0; o >>= 1) {
                 const unsigned long long v = __shfl_xor(least, o, 64);
@@ -144,7 +170,7 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(EvictAccum a)
             last = least;
 #pragma unroll
             for (int i = 0; i < kOneByOne; ++i)
-                if (i == e) out[i] = (unsigned)(INT_MAX - (int)(unsigned)least);
+                if (i == e) out[i] = INT_MAX - (int)(unsigned)least;
         }
         // holes below b in order, and the slots from b on that are none of those that go
         if (tid == 0) {
@@ -153,52 +179,49 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(EvictAccum a)
                 int next = INT_MAX;
 #pragma unroll
                 for (int i = 0; i < kOneByOne; ++i)
-                    if (i < gone && (int)out[i] > hole && (int)out[i] < next) next = (int)out[i];
+                    if (i < gone && out[i] > hole && out[i] < next) next = out[i];
                 if (next >= b) break;
                 for (bool goes = true; goes; mover += goes) {
                     goes = false;
 #pragma unroll
-                    for (int i = 0; i < kOneByOne; ++i) goes |= i < gone && (int)out[i] == mover;
+                    for (int i = 0; i < kOneByOne; ++i) goes |= i < gone && out[i] == mover;
                 }
-                if (listed) {
-                    listed[1 + 2 * moves] = next;
-                    listed[2 + 2 * moves] = mover;
-                }
-                few[moves++] = make_int2(next, mover);
+                holes_at[moves] = next;
+                movers_at[moves++] = mover++;
                 hole = next;
-                ++mover;
             }
             found[0] = moves;
         }
         __syncthreads();
         moves = found[0];
-        if (tid < moves) {
-            w[few[tid].x] = w[few[tid].y];
-            if (pos) pos[few[tid].x] = pos[few[tid].y];
-        }
     } else {
         // T: the rank of the last one to go; `left`: how many of that rank go
         unsigned T = 0;
         int left = gone;
-        for (int shift = 32 - kDigit, bits = kDigit; bits > 0;) {
-            for (int i = tid; i < (1 << bits); i += THREADS) bins[i] = 0;
-            __syncthreads();
+        for (int i = tid; i < kBins; i += THREADS) bins[0][i] = 0;
+        __syncthreads();
+        for (int shift = 32 - kDigit, bits = kDigit, pass = 0; bits > 0; pass ^= 1) {
             const unsigned mask = (1u << bits) - 1;
-            for (int t = tid; t < n; t += THREADS) {
-                const unsigned r = rank(t);
-                if (shift + bits == 32 || (r >> (shift + bits)) == (T >> (shift + bits))) atomicAdd(&bins[(r >> shift) & mask], 1);
-            }
+            int* count = bins[pass];
+            each([&](int, unsigned r) {
+                if (shift + bits == 32 || (r >> (shift + bits)) == (T >> (shift + bits))) atomicAdd(&count[(r >> shift) & mask], 1);
+            });
+            for (int i = tid; i < kBins; i += THREADS) bins[pass ^ 1][i] = 0;        // the next pass's
             __syncthreads();
             // the bin in which the `left`-th lies: threads on runs of bins
-            const int run = (1 << bits) / THREADS > 0 ? (1 << bits) / THREADS : 1;
-            int sum = 0, none = 0, total, total2;
-            if (tid * run < (1 << bits))
-                for (int i = 0; i < run; ++i) sum += bins[tid * run + i];
-            int before = sum;
-            scan2<THREADS>(scan, before, none, total, total2);
+            constexpr int per = kBins / THREADS;
+            int sum = 0;
+#pragma unroll
+            for (int i = 0; i < per; ++i) sum += count[tid * per + i];               // (the last digit's unused bins are 0)
+            const int upto = wave_incl(sum);
+            if (lane == 63) digit_total[pass][wave] = upto;
+            __syncthreads();
+            int before = upto - sum;
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) before += i < wave ? digit_total[pass][i] : 0;
             if (before < left && left <= before + sum) {
-                int i = tid * run;
-                while (before + bins[i] < left) before += bins[i++];
+                int i = tid * per;
+                while (before + count[i] < left) before += count[i++];
                 found[0] = i;
                 found[1] = left - before;
             }
@@ -208,42 +231,92 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(EvictAccum a)
             bits = shift < kDigit ? shift : kDigit;
             shift -= bits;
         }
-        // a thread takes a run of slots: how many of rank T before it, then how many holes and movers
-        const int run = (n + THREADS - 1) / THREADS, t0 = min(tid * run, n), t1 = min(t0 + run, n);
-        int equal = 0, none = 0, equals, total2;
-        for (int t = t0; t < t1; ++t) equal += rank(t) == T;
-        scan2<THREADS>(scan, equal, none, equals, total2);
-        const int stay = equals - left;                           // of rank T, the first ones
-        int holes = 0, movers = 0, at = equal;
-        for (int t = t0; t < t1; ++t) {
-            const unsigned r = rank(t);
-            const bool goes = r < T || (r == T && at >= stay);
-            at += r == T;
-            holes += goes && t < b;
-            movers += !goes && t >= b;
-        }
-        int all_movers;
-        scan2<THREADS>(scan, holes, movers, moves, all_movers);   // (as many of the one as of the other)
-        at = equal;
-        for (int t = t0; t < t1; ++t) {
-            const unsigned r = rank(t);
-            const bool goes = r < T || (r == T && at >= stay);
-            at += r == T;
-            if (goes && t < b) {
-                if (listed) listed[1 + 2 * holes] = t; else few[holes].x = t;
-                ++holes;
+        if constexpr (REGS) {
+            // Slots of a wave are consecutive in every e: a lane mask counts them, and every wave scans the counts of all for itself,
+            // (e, wave) in order, two to a lane.
+            static_assert(kRun * WAVES <= 128);
+            auto before_waves = [&](int which, const int (&mine)[kRun], int (&before)[kRun], int* total) {
+#pragma unroll
+                for (int e = 0; e < kRun; ++e)
+                    if (lane == 0) wave_count[which][e * WAVES + wave] = mine[e];
+                __syncthreads();
+                const int c0 = 2 * lane < kRun * WAVES ? wave_count[which][2 * lane] : 0, c1 = 2 * lane < kRun * WAVES ? wave_count[which][2 * lane + 1] : 0;
+                const int upto = wave_incl(c0 + c1);
+                *total = __builtin_amdgcn_readlane(upto, 63);
+#pragma unroll
+                for (int e = 0; e < kRun; ++e) {
+                    const int i = e * WAVES + wave, l = i >> 1;
+                    before[e] = __builtin_amdgcn_readlane(upto - c0 - c1, l) + (i & 1 ? __builtin_amdgcn_readlane(c0, l) : 0);
+                }
+            };
+            const unsigned long long below = (1ull << lane) - 1;
+            unsigned long long same[kRun], hole[kRun], mover[kRun];
+            int mine[kRun], before[kRun], equals, both;
+#pragma unroll
+            for (int e = 0; e < kRun; ++e) {
+                same[e] = __builtin_amdgcn_ballot_w64(e * THREADS + tid < n && ranks[e] == T);
+                mine[e] = __builtin_popcountll(same[e]);
             }
-            if (!goes && t >= b) {
-                if (listed) listed[2 + 2 * movers] = t; else few[movers].y = t;
-                ++movers;
+            before_waves(0, mine, before, &equals);
+            const int stay = equals - left;                       // of rank T, the first ones
+#pragma unroll
+            for (int e = 0; e < kRun; ++e) {
+                const int t = e * THREADS + tid;
+                const bool goes = ranks[e] < T || (ranks[e] == T && before[e] + __builtin_popcountll(same[e] & below) >= stay);
+                hole[e] = __builtin_amdgcn_ballot_w64(t < b && goes);
+                mover[e] = __builtin_amdgcn_ballot_w64(t >= b && t < n && !goes);
+                mine[e] = __builtin_popcountll(hole[e]) | __builtin_popcountll(mover[e]) << 16;
             }
+            before_waves(1, mine, before, &both);                 // (as many of the one as of the other)
+            moves = both & 0xffff;
+#pragma unroll
+            for (int e = 0; e < kRun; ++e) {
+                const int t = e * THREADS + tid;
+                if (hole[e] >> lane & 1) holes_at[(before[e] & 0xffff) + __builtin_popcountll(hole[e] & below)] = t;
+                if (mover[e] >> lane & 1) movers_at[(before[e] >> 16) + __builtin_popcountll(mover[e] & below)] = t;
+            }
+        } else {
+            // how many of rank T lie before a thread's slots, then how many holes and movers
+            int equal = 0, none = 0, equals, total2;
+            each([&](int, unsigned r) { equal += r == T; });
+            scan2<THREADS>(scan, equal, none, equals, total2);
+            const int stay = equals - left;
+            int holes = 0, movers = 0, at = equal, all_movers;
+            auto goes = [&](unsigned r) {
+                const bool g = r < T || (r == T && at >= stay);
+                at += r == T;
+                return g;
+            };
+            each([&](int t, unsigned r) {
+                const bool g = goes(r);
+                holes += g && t < b;
+                movers += !g && t >= b;
+            });
+            scan2<THREADS>(scan, holes, movers, moves, all_movers);
+            at = equal;
+            each([&](int t, unsigned r) {
+                const bool g = goes(r);
+                if (g && t < b) {
+                    if (listed) listed[1 + 2 * holes] = t; else holes_at[holes] = t;
+                    ++holes;
+                }
+                if (!g && t >= b) {
+                    if (listed) listed[2 + 2 * movers] = t; else movers_at[movers] = t;
+                    ++movers;
+                }
+            });
         }
         __syncthreads();                                          // (also: every rank has been read)
-        for (int i = tid; i < moves; i += THREADS) {
-            const int hole = listed ? listed[1 + 2 * i] : few[i].x, mover = listed ? listed[2 + 2 * i] : few[i].y;
-            w[hole] = w[mover];
-            if (pos) pos[hole] = pos[mover];
+    }
+    const bool in_lds = REGS || !listed || gone <= kOneByOne;
+    for (int i = tid; i < moves; i += THREADS) {
+        const int hole = in_lds ? holes_at[i] : listed[1 + 2 * i], mover = in_lds ? movers_at[i] : listed[2 + 2 * i];
+        if (listed && in_lds) {
+            listed[1 + 2 * i] = hole;
+            listed[2 + 2 * i] = mover;
         }
+        w[hole] = w[mover];
+        if (pos) pos[hole] = pos[mover];
     }
     if (tid == 0) {
         a.lengths[head] = b;
@@ -251,7 +324,7 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(EvictAccum a)
     }
     if (!listed) {
         const int per = a.g.D >> 2;                               // pieces of a move, of K and V
-        for (int i = tid; i < moves * per; i += THREADS) move_piece(a, x, h, few[i / per].x, few[i / per].y, i % per);
+        for (int i = tid; i < moves * per; i += THREADS) move_piece(a, x, h, holes_at[i / per], movers_at[i / per], i % per);
     }
 }
 
@@ -294,13 +367,15 @@ hipError_t launch_evict_accumulated(const Geom& g, const EvictAccumCall& c, void
     const bool few = a.max_moves <= kFewMoves;
     a.moves = few ? nullptr : static_cast<int32_t*>(workspace);
     const int heads = g.n_items * g.H_kv;
-    if (c.max_own <= 2048) hipLaunchKernelGGL(evict_rank_kernel<256>, dim3((unsigned)heads), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(evict_rank_kernel<1024>, dim3((unsigned)heads), dim3(1024), 0, s, a);
+    const dim3 grid((unsigned)heads);
+    if (c.max_own <= 256 * kRun) hipLaunchKernelGGL((evict_rank_kernel<256, true>), grid, dim3(256), 0, s, a);
+    else if (c.max_own <= 1024 * kRun) hipLaunchKernelGGL((evict_rank_kernel<1024, true>), grid, dim3(1024), 0, s, a);
+    else hipLaunchKernelGGL((evict_rank_kernel<1024, false>), grid, dim3(1024), 0, s, a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || few) return e;
-    // workgroups per head: 32 rows of K and V each, as long as there are fewer than eight per CU
+    // workgroups per head: 32 rows of K and V each, as long as there are fewer than sixteen per CU
     int parts = (a.max_moves + 31) / 32;
-    const int most = (2048 + heads - 1) / heads;
+    const int most = (4096 + heads - 1) / heads;
     if (parts > most) parts = most;
     hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(heads * parts)), dim3(256), 0, s, a, parts);
     return hipGetLastError();
