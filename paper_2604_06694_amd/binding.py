@@ -243,6 +243,13 @@ def _need(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
     return t
 
 
+def _here(t: torch.Tensor, name: str) -> None:
+    """Kernels go to the current stream of the current device: tensors of another one are refused."""
+    at = _raw_device() if _raw_device is not None else torch.cuda.current_device()
+    if t.get_device() != at:
+        raise ValueError(f"{name} is on device {t.get_device()}, the current one is {at}")
+
+
 def version() -> int:
     return _lib.audiokv_version()
 
@@ -486,7 +493,7 @@ def accumulate(p: Params, q: torch.Tensor, k: torch.Tensor, seqlens: Sequence[in
     """Adds the attention weight that every token receives from the last queries[i] positions of each item to `weights`
     (fp32; zeros of the scores' layout if not given) and returns it. `pitch`: distance between heads of `weights`, 0:
     packed like scores. `lse`: fp32, [n_q_heads][queries[i]] of item after item."""
-    _need(q, torch.bfloat16, "q"); _need(k, torch.bfloat16, "k")
+    _need(q, torch.bfloat16, "q"); _need(k, torch.bfloat16, "k"); _here(k, "k")
     if len(queries) != len(seqlens):
         raise ValueError(f"{len(queries)} numbers of queries for {len(seqlens)} lengths")
     dev = k.device
@@ -528,7 +535,7 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
                   out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """One decoding step of q.shape[0] sequences (q: bf16 [n_seqs, n_q_heads, head_dim]) on the compacted caches that they
     share (`k_prompt` None: on none) and the rows that they own; bf16 output of q's shape. Updates `slots` in place."""
-    _need(q, torch.bfloat16, "q")
+    _need(q, torch.bfloat16, "q"); _here(q, "q")
     dev, n_seqs = q.device, q.shape[0]
     if q.numel() != n_seqs * p.n_q_heads * p.head_dim:
         raise ValueError("q must be [n_seqs, n_q_heads, head_dim]")
@@ -572,6 +579,7 @@ def evict_accumulated(p: Params, slots: Slots, n_seqs: int, budget: int, recent:
                       budgets: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """Cuts the rows of every head of `slots` to its budget (`budget`, or the larger of it and budgets[head]) in place, by
     recency and accumulated weight."""
+    _here(slots.lengths, "slots.lengths")
     if budgets is not None and _need(budgets, torch.int32, "budgets").numel() < n_seqs * p.n_kv_heads:
         raise ValueError(f"budgets has {budgets.numel()} values, {n_seqs * p.n_kv_heads} needed")
     ws = workspace

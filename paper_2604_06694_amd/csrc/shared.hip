@@ -413,81 +413,88 @@ __device__ __forceinline__ Chunks chunks_of(const Shared& a, int x, ItemOf it, i
     return t;
 }
 
-// A workgroup per query: its chunks joined. Behind those, workgroups of kWeightRows own rows each add the rows' weights.
-constexpr int kJoinLds = 1024;                // chunks whose factors fit the LDS array (more: recomputed where used)
+// The weights of kWeightRows own rows of a head
 constexpr int kWeightRows = 4 * kThreads;
 
-__global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int weight_blocks)
+__device__ __forceinline__ void add_weights(const Shared& a, int own, int j0)
 {
-    __shared__ float factor[kJoinLds];
-    __shared__ float wave_m[kWaves], wave_l[kWaves];
-    __shared__ __attribute__((aligned(16))) f32x4 red[kThreads];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, G = a.g.G, D = a.g.D;
-    const int queries = a.n_seqs * a.g.H_q;
-    if ((int)blockIdx.x >= queries) {
-        const int id = blockIdx.x - queries, own = id / weight_blocks, j0 = (id - own * weight_blocks) * kWeightRows;
-        const int x = own / a.g.H_kv, h = own - x * a.g.H_kv, after = a.after[own], n = after >> 1;
-        const ItemOf it = item_of(a, x);
-        if (it.item < 0 || j0 >= n) return;
-        // the logits of the first heads are on their way while the statistics are joined
-        constexpr int kRows = kWeightRows / kThreads, kEarly = 8;
-        const float* z = a.logits + (int64_t)own * G * a.logit_pitch;
-        float early[kEarly][kRows];
+    __shared__ float norm[32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, G = a.g.G;
+    const int x = own / a.g.H_kv, h = own - x * a.g.H_kv, after = a.after[own], n = after >> 1;
+    const ItemOf it = item_of(a, x);
+    if (it.item < 0 || j0 >= n) return;
+    // the logits of the first heads are on their way while the statistics are joined
+    constexpr int kRows = kWeightRows / kThreads, kEarly = 8;
+    const float* z = a.logits + (int64_t)own * G * a.logit_pitch;
+    float early[kEarly][kRows];
+#pragma unroll
+    for (int gq = 0; gq < kEarly; ++gq)
+#pragma unroll
+        for (int u = 0; u < kRows; ++u) early[gq][u] = z[(int64_t)min(gq, G - 1) * a.logit_pitch + min(j0 + u * kThreads + tid, n - 1)];
+    // max + log2(sum) of the group's queries, a wave on every fourth
+    for (int gq = wave; gq < G; gq += kWaves) {
+        const Chunks t = chunks_of(a, x, it, h, gq, after);
+        float m = -INFINITY, l = 0.f;
+        for (int c = lane; c < t.np + t.no; c += 64) {
+            const float2 s = t.stat(c);
+            const float m2 = fmaxf(m, s.x), ref = m2 == -INFINITY ? 0.f : m2;
+            l = l * fast_exp2(m - ref) + s.y * fast_exp2(s.x - ref);
+            m = m2;
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+            const float mo = __shfl_xor(m, o, 64), lo = __shfl_xor(l, o, 64);
+            const float m2 = fmaxf(m, mo), ref = m2 == -INFINITY ? 0.f : m2;
+            l = l * fast_exp2(m - ref) + lo * fast_exp2(mo - ref);
+            m = m2;
+        }
+        if (lane == 0) norm[gq] = l == 0.f ? INFINITY : m + __log2f(l);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+        const int j = j0 + u * kThreads + tid;
+        if (j >= n) break;
+        float w = 0.f;
 #pragma unroll
         for (int gq = 0; gq < kEarly; ++gq)
-#pragma unroll
-            for (int u = 0; u < kRows; ++u) early[gq][u] = z[(int64_t)min(gq, G - 1) * a.logit_pitch + min(j0 + u * kThreads + tid, n - 1)];
-        // max + log2(sum) of the group's queries, a wave on every fourth
-        for (int gq = wave; gq < G; gq += kWaves) {
-            const Chunks t = chunks_of(a, x, it, h, gq, after);
-            float m = -INFINITY, l = 0.f;
-            for (int c = lane; c < t.np + t.no; c += 64) {
-                const float2 s = t.stat(c);
-                const float m2 = fmaxf(m, s.x), ref = m2 == -INFINITY ? 0.f : m2;
-                l = l * fast_exp2(m - ref) + s.y * fast_exp2(s.x - ref);
-                m = m2;
-            }
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) {
-                const float mo = __shfl_xor(m, o, 64), lo = __shfl_xor(l, o, 64);
-                const float m2 = fmaxf(m, mo), ref = m2 == -INFINITY ? 0.f : m2;
-                l = l * fast_exp2(m - ref) + lo * fast_exp2(mo - ref);
-                m = m2;
-            }
-            if (lane == 0) factor[gq] = l == 0.f ? INFINITY : m + __log2f(l);
-        }
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < kRows; ++u) {
-            const int j = j0 + u * kThreads + tid;
-            if (j >= n) break;
-            float w = 0.f;
-#pragma unroll
-            for (int gq = 0; gq < kEarly; ++gq)
-                if (gq < G) w += fast_exp2(early[gq][u] - factor[gq]);
-            for (int gq = kEarly; gq < G; ++gq) w += fast_exp2(z[(int64_t)gq * a.logit_pitch + j] - factor[gq]);
-            float* dst = a.weights + (int64_t)own * a.capacity + j;
-            *dst = (after & 1) && j == n - 1 ? w : *dst + w;  // the appended row begins at nothing
-        }
+            if (gq < G) w += fast_exp2(early[gq][u] - norm[gq]);
+        for (int gq = kEarly; gq < G; ++gq) w += fast_exp2(z[(int64_t)gq * a.logit_pitch + j] - norm[gq]);
+        float* dst = a.weights + (int64_t)own * a.capacity + j;
+        *dst = (after & 1) && j == n - 1 ? w : *dst + w;      // the appended row begins at nothing
+    }
+}
+
+// Workgroups of kWeightRows own rows each add the rows' weights; behind those, THREADS threads per query join its chunks: a wave,
+// four queries to a workgroup, or a whole workgroup where heads have many chunks (launch_shared).
+template <int THREADS>
+__global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int weight_blocks)
+{
+    constexpr int WAVES = THREADS / 64;
+    __shared__ float wave_m[kWaves], wave_l[kWaves];
+    __shared__ __attribute__((aligned(16))) f32x4 red[kThreads];
+    if ((int)blockIdx.x < a.n_seqs * a.g.H_kv * weight_blocks) {
+        const int own = blockIdx.x / weight_blocks;
+        add_weights(a, own, (blockIdx.x - own * weight_blocks) * kWeightRows);
         return;
     }
-    const int x = blockIdx.x / a.g.H_q, hq = blockIdx.x - x * a.g.H_q, h = hq / G, gq = hq - h * G;
+    const int tid = threadIdx.x % THREADS, lane = threadIdx.x & 63, wave = tid >> 6, G = a.g.G, D = a.g.D;
+    const int query = (blockIdx.x - a.n_seqs * a.g.H_kv * weight_blocks) * (kThreads / THREADS) + (int)threadIdx.x / THREADS;
+    if (query >= a.n_seqs * a.g.H_q) return;                  // (a whole wave, or workgroup)
+    const int x = query / a.g.H_q, hq = query - x * a.g.H_q, h = hq / G, gq = hq - h * G;
     const int after = a.own_chunks > 0 ? a.after[x * a.g.H_kv + h] : 0;      // (of a sequence that takes no part: anything)
     const ItemOf it = item_of(a, x);
     if (it.item < 0) return;
     const Chunks t = chunks_of(a, x, it, h, gq, after);
-    if (gq == 0 && tid == 0) {
+    if (gq == 0 && tid == 0 && (after & 1)) {
         const int own = x * a.g.H_kv + h;
-        if (after & 1) {
-            a.lengths[own] = after >> 1;
-            if (a.positions) a.positions[(int64_t)own * a.capacity + (after >> 1) - 1] = a.pos_new[x];
-        }
+        a.lengths[own] = after >> 1;
+        if (a.positions) a.positions[(int64_t)own * a.capacity + (after >> 1) - 1] = a.pos_new[x];
     }
     const int nc = t.np + t.no;
     float m = -INFINITY, l = 0.f;
-    for (int c = tid; c < nc; c += kThreads) {
+    for (int c = tid; c < nc; c += THREADS) {
         const float2 s = t.stat(c);
-        if (c < kJoinLds) factor[c] = s.x;
         const float m2 = fmaxf(m, s.x), ref = m2 == -INFINITY ? 0.f : m2;
         l = l * fast_exp2(m - ref) + s.y * fast_exp2(s.x - ref);
         m = m2;
@@ -495,36 +502,44 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int wei
     float M = m;
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
-    if (lane == 0) wave_m[wave] = M;
-    __syncthreads();
+    if constexpr (WAVES > 1) {
+        if (lane == 0) wave_m[wave] = M;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) M = fmaxf(M, wave_m[w]);
+        for (int w = 0; w < WAVES; ++w) M = fmaxf(M, wave_m[w]);
+    }
     const float ref = M == -INFINITY ? 0.f : M;
     l *= fast_exp2(m - ref);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
-    if (lane == 0) wave_l[wave] = l;
-    for (int c = tid; c < min(nc, kJoinLds); c += kThreads) factor[c] = fast_exp2(factor[c] - ref);
-    __syncthreads();
-    const float den = ((wave_l[0] + wave_l[1]) + wave_l[2]) + wave_l[3];
-
-    const int quads = D >> 2, groups = kThreads / quads, ch = tid % quads, grp = tid / quads;
+    float den = l;
+    if constexpr (WAVES > 1) {
+        if (lane == 0) wave_l[wave] = l;
+        __syncthreads();
+        den = ((wave_l[0] + wave_l[1]) + wave_l[2]) + wave_l[3];
+    }
+    // a thread has four channels of every (THREADS / (D / 4))-th chunk
+    const int quads = D >> 2, groups = THREADS / quads, ch = tid % quads, grp = tid / quads;
     const f32x4* pp = reinterpret_cast<const f32x4*>(a.part_p + (t.sp - a.stats_p) * D) + ch;
     const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + (t.so - a.stats_o) * D) + ch;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int c = grp; c < nc; c += groups) {
-        const float f = c < kJoinLds ? factor[c] : fast_exp2(t.stat(c).x - ref);
-        acc += (c < t.np ? pp[c * t.step_p * quads] : po[(c - t.np) * t.step_o * quads]) * f;
+    for (int c = grp; c < nc; c += groups)
+        acc += (c < t.np ? pp[c * t.step_p * quads] : po[(c - t.np) * t.step_o * quads]) * fast_exp2(t.stat(c).x - ref);
+    if constexpr (WAVES > 1) {
+        red[tid] = acc;
+        __syncthreads();
+        if (grp == 0)
+            for (int k = 1; k < groups; ++k) acc += red[k * quads + ch];
+    } else {
+        for (int o = quads; o < 64; o <<= 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o, 64);
     }
-    red[tid] = acc;
-    __syncthreads();
     if (grp == 0) {
-        f32x4 num = acc;
-        for (int k = 1; k < groups; ++k) num += red[k * quads + ch];
         bf16x4 o;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = (__bf16)(den == 0.f ? 0.f : num[i] / den);     // no row, or nothing but -inf: zeros
+        for (int i = 0; i < 4; ++i) o[i] = (__bf16)(den == 0.f ? 0.f : acc[i] / den);     // no row, or nothing but -inf: zeros
         *reinterpret_cast<bf16x4*>(a.out + ((int64_t)x * a.g.H_q + hq) * D + ch * 4) = o;
     }
 }
@@ -537,6 +552,10 @@ inline size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 // query, 512 bytes written and read at d = 128: few, long ones (32 sequences on 13107 rows, 4 heads: chunks of 128, 256 and 512 rows
 // 32 + 13, 24 + 10 and 23 + 8 us). Own rows: 48 caches of up to 4096 rows, 4 heads, 1024 workgroups 43 us, 2048 39.
 constexpr int kPromptBlocks = 192, kOwnBlocks = 2048;
+// What one wave joins per query: four channels to a lane, 256 floats at a time. Both kernels' weights included: 48 caches of 11 chunks
+// at d = 128 8.8 us by a wave and 10.5 by a workgroup per query, 64 sequences on 9 chunks of eight prompts 19 and 42; at d = 256
+// with 18 chunks 7.0 and 6.2.
+constexpr int kWaveFloats = 4096;
 
 // How a call is cut. Pure function of its sizes, so that the workspace query and the launch agree. The workspace never shrinks as
 // total_rows or max_own grow: one that is sized for the largest step serves the smaller ones.
@@ -579,7 +598,7 @@ bool shared_supported(const Geom& g, const SharedPlan& p, int n_seqs)
 {
     const double most = 8388608.;               // launches stay below 2^32 threads
     return g.G <= 32 && (double)(p.slots + 8) * p.row_blocks + (double)n_seqs * g.H_kv * p.own_chunks < most &&
-           (double)n_seqs * g.H_q + (double)n_seqs * g.H_kv * (p.logit_pitch / kThreads + 1) < most;
+           (double)n_seqs * g.H_q + (double)n_seqs * g.H_kv * (p.logit_pitch / kWeightRows + 1) < most;
 }
 
 hipError_t launch_shared(const Geom& g, const SharedPlan& p, const SharedCall& c, void* workspace, hipStream_t s)
@@ -634,8 +653,13 @@ hipError_t launch_shared(const Geom& g, const SharedPlan& p, const SharedCall& c
         if (e != hipSuccess) return e;
     }
     const int weight_blocks = c.weights ? (c.max_own + kWeightRows - 1) / kWeightRows : 0;
-    hipLaunchKernelGGL(shared_join_kernel, dim3((unsigned)(c.n_seqs * g.H_q + c.n_seqs * g.H_kv * weight_blocks)), threads, 0, s, a,
-                       weight_blocks);
+    const long long weights = (long long)c.n_seqs * g.H_kv * weight_blocks, queries = (long long)c.n_seqs * g.H_q;
+    // chunks of an average head
+    const long long chunks = (c.n_items > 0 ? p.slots / ((long long)c.n_items * g.H_kv) : 0) + p.own_chunks;
+    if (chunks * g.D <= kWaveFloats)
+        hipLaunchKernelGGL(shared_join_kernel<64>, dim3((unsigned)(weights + (queries + 3) / 4)), threads, 0, s, a, weight_blocks);
+    else
+        hipLaunchKernelGGL(shared_join_kernel<kThreads>, dim3((unsigned)(weights + queries)), threads, 0, s, a, weight_blocks);
     return hipGetLastError();
 }
 

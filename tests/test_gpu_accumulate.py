@@ -252,3 +252,48 @@ def test_totals_feed_selection(A):
         rows = slice(int(cu_b[g]), int(cu_b[g + 1]))
         assert np.array_equal(idx[rows], O.select(b.of(w, i)[h], int(budgets[g]), 8))
         assert np.array_equal(kept[rows].astype(np.float64), b.k[i][h][idx[rows]])
+
+
+def test_offsets_beyond_32_bits(A):
+    """Keys further than 2^31 elements from the first: heads far apart, and tokens."""
+    for stride_head, stride_tok in (((1 << 31) + 4096, 64), (64, 1 << 25)):
+        b = Batch(np.random.default_rng(16), 4, 2, 64, [90], [90])
+        q, _ = b.tensors()
+        k = torch.zeros(stride_head + 89 * stride_tok + 64, dtype=torch.bfloat16, device="cuda")
+        k.as_strided((2, 90, 64), (stride_head, stride_tok, 1)).copy_(bf16(b.k[0]))
+        p = A.Params(4, 2, 64, 0, kv_stride_item=8, kv_stride_head=stride_head, kv_stride_tok=stride_tok)
+        b.check(A, A.accumulate(p, q, k, [90], [90]))
+        del k
+
+
+def test_nan_of_a_query_reaches_only_what_it_sees(A):
+    """Query 40 is NaN: the tokens that it sees get NaN, those behind it do not (the queries behind it see them all)."""
+    for G in (1, 4):
+        b = Batch(np.random.default_rng(17), G, 1, 128, [300], [300])
+        b.q[0][0, 40] = np.nan
+        got = b.of(run(A, b), 0)[0]
+        assert np.isnan(got[:41]).all() and np.isfinite(got[41:]).all()
+        b.q[0][0, 40] = 0
+        want = O.accumulate(b.q[0], b.k[0])[0]
+        assert (np.abs(got[41:] - want[41:]) <= b.bound(0) * want[41:]).all()
+
+
+@pytest.mark.parametrize("H_q,H_kv,d", [(28, 4, 128), (8, 2, 256), (8, 2, 64)])
+def test_two_tiles_a_wave(A, H_q, H_kv, d):
+    """Calls large enough for blocks of two tiles a wave, ragged, against torch in 64 bits on the device."""
+    rng = np.random.default_rng(d)
+    lens, queries = [5003, 1700, 3001], [5003, 900, 3001]
+    b = Batch(rng, H_q, H_kv, d, lens, queries, "token")
+    q, k = b.tensors()
+    got = A.accumulate(b.params(A), q, k, lens, queries)
+    for i, (L, Q) in enumerate(zip(lens, queries)):
+        kd, qd, want = torch.from_numpy(b.k[i]).cuda(), torch.from_numpy(b.q[i]).cuda(), torch.zeros(H_kv, L, dtype=torch.float64, device="cuda")
+        for j in range(H_q):
+            z = qd[j] @ kd[j * H_kv // H_q].T.contiguous() * d ** -0.5
+            z.masked_fill_(torch.arange(L, device="cuda") > L - Q + torch.arange(Q, device="cuda")[:, None], -np.inf)
+            want[j * H_kv // H_q] += torch.softmax(z, dim=1).sum(0)
+        want = want.cpu().numpy()
+        part = Batch.__new__(Batch)
+        part.H_q, part.H_kv, part.d, part.q, part.k = H_q, H_kv, d, [b.q[i][:, ::37]], [b.k[i][:, ::37]]
+        tol = part.bound(0) + (L / 16 + H_q // H_kv * Q / 16) * U
+        assert (np.abs(b.of(got, i) - want) <= tol * want).all(), i

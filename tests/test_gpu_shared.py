@@ -332,3 +332,68 @@ def test_steps_in_a_row_are_one_long_attention(A):
     assert t["slots"].lengths.tolist() == [12] * 4
     got = t["slots"].weights.cpu().numpy()
     assert (np.abs(got - total) <= 1e-4 * total + 1e-30).all()
+
+
+def test_offsets_beyond_32_bits(A):
+    """Prompts and own rows whose elements lie further than 2^31 from the first: strided heads far apart, a stride from row to
+    row that passes it within the cache, and a capacity that does."""
+    rng = np.random.default_rng(13)
+    for stride_head, stride_tok in (((1 << 31) + 4096, 64), (64, 1 << 25)):
+        s = Step(rng, 4, 2, 64, None, None, [[70, 66]], 72)
+        t = s.tensors(A, positions=False)
+        span = stride_head + 71 * stride_tok + 64
+        k, v = (torch.zeros(span, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        views = [x.as_strided((2, 72, 64), (stride_head, stride_tok, 1)) for x in (k, v)]
+        views[0].copy_(bf16(s.ko[0])); views[1].copy_(bf16(s.vo[0]))
+        slots = A.Slots(k, v, t["slots"].lengths, 72, t["slots"].weights)
+        p = A.Params(4, 2, 64, 0, kv_stride_item=8, kv_stride_head=stride_head, kv_stride_tok=stride_tok)
+        A.decode_shared(p, t["q"], None, None, None, 0, None, 1, slots=slots, max_own=71, k_new=t["k_new"], v_new=t["v_new"], out=t["out"])
+        t["slots"] = A.Slots(views[0].contiguous()[None], views[1].contiguous()[None], slots.lengths, 72, slots.weights)
+        s.check(t)
+        A.evict_accumulated(p, slots, 1, 40, 0, 71)
+        w = t["slots"].weights.cpu().numpy()
+        del k, v, views
+    s = Step(rng, 2, 2, 256, None, None, [[33, 5]], 40)
+    t = s.tensors(A)
+    C = (1 << 23) + 8                                             # slots of a head: head 1 begins 2^31 elements on
+    big = [torch.zeros(1, 2, C, 256, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    big[0][:, :, :40], big[1][:, :, :40] = t["slots"].k, t["slots"].v
+    weights = torch.zeros(2, C, device="cuda")
+    weights[:, :40] = t["slots"].weights.view(2, 40)
+    slots = A.Slots(big[0], big[1], t["slots"].lengths, C, weights)
+    A.decode_shared(t["p"], t["q"], None, None, None, 0, None, 1, slots=slots, max_own=40, k_new=t["k_new"], v_new=t["v_new"], out=t["out"])
+    t["slots"] = A.Slots(big[0][:, :, :40].contiguous(), big[1][:, :, :40].contiguous(), slots.lengths, 40, weights[:, :40].contiguous())
+    s.check(t, max_own=40)
+
+
+@pytest.mark.parametrize("n_items", [1, 40, 70, 130])
+def test_many_items(A, n_items):
+    """Tables of items and heads that a wave loads at once, and longer ones that it probes."""
+    rng = np.random.default_rng(n_items)
+    sharing = [int(x) for x in rng.integers(0, 3, n_items)]
+    sharing[-1] = 2
+    budgets = [int(x) for x in rng.integers(0, 9, 2 * n_items)]
+    own = rng.integers(0, 4, (sum(sharing), 2))
+    run(A, Step(rng, 4, 2, 64, budgets, sharing, own, 5, spare=2))
+
+
+def test_what_the_binding_refuses(A):
+    s = Step(np.random.default_rng(14), 4, 2, 64, [5, 6], [2], [[1, 2]] * 2, 8)
+    t = s.tensors(A)
+
+    def call(**change):
+        u = {**t, **change}
+        A.decode_shared(u["p"], u["q"], u["kp"], u["vp"], u["cu_b"], u.get("rows", 11), u["cu_s"], 2, slots=u["slots"], max_own=4,
+                        k_new=u["k_new"], v_new=u["v_new"], pos_new=u["pos"], out=u["out"])
+    short = A.Slots(t["slots"].k, t["slots"].v, t["slots"].lengths, 9, t["slots"].weights, t["slots"].positions)
+    for change in (dict(q=t["q"].float()), dict(q=t["q"].cpu()), dict(q=t["q"].transpose(1, 2)), dict(kp=t["kp"][:10].contiguous()),
+                   dict(rows=12), dict(cu_b=t["cu_b"][:2].contiguous()), dict(cu_b=t["cu_b"].long()), dict(k_new=t["k_new"][:1]),
+                   dict(pos=t["pos"][:1]), dict(out=t["out"][:1]), dict(out=t["out"].float()), dict(slots=short)):
+        with pytest.raises(ValueError):
+            call(**change)
+    call()
+    s.check(t, max_own=4)
+    slots = t["slots"]
+    slots.lengths = slots.lengths[:3].contiguous()                # what was looked at before is looked at again
+    with pytest.raises(ValueError):
+        call()
