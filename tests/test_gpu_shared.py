@@ -397,3 +397,30 @@ def test_what_the_binding_refuses(A):
     slots.lengths = slots.lengths[:3].contiguous()                # what was looked at before is looked at again
     with pytest.raises(ValueError):
         call()
+
+
+@pytest.mark.parametrize("H_q,H_kv,d", [(28, 4, 128), (16, 2, 64), (8, 1, 128)])
+def test_prompts_that_many_sequences_share(A, H_q, H_kv, d):
+    """Several blocks of query rows on long prompts, ragged, and sequences in different numbers, own rows beside them."""
+    rng = np.random.default_rng(d + H_q)
+    G = H_q // H_kv
+    sharing = [max(1, 130 // G), 300 // G + 1, 1]
+    budgets = [int(x) for x in rng.integers(40000 // H_kv, 60000 // H_kv, 3 * H_kv)]
+    budgets[0], budgets[-1] = 33, 0
+    n = sum(sharing)
+    s = Step(rng, H_q, H_kv, d, budgets, sharing, rng.integers(0, 70, (n, H_kv)), 72)
+    t = s.tensors(A)
+    s.call(A, t)
+    # every seventh sequence, the rest by its being like them
+    keep = list(range(0, n, 7))
+    item_of = np.repeat(np.arange(3), sharing)
+    for name in ("q", "own", "ko", "vo", "k_new", "v_new", "w"):
+        setattr(s, name, getattr(s, name)[keep])
+    s.sharing = [int((item_of[keep] == i).sum()) for i in range(3)]
+    s.n = s.active = len(keep)
+    heads = (np.array(keep)[:, None] * H_kv + np.arange(H_kv)).reshape(-1)
+    at = torch.from_numpy(heads).cuda()
+    sl = t["slots"]
+    t["out"] = t["out"][keep]
+    t["slots"] = A.Slots(sl.k[keep], sl.v[keep], sl.lengths[at], 72, sl.weights.view(n * H_kv, -1)[at], None)
+    s.check(t)
