@@ -62,15 +62,16 @@ def build(jobs: int = 8, verbose: bool = True) -> str:
 
 # Sources whose host code carries the library's own logic (argument validation, workspace and launch planning):
 # the sanitizer build instruments these and links the other objects as they are.
-SANITIZED = ["api.hip", "score.hip"]
+SANITIZED = ["accumulate.hip", "api.hip", "evict_accumulated.hip", "score.hip", "shared.hip"]
+CHECKERS = ["abi_host_check", "abi_accumulated_check"]
 SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
              "-Xarch_host", "-fno-sanitize-recover=undefined"]
 
 
 def build_sanitized(verbose: bool = True) -> str:
     """Host-side AddressSanitizer + UndefinedBehaviorSanitizer build: _build/san/libaudiokv_san.so and, against it,
-    _build/san/abi_host_check (tests/abi_host_check.cpp), which drives the host paths of every entry point.
-    Device code is compiled as usual (GPU sanitizers are not used). Returns the path of the checker."""
+    the checkers in _build/san/ (tests/abi_host_check.cpp and tests/abi_accumulated_check.cpp), which drive the host paths of the
+    entry points. Device code is compiled as usual (GPU sanitizers are not used). Returns the path of the first checker."""
     if not all(os.path.exists(os.path.join(BUILD, f.replace(".hip", ".o"))) for f in sources()):
         build(verbose=False)
     san = os.path.join(BUILD, "san")
@@ -91,13 +92,15 @@ def build_sanitized(verbose: bool = True) -> str:
                         "-o", lib] + objs, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"sanitizer link failed:\n{r.stderr}")
-    exe = os.path.join(san, "abi_host_check")
-    r = subprocess.run(["hipcc", "-x", "c++", "-std=c++17", "-O1", "-g", "-fsanitize=address", "-fsanitize=undefined",
-                        "-fno-sanitize-recover=undefined", "-I", os.path.join(ROOT, "include"),
-                        os.path.join(ROOT, "tests", "abi_host_check.cpp"), "-o", exe, "-L", san, "-laudiokv_san",
-                        f"-Wl,-rpath,{san}"], capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"checker build failed:\n{r.stderr}")
+    for check in CHECKERS:
+        exe = os.path.join(san, check)
+        r = subprocess.run(["hipcc", "-x", "c++", "-std=c++17", "-O1", "-g", "-fsanitize=address", "-fsanitize=undefined",
+                            "-fno-sanitize-recover=undefined", "-I", os.path.join(ROOT, "include"),
+                            os.path.join(ROOT, "tests", check + ".cpp"), "-o", exe, "-L", san, "-laudiokv_san",
+                            f"-Wl,-rpath,{san}"], capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"checker build failed:\n{r.stderr}")
+    exe = os.path.join(san, CHECKERS[0])
     if verbose:
         print(f"built {lib} and {exe}")
     return exe
