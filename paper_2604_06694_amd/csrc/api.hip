@@ -782,7 +782,7 @@ int32_t audiokv_decode_shared(const audiokv_params* params, const void* q_dev, c
     Geom g;
     SharedPlan plan;
     AUDIOKV_TRY(plan_shared(params, n_items, total_rows, n_seqs, max_seqs, max_own, &g, &plan));
-    if (!q_dev || !out_dev || !workspace || (n_items > 0 && (!k_prompt || !v_prompt || !cu_budgets_dev || !cu_seqs_dev)))
+    if (!q_dev || !out_dev || !workspace || (n_items > 0 && (!cu_budgets_dev || !cu_seqs_dev)) || (n_items > 0 && total_rows > 0 && (!k_prompt || !v_prompt)))
         return fail(AUDIOKV_E_INVALID_ARG, "audiokv_decode_shared: NULL pointer argument");
     if (!aligned16(q_dev) || !aligned16(out_dev) || !aligned16(workspace) || (n_items > 0 && (!aligned16(k_prompt) || !aligned16(v_prompt))))
         return fail(AUDIOKV_E_INVALID_ARG, "q, out, k_prompt, v_prompt and the workspace must be 16-byte aligned");

@@ -61,7 +61,7 @@ struct Shared {
     __bf16* out;
 };
 
-__device__ __forceinline__ int head_start(const Shared& a, int g) { return min(a.cu_b[g], a.total_rows); }
+__device__ __forceinline__ int head_start(const Shared& a, int g) { return min(max(a.cu_b[g], 0), a.total_rows); }
 __device__ __forceinline__ int first_slot(const Shared& a, int g) { return (head_start(a, g) >> a.log_r) + g; }
 
 // The last of n entries of a rising table of n + 1 whose value is not past v; the first is not. Tables of up to 63 entries are

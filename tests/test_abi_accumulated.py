@@ -95,6 +95,14 @@ def test_decode_shared_refusals(A):
     assert shared(A, p, items=0, rows=0, most=0, kp=None, vp=None, cu=None, cu_s=None, s=slots(A), own=8, size=64) == -3
 
 
+def test_decode_shared_of_prompts_without_rows(A):
+    # a compacted cache without rows has no address; its table and the sequences still have
+    p = A.Params(8, 2, 64, 0)
+    assert shared(A, p, rows=0, kp=None, vp=None, size=64) == -3
+    assert shared(A, p, rows=0, kp=None, vp=None, cu=None) == -1
+    assert shared(A, p, rows=0, kp=None, vp=None, cu_s=None) == -1
+
+
 def test_decode_shared_of_nothing(A):
     p = A.Params(8, 2, 64, 0)
     assert shared(A, p, items=0, n=0, q=None, kp=None, vp=None, cu=None, cu_s=None, out=None, ws=None, size=0) == 0

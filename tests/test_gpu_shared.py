@@ -424,3 +424,9 @@ def test_prompts_that_many_sequences_share(A, H_q, H_kv, d):
     t["out"] = t["out"][keep]
     t["slots"] = A.Slots(sl.k[keep], sl.v[keep], sl.lengths[at], 72, sl.weights.view(n * H_kv, -1)[at], None)
     s.check(t)
+
+
+def test_prompts_without_rows(A):
+    """A compacted cache that kept nothing: sequences have their own rows, or nothing at all."""
+    rng = np.random.default_rng(16)
+    run(A, Step(rng, 4, 2, 64, [0] * 4, [1, 2], [[3, 0], [0, 70], [1, 5]], 80, spare=1))
