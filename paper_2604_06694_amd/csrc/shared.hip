@@ -550,7 +550,9 @@ inline size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 
 // Workgroups that a call's prompts, and own rows, are cut for at least, where they are long enough. A prompt's chunk costs a result per
 // query, 512 bytes written and read at d = 128: few, long ones (32 sequences on 13107 rows, 4 heads: chunks of 128, 256 and 512 rows
-// 32 + 13, 24 + 10 and 23 + 8 us). Own rows: 48 caches of up to 4096 rows, 4 heads, 1024 workgroups 43 us, 2048 39.
+// 32 + 13, 24 + 10 and 23 + 8 us). At d = 128, from three blocks of query rows on, the products are most of it and two workgroups
+// share a CU: 64 sequences on the same rows 35 + 7 us with one, 30 + 9 with two; 512 on eight prompts 87 + 20 and 79 + 21 (at d = 64
+// 35 + 14 and 36 + 15, at d = 256 79 + 10 and 86 + 14: not there). Own rows: 48 caches of up to 4096 rows, 4 heads, 1024 workgroups 43 us, 2048 39.
 constexpr int kPromptBlocks = 192, kOwnBlocks = 2048;
 // What one wave joins per query: four channels to a lane, 256 floats at a time. Both kernels' weights included: 48 caches of 11 chunks
 // at d = 128 8.8 us by a wave and 10.5 by a workgroup per query, 64 sequences on 9 chunks of eight prompts 19 and 42; at d = 256
@@ -566,7 +568,8 @@ SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_s
     if (n_items > 0) {
         p.row_block = max_row_block(g.D);
         p.row_blocks = (int)(((long long)max_seqs * g.G + p.row_block - 1) / p.row_block);
-        const long long wanted = (kPromptBlocks + p.row_blocks - 1) / p.row_blocks;
+        const int blocks = g.D == 128 && p.row_blocks > 2 ? 2 * kPromptBlocks : kPromptBlocks;
+        const long long wanted = (blocks + p.row_blocks - 1) / p.row_blocks;
         p.log_r = 7;
         while (p.log_r < 16 && (total_rows >> (p.log_r + 1)) >= wanted) ++p.log_r;
         p.slots = (total_rows >> p.log_r) + (long long)n_items * g.H_kv;
