@@ -479,7 +479,8 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int wei
         return;
     }
     const int tid = threadIdx.x % THREADS, lane = threadIdx.x & 63, wave = tid >> 6, G = a.g.G, D = a.g.D;
-    const int query = (blockIdx.x - a.n_seqs * a.g.H_kv * weight_blocks) * (kThreads / THREADS) + (int)threadIdx.x / THREADS;
+    const int query = (blockIdx.x - a.n_seqs * a.g.H_kv * weight_blocks) * (kThreads / THREADS) +
+                      __builtin_amdgcn_readfirstlane((int)threadIdx.x / THREADS);
     if (query >= a.n_seqs * a.g.H_q) return;                  // (a whole wave, or workgroup)
     const int x = query / a.g.H_q, hq = query - x * a.g.H_q, h = hq / G, gq = hq - h * G;
     const int after = a.own_chunks > 0 ? a.after[x * a.g.H_kv + h] : 0;      // (of a sequence that takes no part: anything)
@@ -519,7 +520,7 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int wei
         den = ((wave_l[0] + wave_l[1]) + wave_l[2]) + wave_l[3];
     }
     // a thread has four channels of every (THREADS / (D / 4))-th chunk
-    const int quads = D >> 2, groups = THREADS / quads, ch = tid % quads, grp = tid / quads;
+    const int log_quads = 29 - __builtin_clz(D), quads = 1 << log_quads, groups = THREADS >> log_quads, ch = tid & (quads - 1), grp = tid >> log_quads;
     const f32x4* pp = reinterpret_cast<const f32x4*>(a.part_p + (t.sp - a.stats_p) * D) + ch;
     const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + (t.so - a.stats_o) * D) + ch;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -537,9 +538,10 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int wei
             for (int i = 0; i < 4; ++i) acc[i] += __shfl_xor(acc[i], o, 64);
     }
     if (grp == 0) {
+        const float by = 1.f / den;
         bf16x4 o;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] = (__bf16)(den == 0.f ? 0.f : acc[i] / den);     // no row, or nothing but -inf: zeros
+        for (int i = 0; i < 4; ++i) o[i] = (__bf16)(den == 0.f ? 0.f : acc[i] * by);      // no row, or nothing but -inf: zeros
         *reinterpret_cast<bf16x4*>(a.out + ((int64_t)x * a.g.H_q + hq) * D + ch * 4) = o;
     }
 }
