@@ -8,7 +8,10 @@
  *   3. smooth    Spectral Score Smoothing of each head's score sequence
  *   4. select    per-head top-k at the allocated budget
  *   5. compact   gather of the retained K/V rows into a packed cache
- * plus audiokv_evict, which runs 1-5 in one call.
+ * plus audiokv_evict, which runs 1-5 in one call. Around it: audiokv_accumulate
+ * (step 1 with all queries instead of a window), audiokv_decode_attend and
+ * audiokv_decode_shared (decoding steps on the packed cache, the latter with rows
+ * that the sequences add) and audiokv_evict_accumulated (those kept at a budget).
  *
  * Conventions common to every entry point
  * ---------------------------------------
