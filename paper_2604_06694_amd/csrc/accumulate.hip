@@ -21,7 +21,6 @@
 // range is redone against a new one. Everything is in base-2 units: z = <q,k> * scale * log2(e).
 #include "accumulate_plan.h"
 #include "mfma_tile.h"
-#include "score_ring.h"
 
 namespace audiokv {
 
@@ -83,8 +82,8 @@ __device__ __forceinline__ int64_t stat_row(const Accum& a, const Place& p, int 
 
 // Compute waves of a workgroup; one more wave loads. The waves of a workgroup hold kComputeWaves * NB tiles of 32 rows (or keys) as
 // stationary operands, tiles of kStream keys (or rows) come through a ring of LDS buffers that the loader fills straight from HBM
-// or L2 (score_ring.h), one barrier per tile.
-constexpr int kLeastTiles = 2;           // fewer are not worth a workgroup
+// or L2, one barrier per tile.
+constexpr int kLeastTiles = 1;           // 700 tokens, four heads: two 10.2 + 13.2 us on 160 + 144 CUs, one 9.6 + 13.1 on 200 + 176
 constexpr int kComputeWaves = 7, kSweepThreads = 64 * (kComputeWaves + 1), kStages = 4;
 constexpr int stationary(int NB) { return kComputeWaves * NB * 32; }
 
@@ -110,21 +109,26 @@ __device__ __forceinline__ void load_stream(unsigned char* ring, int n_tiles, Wa
 #pragma unroll
     for (int v = 0; v < 8 / RPI; ++v) from[v] = ((slot & ~7) | ((slot - (v * RPI + row)) & 7)) * 8;
     walk.begin(row, RPI);
-    score_detail::fill_ring<kStages>(
-        n_tiles,
-        [&](int t) {
-            unsigned char* dst = ring + (t % kStages) * (kStream * D * 2);
+    auto issue = [&](int t) {
+        unsigned char* dst = ring + (t % kStages) * (kStream * D * 2);
 #pragma unroll
-            for (int it = 0; it < CH; ++it)
-                // a wave-wide instruction fills consecutive LDS: the lane fetches the chunk that belongs in its slot (slot_of)
-                __builtin_amdgcn_global_load_lds((global_void_ptr)(walk.next() + from[it % (8 / RPI)]), (lds_void_ptr)(dst + it * 1024), 16, 0, 0);
-            more(t);
-        },
-        [&]() {
-            __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));         // vmcnt(0): all that was requested is there
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-            __builtin_amdgcn_s_barrier();
-        });
+        for (int it = 0; it < CH; ++it)
+            // a wave-wide instruction fills consecutive LDS: the lane fetches the chunk that belongs in its slot (slot_of)
+            __builtin_amdgcn_global_load_lds((global_void_ptr)(walk.next() + from[it % (8 / RPI)]), (lds_void_ptr)(dst + it * 1024), 16, 0, 0);
+        more(t);
+    };
+    // Compute waves reduce tile t and begin with the next one between the barrier that opens iteration t and the one that ends it: at the
+    // first, tiles up to t + 1 have landed. More of them requested ahead only put off the first barrier (a request takes some
+    // 70 cycles to issue). Tile t + 2 goes where tile t - 2 was, which every wave has left.
+    int t = 0;
+    for (; t < 2 && t < n_tiles; ++t) issue(t);
+    for (int ended = 0;; ++ended) {
+        __builtin_amdgcn_s_waitcnt(0 | (7 << 4) | (15 << 8));             // vmcnt(0): all that was requested is there
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        if (ended == n_tiles) break;
+        if (t < n_tiles) issue(t++);
+    }
 }
 // Keys of a head from j0 on
 struct KeyWalk {
@@ -375,22 +379,21 @@ struct Wave {
 
 // The parts of blocks in a workgroup's span: body(place, head, block, first tile, tiles, part, whether the block has others).
 // Neighbouring spans go to one XCD, whose L2 then holds the head that they are about.
-template <bool COLS, class Body>
+template <bool COLS, int SIZE, class Body>
 __device__ __forceinline__ void for_parts(const Accum& a, Body body)
 {
     const AccumSpans& s = a.spans;
     const int w = (int)(blockIdx.x & 7) * (int)(gridDim.x >> 3) + (int)(blockIdx.x >> 3);
-    if (w >= s.n) return;
-    const SpanStart end = s.at[w + 1];
-    int head = s.at[w].head, block = s.at[w].block, tile = s.at[w].tile;
+    const SpanStart begin = s.at[w], end = s.at[w + 1];           // (the same behind the last span)
+    int head = begin.head, block = begin.block, tile = begin.tile;
     while (head < end.head || (head == end.head && (block < end.block || (block == end.block && tile < end.tile)))) {
         const Place p = place_of(a, head);
-        if (block >= p.item_of.blocks(COLS, a.block)) {
+        if (block >= p.item_of.blocks(COLS, SIZE)) {
             ++head;
             block = tile = 0;
             continue;
         }
-        const int tiles = p.item_of.tiles(COLS, block, a.block), stop = head == end.head && block == end.block ? min(tiles, end.tile) : tiles;
+        const int tiles = p.item_of.tiles(COLS, block, SIZE), stop = head == end.head && block == end.block ? min(tiles, end.tile) : tiles;
         if (tile < stop) body(p, head, block, tile, stop - tile, tile > 0 ? w - s.first_of(head, block, w) : 0, stop - tile < tiles);
         ++block;
         tile = 0;
@@ -403,7 +406,7 @@ __global__ __launch_bounds__(kSweepThreads, 2) void accumulate_rows_kernel(Accum
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    for_parts<false>(a, [&](const Place& p, int, int block, int tile0, int n_tiles, int part, bool shared) {
+    for_parts<false, stationary(NB)>(a, [&](const Place& p, int, int block, int tile0, int n_tiles, int part, bool shared) {
         const int j0 = tile0 * kStream;
         if (wave == kComputeWaves) {
             load_stream<D>(lds, n_tiles, KeyWalk(a, p, j0), [](int) {});
@@ -482,8 +485,8 @@ __global__ __launch_bounds__(kSweepThreads, 2) void accumulate_cols_kernel(Accum
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     float* norm = reinterpret_cast<float*>(lds + kStages * kStream * D * 2);      // of a tile's rows, beside the tile in the ring
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    for_parts<true>(a, [&](const Place& p, int head, int block, int tile0, int n_tiles, int part, bool shared) {
-        const int r0 = p.item_of.key_tiles_from(block, a.block) + tile0 * kStream;
+    for_parts<true, stationary(NB)>(a, [&](const Place& p, int head, int block, int tile0, int n_tiles, int part, bool shared) {
+        const int r0 = p.item_of.key_tiles_from(block, stationary(NB)) + tile0 * kStream;
         if (wave == kComputeWaves) {
             load_stream<D>(lds, n_tiles, RowWalk(a, p, r0), [&](int t) {
                 const int r = min(r0 + t * kStream + lane, p.R - 1);

@@ -49,7 +49,7 @@ struct SpanStart {
 };
 struct AccumSpans {
     int n = 0;                            // workgroups
-    SpanStart at[kSpans + 1];             // workgroup w ends where w + 1 begins
+    SpanStart at[kSpans + 1];             // workgroup w ends where w + 1 begins; from n on: the end
     // The first workgroup with tiles of a block, `near` one that has some
     __host__ __device__ int first_of(int head, int block, int near) const {
         int w = near;
@@ -131,7 +131,7 @@ __host__ inline AccumSweep plan_sweep(bool cols, int size, int n_items, int head
         }
         before += per * heads;
     }
-    s.spans.at[s.spans.n] = SpanStart{n_items * heads, 0, 0};
+    for (w = s.spans.n; w <= kSpans; ++w) s.spans.at[w] = SpanStart{n_items * heads, 0, 0};
     if (cut) s.max_parts = (int)((longest + span - 1) / span) + 1;
     return s;
 }
