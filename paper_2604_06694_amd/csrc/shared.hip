@@ -281,9 +281,37 @@ __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int fi
     // ones are stored, and where a second wave had the other half of the keys it hands its share over there. Groups of four are
     // rotated by the row.
     constexpr int kGroups = CT * 8;
-    f32x4* mine = reinterpret_cast<f32x4*>(&tile[0][0][0]) + (wq * W::kSplit + part_of) * (32 * kGroups);
+    f32x4* const all = reinterpret_cast<f32x4*>(&tile[0][0][0]);
+    f32x4* mine = all + (wq * W::kSplit + part_of) * (32 * kGroups);
     auto group = [&](int ct, int i) { return col * kGroups + ((ct * 8 + i / 2 + hf) ^ (col & 15)); };
     l += __shfl_xor(l, 32, 64);
+    // At d = 128 both waves' shares go there and all threads join and store them: one wave took 5000 cycles for it, a third of a short
+    // workgroup's time (48 caches of up to 4096 rows 39.5 -> 36.4 us). At d = 64 this takes 182 registers instead of 150 (1024
+    // sequences with few rows 34 -> 44 us).
+    if constexpr (D == 128) {
+        if (halves) {                                         // uniform
+            if (works) {
+                mine = all + wave * (32 * kGroups);
+                if (hf == 0) joint[wave][col] = make_float2(m, l);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4) mine[group(ct, i)] = f32x4{acc[ct][i], acc[ct][i + 1], acc[ct][i + 2], acc[ct][i + 3]};
+            }
+            __syncthreads();
+            f32x4* dst = reinterpret_cast<f32x4*>(part + (int64_t)r_first * D);
+#pragma unroll 2
+            for (int u = tid; u < left * kGroups; u += kThreads) {
+                const int row = u / kGroups, c = u % kGroups, w = row >> 5, r = row & 31;
+                const f32x4* at = all + (w * 32 + r) * kGroups + (c ^ (r & 15));
+                const float2 s0 = joint[w][r], s1 = joint[w + wq_n][r];
+                const float M = fmaxf(s0.x, s1.x), ref = M == -INFINITY ? 0.f : M, by = fast_exp2(s0.x - ref), other = fast_exp2(s1.x - ref);
+                dst[u] = at[0] * by + at[wq_n * 32 * kGroups] * other;
+                if (c == 0) stats[r_first + row] = make_float2(M, s0.y * by + s1.y * other);
+            }
+            return;
+        }
+    }
     if (halves) {                                             // uniform
         if (wk == 1) {
             joint[wq][lane] = make_float2(m, l);
