@@ -14,7 +14,7 @@
 //
 // Work is cut into spans of equal numbers of tiles, one workgroup per CU, across blocks and heads (accumulate_plan.h): the
 // triangle leaves blocks of very different lengths, and a workgroup costs as much to start as three tiles. A grid of (block,
-// range of 13 to 32 tiles) took 350 + 340 us for one layer of 8192 tokens where this takes 262 + 274. What the parts of a block that several
+// range of 13 to 32 tiles) took 350 + 340 us for one layer of 8192 tokens where this took 262 + 274 on the same card. What the parts of a block that several
 // workgroups share have found is joined by two small kernels in fixed order (row statistics; column sums). No atomics.
 //
 // References of a row are not maxima (see score_impl.h): the first logits set one, and only a tile whose sum leaves the safe
