@@ -101,6 +101,10 @@ class Params:
                         self.kv_stride_item, self.kv_stride_head, self.kv_stride_tok)
 
 
+_SLOTS_SIZE = C.sizeof(_CSlots)
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
 @dataclass
 class Slots:
     """Rows that sequences own: device tensors, see audiokv_slots. `weights` and `positions` may be missing."""
@@ -111,32 +115,23 @@ class Slots:
     weights: Optional[torch.Tensor] = None   # fp32 [n_seqs * n_kv_heads, capacity]
     positions: Optional[torch.Tensor] = None # int32, the same
 
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        self.__dict__.pop("_kept", None)
-
     def _c(self, p: Params, n_seqs: int) -> _CSlots:
-        """The C struct. Types and sizes are looked at once for the same tensors and heads (a step is a few microseconds of
-        the host's, and this look three)."""
-        w, pos = self.weights, self.positions
-        where = (self.k.data_ptr(), self.v.data_ptr(), self.lengths.data_ptr(), None if w is None else w.data_ptr(),
-                 None if pos is None else pos.data_ptr(), n_seqs, p.n_kv_heads, p.head_dim, p.kv_stride_tok)
-        kept = self.__dict__.get("_kept")
-        if kept is not None and kept[0] == where:
-            return kept[1]
+        """The C struct, after a look at types and sizes (in one expression: a step is some twenty microseconds of the host's)."""
+        k, v, lengths, w, pos = self.k, self.v, self.lengths, self.weights, self.positions
         heads = n_seqs * p.n_kv_heads
-        for name, t, dtype, n in (("lengths", self.lengths, torch.int32, heads), ("weights", w, torch.float32, heads * self.capacity),
-                                  ("positions", pos, torch.int32, heads * self.capacity)):
-            if t is not None and _need(t, dtype, "slots." + name).numel() < n:
-                raise ValueError(f"slots.{name} has {t.numel()} values, {n} needed")
-        for name, t in (("k", self.k), ("v", self.v)):
-            if not t.is_cuda or t.dtype != torch.bfloat16:
-                raise ValueError(f"slots.{name} must be a device tensor of dtype {torch.bfloat16}")
-            if p.kv_stride_tok == 0 and _need(t, torch.bfloat16, "slots." + name).numel() < heads * self.capacity * p.head_dim:
-                raise ValueError(f"slots.{name} has {t.numel()} values, {heads * self.capacity * p.head_dim} needed")
-        c = _CSlots(C.sizeof(_CSlots), self.capacity, *where[:5])
-        self.__dict__["_kept"] = (where, c)
-        return c
+        slots = heads * self.capacity
+        if (k.dtype is not _BF16 or v.dtype is not _BF16 or not k.is_cuda or not v.is_cuda
+                or p.kv_stride_tok == 0 and (not k.is_contiguous() or not v.is_contiguous() or k.numel() < slots * p.head_dim
+                                             or v.numel() < slots * p.head_dim)):
+            raise ValueError(f"slots.k and slots.v must be device tensors of dtype {_BF16}, and contiguous with {slots * p.head_dim} values "
+                             "where params has no strides")
+        if lengths.dtype is not _I32 or not lengths.is_cuda or not lengths.is_contiguous() or lengths.numel() < heads:
+            raise ValueError(f"slots.lengths must be a contiguous device tensor of {heads} values of dtype {_I32}")
+        if w is not None and (w.dtype is not _F32 or not w.is_cuda or not w.is_contiguous() or w.numel() < slots):
+            raise ValueError(f"slots.weights must be a contiguous device tensor of {slots} values of dtype {_F32}")
+        if pos is not None and (pos.dtype is not _I32 or not pos.is_cuda or not pos.is_contiguous() or pos.numel() < slots):
+            raise ValueError(f"slots.positions must be a contiguous device tensor of {slots} values of dtype {_I32}")
+        return _CSlots(_SLOTS_SIZE, self.capacity, k.data_ptr(), v.data_ptr(), lengths.data_ptr(), _ptr(w), _ptr(pos))
 
 
 def lib_path() -> str:
@@ -238,7 +233,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _need(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
-    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+    if t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous device tensor of dtype {dtype}")
     return t
 
@@ -535,27 +530,27 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
                   out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """One decoding step of q.shape[0] sequences (q: bf16 [n_seqs, n_q_heads, head_dim]) on the compacted caches that they
     share (`k_prompt` None: on none) and the rows that they own; bf16 output of q's shape. Updates `slots` in place."""
-    _need(q, torch.bfloat16, "q"); _here(q, "q")
+    _need(q, _BF16, "q"); _here(q, "q")
     dev, n_seqs = q.device, q.shape[0]
     if q.numel() != n_seqs * p.n_q_heads * p.head_dim:
         raise ValueError("q must be [n_seqs, n_q_heads, head_dim]")
     n_items = 0
     if k_prompt is not None:
-        _need(k_prompt, torch.bfloat16, "k_prompt"); _need(v_prompt, torch.bfloat16, "v_prompt")
-        _need(cu_budgets, torch.int32, "cu_budgets"); _need(cu_seqs, torch.int32, "cu_seqs")
+        _need(k_prompt, _BF16, "k_prompt"); _need(v_prompt, _BF16, "v_prompt")
+        _need(cu_budgets, _I32, "cu_budgets"); _need(cu_seqs, _I32, "cu_seqs")
         n_items = cu_seqs.numel() - 1
         if cu_budgets.numel() < n_items * p.n_kv_heads + 1:
             raise ValueError(f"cu_budgets has {cu_budgets.numel()} values, {n_items * p.n_kv_heads + 1} needed")
         if min(k_prompt.numel(), v_prompt.numel()) < total_rows * p.head_dim:
             raise ValueError(f"k_prompt or v_prompt holds fewer than {total_rows} rows")
     for name, t in (("k_new", k_new), ("v_new", v_new)):
-        if t is not None and _need(t, torch.bfloat16, name).numel() < n_seqs * p.n_kv_heads * p.head_dim:
+        if t is not None and _need(t, _BF16, name).numel() < n_seqs * p.n_kv_heads * p.head_dim:
             raise ValueError(f"{name} must be [n_seqs, n_kv_heads, head_dim]")
-    if pos_new is not None and _need(pos_new, torch.int32, "pos_new").numel() < n_seqs:
+    if pos_new is not None and _need(pos_new, _I32, "pos_new").numel() < n_seqs:
         raise ValueError("pos_new must have a value per sequence")
     if out is None:
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
-    elif _need(out, torch.bfloat16, "out").numel() < q.numel():
+    elif _need(out, _BF16, "out").numel() < q.numel():
         raise ValueError("out is smaller than q")
     ws = workspace
     if ws is None:
