@@ -543,9 +543,12 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
             raise ValueError(f"cu_budgets has {cu_budgets.numel()} values, {n_items * p.n_kv_heads + 1} needed")
         if min(k_prompt.numel(), v_prompt.numel()) < total_rows * p.head_dim:
             raise ValueError(f"k_prompt or v_prompt holds fewer than {total_rows} rows")
-    for name, t in (("k_new", k_new), ("v_new", v_new)):
-        if t is not None and _need(t, _BF16, name).numel() < n_seqs * p.n_kv_heads * p.head_dim:
-            raise ValueError(f"{name} must be [n_seqs, n_kv_heads, head_dim]")
+    if k_new is not None:
+        rows = n_seqs * p.n_kv_heads * p.head_dim
+        if _need(k_new, _BF16, "k_new").numel() < rows or v_new is None or _need(v_new, _BF16, "v_new").numel() < rows:
+            raise ValueError("k_new and v_new must be [n_seqs, n_kv_heads, head_dim]")
+    elif v_new is not None:
+        raise ValueError("k_new and v_new come together")
     if pos_new is not None and _need(pos_new, _I32, "pos_new").numel() < n_seqs:
         raise ValueError("pos_new must have a value per sequence")
     if out is None:
@@ -557,9 +560,10 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
         ws = torch.empty(max(decode_shared_workspace_bytes(p, n_items, total_rows, n_seqs, max_seqs, max_own if slots else 0), 256),
                          dtype=torch.uint8, device=dev)
     cs = C.byref(slots._c(p, n_seqs)) if slots is not None else None
-    _check(_lib.audiokv_decode_shared(C.byref(p._c()), _ptr(q), _ptr(k_prompt), _ptr(v_prompt), _ptr(cu_budgets), n_items, int(total_rows),
-                                      _ptr(cu_seqs), n_seqs, int(max_seqs), cs, int(max_own),
-                                      _ptr(k_new), _ptr(v_new), _ptr(pos_new), _ptr(out), _ptr(ws), ws.numel(), _stream()))
+    prompts = (k_prompt.data_ptr(), v_prompt.data_ptr(), cu_budgets.data_ptr()) if n_items > 0 else (None, None, None)
+    _check(_lib.audiokv_decode_shared(C.byref(p._c()), q.data_ptr(), *prompts, n_items, int(total_rows),
+                                      cu_seqs.data_ptr() if n_items > 0 else None, n_seqs, int(max_seqs), cs, int(max_own),
+                                      _ptr(k_new), _ptr(v_new), _ptr(pos_new), out.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
     return out
 
 
