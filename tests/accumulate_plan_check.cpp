@@ -20,6 +20,9 @@ static void check(bool cols, int size, const std::vector<AccumItem>& items, int 
     const AccumSweep s = plan_sweep(cols, size, (int)items.size(), heads, least, [&](int i) { return items[i]; });
     const AccumSpans& sp = s.spans;
     CHECK(sp.n <= kSpans);
+    // workgroups beyond the last span find nothing to do
+    if (sp.n > 0)
+        for (int w = sp.n; w <= kSpans; ++w) CHECK(sp.at[w].head == (int)items.size() * heads && sp.at[w].block == 0 && sp.at[w].tile == 0);
     // what the workgroups do, as the kernels walk through it
     long long lo = 1LL << 60, hi = 0;
     std::vector<std::vector<std::vector<int>>> by(items.size() * heads);      // head, block: workgroups in order
