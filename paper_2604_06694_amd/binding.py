@@ -238,6 +238,27 @@ def _need(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
     return t
 
 
+def _table(t: Optional[torch.Tensor], n: int, name: str) -> None:
+    """Exclusive prefix sums of n numbers, if given."""
+    if t is not None and _need(t, _I32, name).numel() < n + 1:
+        raise ValueError(f"{name} has {t.numel()} values, {n + 1} needed")
+
+
+def _rows_end(p: Params, lens: Sequence[int]) -> int:
+    """Elements from the first of K (or V) to the end of the last row that items of these lengths have."""
+    if p.kv_stride_tok == 0:
+        return sum(int(x) for x in lens) * p.n_kv_heads * p.head_dim
+    last_head = (p.n_kv_heads - 1) * p.kv_stride_head + p.head_dim
+    return max((i * p.kv_stride_item + (int(x) - 1) * p.kv_stride_tok + last_head for i, x in enumerate(lens)), default=0)
+
+
+def _room(p: Params, t: torch.Tensor) -> int:
+    """Elements of memory from t's first: a tensor that strides address may be a view of a part of it."""
+    if p.kv_stride_tok == 0:
+        return t.numel()
+    return t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+
+
 def _here(t: torch.Tensor, name: str) -> None:
     """Kernels go to the current stream of the current device: tensors of another one are refused."""
     at = _raw_device() if _raw_device is not None else torch.cuda.current_device()
@@ -494,6 +515,9 @@ def accumulate(p: Params, q: torch.Tensor, k: torch.Tensor, seqlens: Sequence[in
     dev = k.device
     if q.numel() < sum(queries) * p.n_q_heads * p.head_dim:
         raise ValueError("q is smaller than its queries")
+    if _room(p, k) < _rows_end(p, seqlens):
+        raise ValueError(f"k has room for {_room(p, k)} values, {_rows_end(p, seqlens)} needed")
+    _table(cu_seqlens, len(seqlens), "cu_seqlens"); _table(cu_queries, len(seqlens), "cu_queries")
     cu = cu_seqlens if cu_seqlens is not None else _cu(seqlens, dev)
     cu_q = cu_queries if cu_queries is not None else _cu(queries, dev)
     total = (pitch * len(seqlens) if pitch else sum(int(x) for x in seqlens)) * p.n_kv_heads

@@ -1,0 +1,83 @@
+"""What the binding of accumulate, decode_shared and evict_accumulated refuses before the library is called, and what it lets
+through. CPU only: tensors without memory stand for the device's, and the library's functions note that they were reached."""
+import warnings
+
+import pytest
+import torch
+from torch._subclasses.fake_tensor import FakeTensorMode
+
+BF16, F32, I32 = torch.bfloat16, torch.float32, torch.int32
+
+
+class Library:
+    """Stands for the loaded library: every entry point succeeds and is listed in `reached`."""
+
+    def __init__(self):
+        self.reached = []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.reached.append(name)
+            return 0
+        return call
+
+
+@pytest.fixture
+def A(monkeypatch):
+    import paper_2604_06694_amd as A
+    library = Library()
+    monkeypatch.setattr(A.binding, "_lib", library)
+    monkeypatch.setattr(A.binding, "_raw_device", lambda: 0)
+    monkeypatch.setattr(A.binding, "_stream", lambda: 0)
+    A.reached = library.reached
+    with FakeTensorMode(), warnings.catch_warnings():
+        warnings.simplefilter("ignore")                       # (that tensors here have no address)
+        yield A
+    del A.reached
+
+
+def dev(*shape, dtype=BF16, device="cuda:0"):
+    return torch.empty(shape, dtype=dtype, device=device)
+
+
+def refused(call, A, **change):
+    del A.reached[:]
+    with pytest.raises(ValueError):
+        call(A, **change)
+    assert not any(name in ("audiokv_accumulate", "audiokv_decode_shared", "audiokv_evict_accumulated") for name in A.reached), change
+
+
+# ---- accumulate: two items of 50 and 30 tokens, 20 and 30 queries, 4 query heads on 2 KV heads of 64 channels ----
+
+def accumulate(A, **change):
+    given = dict(p=A.Params(4, 2, 64, 0), q=dev(50 * 4 * 64), k=dev(80 * 2 * 64), weights=dev(160, dtype=F32), lse=dev(200, dtype=F32),
+                 cu_seqlens=dev(3, dtype=I32), cu_queries=dev(3, dtype=I32), workspace=dev(1 << 16, dtype=torch.uint8), pitch=0)
+    given.update(change)
+    p, q, k = (given.pop(x) for x in ("p", "q", "k"))
+    return A.accumulate(p, q, k, [50, 30], [20, 30], **given)
+
+
+def test_accumulate_takes_what_fits(A):
+    accumulate(A)
+    accumulate(A, cu_seqlens=dev(9, dtype=I32), k=dev(81 * 2 * 64), lse=None, weights=None)
+    assert A.reached == ["audiokv_accumulate"] * 2
+
+
+def test_accumulate_refuses_keys_that_end_too_early(A):
+    refused(accumulate, A, k=dev(80 * 2 * 64 - 1))
+    slab = dict(kv_stride_item=2 * 52 * 64, kv_stride_head=52 * 64, kv_stride_tok=64)
+    end = (2 * 52 + 52 + 29) * 64 + 64                        # of item 1's last row, behind which the slab may end
+    accumulate(A, p=A.Params(4, 2, 64, 0, **slab), k=dev(end))
+    refused(accumulate, A, p=A.Params(4, 2, 64, 0, **slab), k=dev(end - 1))
+    accumulate(A, p=A.Params(4, 2, 64, 0, **slab), k=dev(end + 64)[64:80])         # a view: what it is a view of counts
+    refused(accumulate, A, p=A.Params(4, 2, 64, 0, **slab), k=dev(end + 63)[64:80])
+    # an earlier item may reach further than the last one
+    long = dict(kv_stride_item=8, kv_stride_head=64, kv_stride_tok=128)
+    accumulate(A, p=A.Params(4, 2, 64, 0, **long), k=dev(49 * 128 + 128))
+    refused(accumulate, A, p=A.Params(4, 2, 64, 0, **long), k=dev(49 * 128 + 127))
+
+
+@pytest.mark.parametrize("name", ["cu_seqlens", "cu_queries"])
+def test_accumulate_refuses_tables_that_are_none(A, name):
+    for bad in (dev(2, dtype=I32), dev(3, dtype=torch.int64), dev(3, dtype=F32), torch.empty(3, dtype=I32), dev(6, dtype=I32)[::2]):
+        refused(accumulate, A, **{name: bad})
