@@ -125,6 +125,10 @@ class Slots:
                                              or v.numel() < slots * p.head_dim)):
             raise ValueError(f"slots.k and slots.v must be device tensors of dtype {_BF16}, and contiguous with {slots * p.head_dim} values "
                              "where params has no strides")
+        if p.kv_stride_tok != 0 and n_seqs > 0:
+            end = ((n_seqs - 1) * p.kv_stride_item + (p.n_kv_heads - 1) * p.kv_stride_head + (self.capacity - 1) * p.kv_stride_tok + p.head_dim)
+            if _room(p, k) < end or _room(p, v) < end:
+                raise ValueError(f"slots.k or slots.v has room for {min(_room(p, k), _room(p, v))} values, {end} needed by the strides")
         if lengths.dtype is not _I32 or not lengths.is_cuda or not lengths.is_contiguous() or lengths.numel() < heads:
             raise ValueError(f"slots.lengths must be a contiguous device tensor of {heads} values of dtype {_I32}")
         if w is not None and (w.dtype is not _F32 or not w.is_cuda or not w.is_contiguous() or w.numel() < slots):

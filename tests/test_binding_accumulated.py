@@ -81,3 +81,44 @@ def test_accumulate_refuses_keys_that_end_too_early(A):
 def test_accumulate_refuses_tables_that_are_none(A, name):
     for bad in (dev(2, dtype=I32), dev(3, dtype=torch.int64), dev(3, dtype=F32), torch.empty(3, dtype=I32), dev(6, dtype=I32)[::2]):
         refused(accumulate, A, **{name: bad})
+
+
+# ---- decode_shared: two sequences with 10 own slots a head, on one prompt of 11 rows; the same geometry ----
+
+SLAB = dict(kv_stride_item=2 * 12 * 64, kv_stride_head=12 * 64, kv_stride_tok=64)
+SLAB_END = (2 * 12 + 12 + 9) * 64 + 64                        # of the last slot
+
+
+def slots(A, **change):
+    return A.Slots(**{**dict(k=dev(2 * 2 * 10 * 64), v=dev(2 * 2 * 10 * 64), lengths=dev(4, dtype=I32), capacity=10,
+                             weights=dev(4, 10, dtype=F32), positions=dev(4, 10, dtype=I32)), **change})
+
+
+def decode_shared(A, **change):
+    given = dict(p=A.Params(4, 2, 64, 0), q=dev(2, 4, 64), k_prompt=dev(11, 64), v_prompt=dev(11, 64), cu_budgets=dev(3, dtype=I32), total_rows=11,
+                 cu_seqs=dev(2, dtype=I32), max_seqs=2, slots=slots(A), max_own=8, k_new=dev(2, 2, 64), v_new=dev(2, 2, 64),
+                 pos_new=dev(2, dtype=I32), out=dev(2, 4, 64), workspace=dev(1 << 16, dtype=torch.uint8))
+    given.update(change)
+    return A.decode_shared(**given)
+
+
+def evict(A, p=None, s=None, budgets=None, workspace=None):
+    A.evict_accumulated(p or A.Params(4, 2, 64, 0), s or slots(A), 2, 4, 2, 8, budgets=budgets, workspace=workspace)
+
+
+def test_slots_that_fit(A):
+    decode_shared(A)
+    evict(A)
+    strided = A.Params(4, 2, 64, 0, **SLAB)
+    for s in (slots(A, k=dev(SLAB_END), v=dev(SLAB_END)), slots(A, k=dev(SLAB_END + 8)[8:16], v=dev(2, 2, 12, 64)[:, :, :10])):
+        decode_shared(A, p=strided, slots=s)
+        evict(A, p=strided, s=s)
+    assert A.reached.count("audiokv_decode_shared") == A.reached.count("audiokv_evict_accumulated") == 3
+
+
+def test_slots_that_strides_lead_out_of_are_refused(A):
+    strided = A.Params(4, 2, 64, 0, **SLAB)
+    for change in (dict(k=dev(SLAB_END - 1)), dict(v=dev(SLAB_END - 1)), dict(k=dev(SLAB_END)[8:]), dict(capacity=11)):
+        s = slots(A, **{**dict(k=dev(SLAB_END), v=dev(SLAB_END), weights=dev(4, 11, dtype=F32), positions=dev(4, 11, dtype=I32)), **change})
+        refused(decode_shared, A, p=strided, slots=s)
+        refused(evict, A, p=strided, s=s)
