@@ -135,6 +135,7 @@ class Slots:
             raise ValueError(f"slots.weights must be a contiguous device tensor of {slots} values of dtype {_F32}")
         if pos is not None and (pos.dtype is not _I32 or not pos.is_cuda or not pos.is_contiguous() or pos.numel() < slots):
             raise ValueError(f"slots.positions must be a contiguous device tensor of {slots} values of dtype {_I32}")
+        _here("slots.k slots.v slots.lengths slots.weights slots.positions", k, v, lengths, w, pos)
         return _CSlots(_SLOTS_SIZE, self.capacity, k.data_ptr(), v.data_ptr(), lengths.data_ptr(), _ptr(w), _ptr(pos))
 
 
@@ -263,11 +264,12 @@ def _room(p: Params, t: torch.Tensor) -> int:
     return t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
 
 
-def _here(t: torch.Tensor, name: str) -> None:
-    """Kernels go to the current stream of the current device: tensors of another one are refused."""
+def _here(names: str, *tensors: Optional[torch.Tensor]) -> None:
+    """Kernels go to the current stream of the current device: tensors of another one, or of the host, are refused."""
     at = _raw_device() if _raw_device is not None else torch.cuda.current_device()
-    if t.get_device() != at:
-        raise ValueError(f"{name} is on device {t.get_device()}, the current one is {at}")
+    for i, t in enumerate(tensors):
+        if t is not None and t.get_device() != at:
+            raise ValueError(f"{names.split()[i]} is on {t.device}, the current device is {at}")
 
 
 def version() -> int:
@@ -513,7 +515,8 @@ def accumulate(p: Params, q: torch.Tensor, k: torch.Tensor, seqlens: Sequence[in
     """Adds the attention weight that every token receives from the last queries[i] positions of each item to `weights`
     (fp32; zeros of the scores' layout if not given) and returns it. `pitch`: distance between heads of `weights`, 0:
     packed like scores. `lse`: fp32, [n_q_heads][queries[i]] of item after item."""
-    _need(q, torch.bfloat16, "q"); _need(k, torch.bfloat16, "k"); _here(k, "k")
+    _need(q, torch.bfloat16, "q"); _need(k, torch.bfloat16, "k")
+    _here("q k weights lse cu_seqlens cu_queries workspace", q, k, weights, lse, cu_seqlens, cu_queries, workspace)
     if len(queries) != len(seqlens):
         raise ValueError(f"{len(queries)} numbers of queries for {len(seqlens)} lengths")
     dev = k.device
@@ -558,7 +561,8 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
                   out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """One decoding step of q.shape[0] sequences (q: bf16 [n_seqs, n_q_heads, head_dim]) on the compacted caches that they
     share (`k_prompt` None: on none) and the rows that they own; bf16 output of q's shape. Updates `slots` in place."""
-    _need(q, _BF16, "q"); _here(q, "q")
+    _need(q, _BF16, "q")
+    _here("q k_new v_new pos_new out workspace", q, k_new, v_new, pos_new, out, workspace)
     dev, n_seqs = q.device, q.shape[0]
     if q.numel() != n_seqs * p.n_q_heads * p.head_dim:
         raise ValueError("q must be [n_seqs, n_q_heads, head_dim]")
@@ -566,6 +570,7 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
     if k_prompt is not None:
         _need(k_prompt, _BF16, "k_prompt"); _need(v_prompt, _BF16, "v_prompt")
         _need(cu_budgets, _I32, "cu_budgets"); _need(cu_seqs, _I32, "cu_seqs")
+        _here("k_prompt v_prompt cu_budgets cu_seqs", k_prompt, v_prompt, cu_budgets, cu_seqs)
         n_items = cu_seqs.numel() - 1
         if cu_budgets.numel() < n_items * p.n_kv_heads + 1:
             raise ValueError(f"cu_budgets has {cu_budgets.numel()} values, {n_items * p.n_kv_heads + 1} needed")
@@ -606,7 +611,7 @@ def evict_accumulated(p: Params, slots: Slots, n_seqs: int, budget: int, recent:
                       budgets: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """Cuts the rows of every head of `slots` to its budget (`budget`, or the larger of it and budgets[head]) in place, by
     recency and accumulated weight."""
-    _here(slots.lengths, "slots.lengths")
+    _here("budgets workspace", budgets, workspace)
     if budgets is not None and _need(budgets, torch.int32, "budgets").numel() < n_seqs * p.n_kv_heads:
         raise ValueError(f"budgets has {budgets.numel()} values, {n_seqs * p.n_kv_heads} needed")
     ws = workspace

@@ -122,3 +122,23 @@ def test_slots_that_strides_lead_out_of_are_refused(A):
         s = slots(A, **{**dict(k=dev(SLAB_END), v=dev(SLAB_END), weights=dev(4, 11, dtype=F32), positions=dev(4, 11, dtype=I32)), **change})
         refused(decode_shared, A, p=strided, slots=s)
         refused(evict, A, p=strided, s=s)
+
+
+@pytest.mark.parametrize("where", ["cuda:1", "cpu"])
+def test_tensors_of_another_device_are_refused(A, where):
+    def there(*shape, dtype=BF16):
+        return dev(*shape, dtype=dtype, device=where)
+    for change in (dict(q=there(50 * 4 * 64)), dict(k=there(80 * 2 * 64)), dict(weights=there(160, dtype=F32)), dict(lse=there(200, dtype=F32)),
+                   dict(cu_seqlens=there(3, dtype=I32)), dict(cu_queries=there(3, dtype=I32)), dict(workspace=there(1 << 16, dtype=torch.uint8))):
+        refused(accumulate, A, **change)
+    own = (dict(k=there(2 * 2 * 10 * 64)), dict(v=there(2 * 2 * 10 * 64)), dict(lengths=there(4, dtype=I32)),
+           dict(weights=there(4, 10, dtype=F32)), dict(positions=there(4, 10, dtype=I32)))
+    for change in (dict(q=there(2, 4, 64)), dict(k_prompt=there(11, 64)), dict(v_prompt=there(11, 64)), dict(cu_budgets=there(3, dtype=I32)),
+                   dict(cu_seqs=there(2, dtype=I32)), dict(k_new=there(2, 2, 64)), dict(v_new=there(2, 2, 64)), dict(pos_new=there(2, dtype=I32)),
+                   dict(out=there(2, 4, 64)), dict(workspace=there(1 << 16, dtype=torch.uint8)), *(dict(slots=slots(A, **x)) for x in own)):
+        refused(decode_shared, A, **change)
+    for change in (dict(budgets=there(4, dtype=I32)), dict(workspace=there(1 << 16, dtype=torch.uint8)), *(dict(s=slots(A, **x)) for x in own)):
+        refused(evict, A, **change)
+    with pytest.raises(ValueError):                           # everything elsewhere: the stream is the current device's
+        evict(A, s=slots(A, k=there(2 * 2 * 10 * 64), v=there(2 * 2 * 10 * 64), lengths=there(4, dtype=I32),
+                         weights=there(4, 10, dtype=F32), positions=there(4, 10, dtype=I32)))
