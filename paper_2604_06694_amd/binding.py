@@ -572,6 +572,8 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
         _need(cu_budgets, _I32, "cu_budgets"); _need(cu_seqs, _I32, "cu_seqs")
         _here("k_prompt v_prompt cu_budgets cu_seqs", k_prompt, v_prompt, cu_budgets, cu_seqs)
         n_items = cu_seqs.numel() - 1
+        if n_items < 1:                       # (the library's call without items lets every sequence take part)
+            raise ValueError("cu_seqs must have an entry per item and one more; without prompts, k_prompt is None")
         if cu_budgets.numel() < n_items * p.n_kv_heads + 1:
             raise ValueError(f"cu_budgets has {cu_budgets.numel()} values, {n_items * p.n_kv_heads + 1} needed")
         if min(k_prompt.numel(), v_prompt.numel()) < total_rows * p.head_dim:

@@ -142,3 +142,10 @@ def test_tensors_of_another_device_are_refused(A, where):
     with pytest.raises(ValueError):                           # everything elsewhere: the stream is the current device's
         evict(A, s=slots(A, k=there(2 * 2 * 10 * 64), v=there(2 * 2 * 10 * 64), lengths=there(4, dtype=I32),
                          weights=there(4, 10, dtype=F32), positions=there(4, 10, dtype=I32)))
+
+
+def test_prompts_of_no_item_are_refused(A):
+    """cu_seqs of one entry says that no sequence takes part; a call without items would let all of them."""
+    refused(decode_shared, A, cu_seqs=dev(1, dtype=I32))
+    refused(decode_shared, A, cu_seqs=dev(0, dtype=I32))
+    decode_shared(A, k_prompt=None, v_prompt=None, cu_budgets=None, cu_seqs=None, total_rows=0)      # without prompts all of them do
