@@ -78,17 +78,6 @@ class Params:
     kv_stride_head: int = 0
     kv_stride_tok: int = 0
 
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        self.__dict__.pop("_kept", None)
-
-    def _c(self) -> _CParams:
-        """c(), kept until a field is set: the struct is only read."""
-        kept = self.__dict__.get("_kept")
-        if kept is None:
-            kept = self.__dict__["_kept"] = self.c()
-        return kept
-
     def key(self) -> tuple:
         return (self.n_q_heads, self.n_kv_heads, self.head_dim, self.window, self.pool_kernel, self.pool_mode,
                 self.causal, self.kv_layout, self.softmax_scale, self.floor_frac, self.cutoff_mode, self.taper_bins,
@@ -596,7 +585,7 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
                          dtype=torch.uint8, device=dev)
     cs = C.byref(slots._c(p, n_seqs)) if slots is not None else None
     prompts = (k_prompt.data_ptr(), v_prompt.data_ptr(), cu_budgets.data_ptr()) if n_items > 0 else (None, None, None)
-    _check(_lib.audiokv_decode_shared(C.byref(p._c()), q.data_ptr(), *prompts, n_items, int(total_rows),
+    _check(_lib.audiokv_decode_shared(C.byref(p.c()), q.data_ptr(), *prompts, n_items, int(total_rows),
                                       cu_seqs.data_ptr() if n_items > 0 else None, n_seqs, int(max_seqs), cs, int(max_own),
                                       _ptr(k_new), _ptr(v_new), _ptr(pos_new), out.data_ptr(), ws.data_ptr(), ws.numel(), _stream()))
     return out
@@ -620,7 +609,7 @@ def evict_accumulated(p: Params, slots: Slots, n_seqs: int, budget: int, recent:
     if ws is None:
         ws = torch.empty(max(evict_accumulated_workspace_bytes(p, n_seqs, max_own, budget), 256), dtype=torch.uint8,
                          device=slots.lengths.device)
-    _check(_lib.audiokv_evict_accumulated(C.byref(p._c()), C.byref(slots._c(p, n_seqs)), int(n_seqs), int(budget), _ptr(budgets), int(recent), int(max_own),
+    _check(_lib.audiokv_evict_accumulated(C.byref(p.c()), C.byref(slots._c(p, n_seqs)), int(n_seqs), int(budget), _ptr(budgets), int(recent), int(max_own),
                                           _ptr(ws), ws.numel(), _stream()))
 
 

@@ -149,3 +149,17 @@ def test_prompts_of_no_item_are_refused(A):
     refused(decode_shared, A, cu_seqs=dev(1, dtype=I32))
     refused(decode_shared, A, cu_seqs=dev(0, dtype=I32))
     decode_shared(A, k_prompt=None, v_prompt=None, cu_budgets=None, cu_seqs=None, total_rows=0)      # without prompts all of them do
+
+
+def test_params_are_plain_values(A):
+    """Calls leave nothing in them, setting a field runs no code of ours, and what the library is given is always the fields' values."""
+    p = A.Params(4, 2, 64, 0)
+    decode_shared(A, p=p)
+    evict(A, p=p)
+    assert A.Params(**vars(p)) == p and "__setattr__" not in vars(A.Params)
+    given = []
+    A.binding._lib.__dict__["audiokv_evict_accumulated"] = lambda params, *rest: given.append(bytes(params._obj)) or 0
+    for field, value in (("softmax_scale", 0.5), ("kv_layout", 1), ("softmax_scale", 0.25), ("kv_layout", 0), ("softmax_scale", 0.5)):
+        setattr(p, field, value)
+        evict(A, p=p)
+        assert given[-1] == bytes(p.c())
