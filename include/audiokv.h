@@ -397,8 +397,8 @@ typedef struct audiokv_slots {
  *   account   (slots->weights not NULL) every own row's weight grows by the sum of
  *             what the group's queries gave it.
  * max_own (host): no head has more own rows than this after the step, at most
- * slots->capacity. Rows beyond it are not read, and a head that has max_own rows
- * before the step appends none. max_seqs (host): no item has more sequences.
+ * slots->capacity and below 2^30. Rows beyond it are not read, and a head that has
+ * max_own rows before the step appends none. max_seqs (host): no item has more sequences.
  * Sequences from cu_seqs[n_items] on, and those of an item beyond max_seqs, take
  * no part: their outputs, lengths and rows stay as they are, so that a batch of
  * fixed size can be captured into a graph and filled by cu_seqs.

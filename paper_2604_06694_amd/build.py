@@ -63,14 +63,14 @@ def build(jobs: int = 8, verbose: bool = True) -> str:
 # Sources whose host code carries the library's own logic (argument validation, workspace and launch planning):
 # the sanitizer build instruments these and links the other objects as they are.
 SANITIZED = ["accumulate.hip", "api.hip", "evict_accumulated.hip", "score.hip", "shared.hip"]
-CHECKERS = ["abi_host_check", "abi_accumulated_check"]
+CHECKERS = ["abi_host_check", "abi_accumulated_check", "abi_accumulated_limits_check"]
 SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
              "-Xarch_host", "-fno-sanitize-recover=undefined"]
 
 
 def build_sanitized(verbose: bool = True) -> str:
     """Host-side AddressSanitizer + UndefinedBehaviorSanitizer build: _build/san/libaudiokv_san.so and, against it,
-    the checkers in _build/san/ (tests/abi_host_check.cpp and tests/abi_accumulated_check.cpp), which drive the host paths of the
+    the checkers in _build/san/ (tests/abi_host_check.cpp and its like), which drive the host paths of the
     entry points. Device code is compiled as usual (GPU sanitizers are not used). Returns the path of the first checker."""
     if not all(os.path.exists(os.path.join(BUILD, f.replace(".hip", ".o"))) for f in sources()):
         build(verbose=False)

@@ -748,6 +748,8 @@ static int32_t plan_shared(const audiokv_params* p, int32_t n_items, int64_t tot
         return fail(AUDIOKV_E_INVALID_ARG, "n_items %d, n_seqs %d, max_own %d or total_rows %lld out of range", n_items, n_seqs, max_own,
                     (long long)total_rows);
     if (n_items > 0 && max_seqs < 1) return fail(AUDIOKV_E_INVALID_ARG, "max_seqs %d < 1", max_seqs);
+    // twice a number of rows, and a number rounded up to a tile, are 32-bit in the kernels
+    if (max_own >= 1 << 30) return fail(AUDIOKV_E_UNSUPPORTED, "max_own %d is not below 2^30", max_own);
     if ((long long)n_items * p->n_kv_heads > (1 << 20) || (long long)n_seqs * p->n_q_heads > (1 << 22))
         return fail(AUDIOKV_E_UNSUPPORTED, "too many heads in one call");
     *g = make_geom(p, n_seqs);

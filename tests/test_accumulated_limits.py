@@ -1,0 +1,35 @@
+"""The largest sizes that accumulate, decode_shared and evict_accumulated can be asked for: right, or refused. CPU only."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def A():
+    import paper_2604_06694_amd as A
+    return A
+
+
+def test_decode_shared_workspace_up_to_the_last_number(A):
+    """A logit per query head and own row is the least that a step needs."""
+    p = A.Params(8, 2, 64, 0)
+    for own in (2**30 - 1, 2**30, 2**31 - 64, 2**31 - 1):
+        try:
+            assert A.decode_shared_workspace_bytes(p, 0, 0, 1, 0, own) >= 8 * own * 4, own
+        except A.AudioKVError as e:
+            assert e.code == -2 and own >= 2**30
+
+
+@pytest.mark.skipif(shutil.which("hipcc") is None, reason="hipcc not available")
+def test_limits_under_asan_and_ubsan():
+    from paper_2604_06694_amd.build import build_sanitized
+    exe = os.path.join(os.path.dirname(build_sanitized(verbose=False)), "abi_accumulated_limits_check")
+    env = dict(os.environ)
+    env["ASAN_OPTIONS"] = "detect_leaks=0:abort_on_error=0:verify_asan_link_order=0"
+    env["UBSAN_OPTIONS"] = "print_stacktrace=1:halt_on_error=1"
+    r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=300)
+    assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-4000:]
+    assert "all checks passed" in r.stdout
+    assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr, r.stderr[-4000:]
