@@ -11,6 +11,7 @@
 // Bound: latency of a chain of barriers. The rows themselves are moved by the same workgroup where they are few, otherwise by
 // a second launch with several workgroups per head.
 #include "mfma_tile.h"
+#include "row_moves.h"
 
 namespace audiokv {
 
@@ -332,10 +333,10 @@ __global__ __launch_bounds__(256) void evict_move_kernel(EvictAccum a, int parts
 {
     const int head = blockIdx.x / parts, part = blockIdx.x - head * parts, x = head / a.g.H_kv, h = head - x * a.g.H_kv;
     const int32_t* listed = a.moves + (int64_t)head * (1 + 2 * a.max_moves);
-    const int per = a.g.D >> 2, n = listed[0] * per;
+    const int n = listed[0];
+    const MoveWalk walk = move_walk(part * 256 + threadIdx.x, parts * 256, a.g.D >> 2);
 #pragma unroll 4
-    for (int i = part * 256 + threadIdx.x; i < n; i += parts * 256)
-        move_piece(a, x, h, listed[1 + 2 * (i / per)], listed[2 + 2 * (i / per)], i % per);
+    for (int i = walk.first; i < n; i += walk.step) move_piece(a, x, h, listed[1 + 2 * i], listed[2 + 2 * i], walk.piece);
 }
 
 // no head moves more rows than this

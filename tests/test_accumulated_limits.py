@@ -33,3 +33,17 @@ def test_limits_under_asan_and_ubsan():
     assert r.returncode == 0, r.stdout[-2000:] + r.stderr[-4000:]
     assert "all checks passed" in r.stdout
     assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr, r.stderr[-4000:]
+
+
+def test_pieces_of_moved_rows(tmp_path):
+    """The pieces of 2^25 moved rows at head_dim 256 are more than 32 bits count: moves are counted."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "row_moves_check")
+    r = subprocess.run(["hipcc", "-x", "hip", "--offload-arch=gfx950", "--offload-host-only", "-std=c++20", "-O1", "-I",
+                        os.path.join(root, "paper_2604_06694_amd", "csrc"), os.path.join(root, "tests", "row_moves_check.cpp"), "-o", exe],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0, r.stderr
+    with open(os.path.join(root, "paper_2604_06694_amd", "csrc", "evict_accumulated.hip")) as f:
+        assert "listed[0] * per" not in f.read()
