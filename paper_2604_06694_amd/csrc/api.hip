@@ -712,13 +712,13 @@ int32_t audiokv_accumulate(const audiokv_params* params, const void* q, const vo
     Geom g;
     AccumPlan plan;
     AUDIOKV_TRY(check_queries(params, n_items, seqlens_host, queries_host, &g, &plan));
-    if (!q || !k || !cu_seqlens_dev || !cu_queries_dev || !weights || !workspace)
+    const size_t need = (lse_dev ? 0 : accumulate_stats_bytes(plan)) + accumulate_parts_bytes(g, plan);
+    if ((!q && plan.max_Q > 0) || !k || !cu_seqlens_dev || !cu_queries_dev || !weights || (!workspace && need > 0))
         return fail(AUDIOKV_E_INVALID_ARG, "audiokv_accumulate: NULL pointer argument");
     if (!aligned16(q) || !aligned16(k) || !aligned16(workspace))
         return fail(AUDIOKV_E_INVALID_ARG, "q, k and the workspace must be 16-byte aligned");
     if (weights_pitch != 0 && weights_pitch < plan.max_L)
         return fail(AUDIOKV_E_INVALID_ARG, "weights_pitch %lld < longest item %d", (long long)weights_pitch, plan.max_L);
-    const size_t need = (lse_dev ? 0 : accumulate_stats_bytes(plan)) + accumulate_parts_bytes(g, plan);
     if (workspace_bytes < need)
         return fail(AUDIOKV_E_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
     if (plan.max_Q == 0) return AUDIOKV_OK;           // no query anywhere: nothing to add

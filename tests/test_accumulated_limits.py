@@ -1,4 +1,5 @@
 """The largest sizes that accumulate, decode_shared and evict_accumulated can be asked for: right, or refused. CPU only."""
+import ctypes as C
 import os
 import shutil
 import subprocess
@@ -47,3 +48,22 @@ def test_pieces_of_moved_rows(tmp_path):
     assert r.returncode == 0, r.stderr
     with open(os.path.join(root, "paper_2604_06694_amd", "csrc", "evict_accumulated.hip")) as f:
         assert "listed[0] * per" not in f.read()
+
+
+PTR = C.c_void_p(4096)          # never read
+
+
+def accumulate(A, lens, queries, q=PTR, workspace=PTR, size=1 << 40, lse=None, k=PTR):
+    cp = A.Params(8, 2, 64, 0).c()
+    i32 = C.c_int32 * len(lens)
+    return A.binding._lib.audiokv_accumulate(C.byref(cp), q, k, lse, PTR, i32(*lens), PTR, i32(*queries), len(lens), PTR, C.c_int64(0),
+                                             workspace, C.c_size_t(size), None)
+
+
+def test_accumulate_of_no_query_needs_neither_queries_nor_workspace(A):
+    """An empty tensor of queries has no address, and a workspace of no bytes none either."""
+    assert A.accumulate_workspace_bytes(A.Params(8, 2, 64, 0), [10, 7], [0, 0]) == 0
+    assert accumulate(A, [10, 7], [0, 0], q=None, workspace=None, size=0) == 0
+    assert accumulate(A, [10, 7], [0, 0], k=None) == -1           # the rest is looked at
+    assert accumulate(A, [10, 7], [1, 0], q=None) == -1
+    assert accumulate(A, [10, 7], [1, 0], workspace=None) == -1
