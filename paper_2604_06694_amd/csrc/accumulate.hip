@@ -36,14 +36,12 @@ struct Accum {
     const int32_t* cu_q;
     const float* lse;          // given, or nullptr
     float* norms;              // [row of all items]: log2 of the row's sum of exp2
-    float2* stats;             // [part][row of all items] (reference, sum), of rows whose block has several parts
-    float* parts;              // [part][head][part_pitch] column sums, of keys whose block has several
+    float2* stats;             // [part_slot][row of the block] (reference, sum), of blocks that have several parts
+    float* parts;              // [part_slot][key of the block] column sums, of blocks that have several
     float* weights;
     int64_t pitch;             // between heads of weights; 0: packed like scores
-    int64_t rows_total;        // of all items
     unsigned div_g;            // r / G = umulhi(r, div_g), G > 1
     int block;                 // rows (keys) of a block of the sweep
-    int part_pitch;
     AccumSpans spans;          // of the sweep (a kernel's arguments hold no more than 4 KB)
 };
 static_assert(sizeof(Accum) < 4000);
@@ -377,7 +375,7 @@ struct Wave {
     }
 };
 
-// The parts of blocks in a workgroup's span: body(place, head, block, first tile, tiles, part, whether the block has others).
+// The parts of blocks in a workgroup's span: body(place, head, block, first tile, tiles, the part's slot, whether the block has others).
 // Neighbouring spans go to one XCD, whose L2 then holds the head that they are about.
 template <bool COLS, int SIZE, class Body>
 __device__ __forceinline__ void for_parts(const Accum& a, Body body)
@@ -394,7 +392,7 @@ __device__ __forceinline__ void for_parts(const Accum& a, Body body)
             continue;
         }
         const int tiles = p.item_of.tiles(COLS, block, SIZE), stop = head == end.head && block == end.block ? min(tiles, end.tile) : tiles;
-        if (tile < stop) body(p, head, block, tile, stop - tile, tile > 0 ? w - s.first_of(head, block, w) : 0, stop - tile < tiles);
+        if (tile < stop) body(p, head, block, tile, stop - tile, part_slot(w, tile > 0), stop - tile < tiles);
         ++block;
         tile = 0;
     }
@@ -406,7 +404,7 @@ __global__ __launch_bounds__(kSweepThreads, 2) void accumulate_rows_kernel(Accum
 {
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    for_parts<false, stationary(NB)>(a, [&](const Place& p, int, int block, int tile0, int n_tiles, int part, bool shared) {
+    for_parts<false, stationary(NB)>(a, [&](const Place& p, int, int block, int tile0, int n_tiles, int slot, bool shared) {
         const int j0 = tile0 * kStream;
         if (wave == kComputeWaves) {
             load_stream<D>(lds, n_tiles, KeyWalk(a, p, j0), [](int) {});
@@ -442,7 +440,7 @@ __global__ __launch_bounds__(kSweepThreads, 2) void accumulate_rows_kernel(Accum
             const float sum = w.l[b] * fast_exp2(w.m[b] - ref) + l2 * fast_exp2(m2 - ref);
             const int r = r_wave + b * 32 + w.col;
             if (w.hf == 0 && r < p.R) {
-                if (shared) a.stats[part * a.rows_total + stat_row(a, p, r)] = make_float2(M, sum);
+                if (shared) a.stats[slot * stationary(NB) + wave * NB * 32 + b * 32 + w.col] = make_float2(M, sum);
                 else a.norms[stat_row(a, p, r)] = norm_from(M, sum);
             }
         }
@@ -460,12 +458,12 @@ __global__ __launch_bounds__(kThreads) void accumulate_norm_kernel(Accum a, int 
     if (n == 1) return;
     const int end = min((block + 1) * a.block, p.R);
     for (int r = block * a.block + threadIdx.x; r < end; r += kThreads) {
-        const float2* st = a.stats + stat_row(a, p, r);
+        const float2* st = a.stats + (r - block * a.block);
         float M = -INFINITY, Z = 0.f;
         for (int c0 = 0; c0 < n; c0 += 8) {
             float2 s[8];
 #pragma unroll
-            for (int c = 0; c < 8; ++c) s[c] = st[min(c0 + c, n - 1) * a.rows_total];
+            for (int c = 0; c < 8; ++c) s[c] = st[part_slot_of(first, min(c0 + c, n - 1)) * a.block];
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
                 if (c0 + c >= n) continue;
@@ -485,7 +483,7 @@ __global__ __launch_bounds__(kSweepThreads, 2) void accumulate_cols_kernel(Accum
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
     float* norm = reinterpret_cast<float*>(lds + kStages * kStream * D * 2);      // of a tile's rows, beside the tile in the ring
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    for_parts<true, stationary(NB)>(a, [&](const Place& p, int head, int block, int tile0, int n_tiles, int part, bool shared) {
+    for_parts<true, stationary(NB)>(a, [&](const Place& p, int head, int block, int tile0, int n_tiles, int slot, bool shared) {
         const int r0 = p.item_of.key_tiles_from(block, stationary(NB)) + tile0 * kStream;
         if (wave == kComputeWaves) {
             load_stream<D>(lds, n_tiles, RowWalk(a, p, r0), [&](int t) {
@@ -545,7 +543,7 @@ __global__ __launch_bounds__(kSweepThreads, 2) void accumulate_cols_kernel(Accum
             const int j = key0 + b * 32 + key_of(lane & 15, w.hf);
             if (w.col < 16 && j < p.L) {
                 if (shared) {
-                    a.parts[((int64_t)part * a.g.n_items * a.g.H_kv + head) * a.part_pitch + j] = mine;
+                    a.parts[slot * stationary(NB) + wave * NB * 32 + b * 32 + key_of(lane & 15, w.hf)] = mine;
                 } else {
                     float* to = a.weights + (a.pitch ? head * a.pitch : p.tok0 * a.g.H_kv + (int64_t)p.h * p.L);
                     to[j] += mine;
@@ -564,13 +562,12 @@ __global__ __launch_bounds__(kThreads) void accumulate_join_kernel(Accum a, int 
     int first, n;
     parts_of(a.spans, head, block, &first, &n);
     if (n == 1) return;
-    const int64_t step = (int64_t)a.g.n_items * a.g.H_kv * a.part_pitch;
     const int end = min((block + 1) * a.block, p.L);
     for (int j = block * a.block + threadIdx.x; j < end; j += kThreads) {
-        const float* src = a.parts + (int64_t)head * a.part_pitch + j;
+        const float* src = a.parts + (j - block * a.block);
         float v = 0.f;
 #pragma unroll 8
-        for (int c = 0; c < n; ++c) v += src[c * step];
+        for (int c = 0; c < n; ++c) v += src[part_slot_of(first, c) * a.block];
         a.weights[(a.pitch ? head * a.pitch : p.tok0 * a.g.H_kv + (int64_t)p.h * p.L) + j] += v;
     }
 }
@@ -604,15 +601,14 @@ AccumPlan accumulate_plan(const Geom& g, const int32_t* seqlens, const int32_t* 
 
 namespace {
 inline size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
-inline int part_pitch(const AccumPlan& p) { return p.cols.max_blocks * p.cols.size; }
+// entries for the parts of blocks that have several
+inline size_t part_entries(const AccumSweep& s) { return s.max_parts > 1 ? (size_t)part_slots(s.spans.n) * s.size : 0; }
 }  // namespace
 
 size_t accumulate_stats_bytes(const AccumPlan& p) {
-    return up((size_t)p.rows_total * sizeof(float)) + (p.rows.max_parts > 1 ? up((size_t)p.rows.max_parts * (size_t)p.rows_total * sizeof(float2)) : 0);
+    return up((size_t)p.rows_total * sizeof(float)) + up(part_entries(p.rows) * sizeof(float2));
 }
-size_t accumulate_parts_bytes(const Geom& g, const AccumPlan& p) {
-    return p.cols.max_parts > 1 ? (size_t)p.cols.max_parts * g.n_items * g.H_kv * part_pitch(p) * sizeof(float) : 0;
-}
+size_t accumulate_parts_bytes(const AccumPlan& p) { return part_entries(p.cols) * sizeof(float); }
 namespace {
 // more than 64 KB of LDS have to be asked for, once per device and kernel
 template <class Kernel>
@@ -666,9 +662,7 @@ hipError_t launch_accumulate(const Geom& g, const AccumPlan& p, const void* q, c
     a.parts = reinterpret_cast<float*>(ws + (lse ? 0 : accumulate_stats_bytes(p)));
     a.weights = weights;
     a.pitch = pitch;
-    a.rows_total = p.rows_total;
     a.div_g = g.G > 1 ? (unsigned)((0x100000000ULL + g.G - 1) / g.G) : 0;
-    a.part_pitch = part_pitch(p);
     switch (g.D) {
         case 64:  return launch_sweeps<64>(g, p, a, s);
         case 128: return launch_sweeps<128>(g, p, a, s);

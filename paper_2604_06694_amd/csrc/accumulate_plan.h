@@ -4,7 +4,8 @@
 // A sweep is a list of blocks (of rows, or of keys, head by head), each a number of tiles of the other side, and kBlockCost tiles'
 // time to begin with: its stationary operand is loaded, and what lies on the diagonal goes at half speed. The list is cut into
 // spans of equal cost, one per workgroup and CU, wherever that is; a workgroup does the tiles of its span block by block. A
-// block that a span's end cuts has several parts, in the order of the workgroups.
+// block that a span's end cuts has several parts, in the order of the workgroups. A workgroup has at most two of those: what its
+// span begins with, if that is not a block's beginning, and what it ends with. What it finds for them goes to slots of its own.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -50,13 +51,19 @@ struct SpanStart {
 struct AccumSpans {
     int n = 0;                            // workgroups
     SpanStart at[kSpans + 1];             // workgroup w ends where w + 1 begins; from n on: the end
-    // The first workgroup with tiles of a block, `near` one that has some
+    // The first workgroup with tiles of a block, `near` one that has some (what the host check holds parts_of to)
     __host__ __device__ int first_of(int head, int block, int near) const {
         int w = near;
         while (w > 0 && at[w].after(head, block)) --w;
         return w;
     }
 };
+
+// Slots of workgroup w, for the rest of a block that an earlier workgroup began and for a block that it begins and others end
+__host__ __device__ inline int part_slots(int workgroups) { return 2 * workgroups; }
+__host__ __device__ inline int part_slot(int w, bool begun) { return 2 * w + (begun ? 0 : 1); }
+// part c of a block whose first workgroup is `first`
+__host__ __device__ inline int part_slot_of(int first, int c) { return part_slot(first + c, c > 0); }
 
 // The workgroups of a block, found by a wave at once: how many begin up to its first tile, and up to its last
 __device__ __forceinline__ void parts_of(const AccumSpans& s, int head, int block, int* first, int* n) {

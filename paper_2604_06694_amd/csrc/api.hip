@@ -698,7 +698,7 @@ int32_t audiokv_accumulate_workspace_bytes(const audiokv_params* params, int32_t
     Geom g;
     AccumPlan plan;
     AUDIOKV_TRY(check_queries(params, n_items, seqlens_host, queries_host, &g, &plan));
-    *out_bytes = accumulate_stats_bytes(plan) + accumulate_parts_bytes(g, plan);
+    *out_bytes = accumulate_stats_bytes(plan) + accumulate_parts_bytes(plan);
     return AUDIOKV_OK;
 }
 
@@ -712,7 +712,7 @@ int32_t audiokv_accumulate(const audiokv_params* params, const void* q, const vo
     Geom g;
     AccumPlan plan;
     AUDIOKV_TRY(check_queries(params, n_items, seqlens_host, queries_host, &g, &plan));
-    const size_t need = (lse_dev ? 0 : accumulate_stats_bytes(plan)) + accumulate_parts_bytes(g, plan);
+    const size_t need = (lse_dev ? 0 : accumulate_stats_bytes(plan)) + accumulate_parts_bytes(plan);
     if ((!q && plan.max_Q > 0) || !k || !cu_seqlens_dev || !cu_queries_dev || !weights || (!workspace && need > 0))
         return fail(AUDIOKV_E_INVALID_ARG, "audiokv_accumulate: NULL pointer argument");
     if (!aligned16(q) || !aligned16(k) || !aligned16(workspace))

@@ -148,7 +148,7 @@ hipError_t launch_decode(const Geom& g, const void* q, const void* k_cache, cons
 struct AccumPlan;                          // accumulate_plan.h
 AccumPlan accumulate_plan(const Geom& g, const int32_t* seqlens_host, const int32_t* queries_host, int n_items);
 size_t accumulate_stats_bytes(const AccumPlan& p);       // none of it is used where the log-sum-exp is given
-size_t accumulate_parts_bytes(const Geom& g, const AccumPlan& p);
+size_t accumulate_parts_bytes(const AccumPlan& p);
 hipError_t launch_accumulate(const Geom& g, const AccumPlan& p, const void* q, const void* k, const int32_t* cu_seqlens,
                              const int32_t* cu_queries, const float* lse, float* weights, int64_t pitch, void* workspace, hipStream_t s);
 

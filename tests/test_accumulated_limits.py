@@ -36,17 +36,23 @@ def test_limits_under_asan_and_ubsan():
     assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr, r.stderr[-4000:]
 
 
-def test_pieces_of_moved_rows(tmp_path):
-    """The pieces of 2^25 moved rows at head_dim 256 are more than 32 bits count: moves are counted."""
-    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-    exe = str(tmp_path / "row_moves_check")
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def run_on_host(check, tmp_path):
+    exe = str(tmp_path / check)
     r = subprocess.run(["hipcc", "-x", "hip", "--offload-arch=gfx950", "--offload-host-only", "-std=c++20", "-O1", "-I",
-                        os.path.join(root, "paper_2604_06694_amd", "csrc"), os.path.join(root, "tests", "row_moves_check.cpp"), "-o", exe],
-                       capture_output=True, text=True)
+                        os.path.join(ROOT, "paper_2604_06694_amd", "csrc"), "-I", os.path.join(ROOT, "include"),
+                        os.path.join(ROOT, "tests", check + ".cpp"), "-o", exe], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert r.returncode == 0, r.stderr
-    with open(os.path.join(root, "paper_2604_06694_amd", "csrc", "evict_accumulated.hip")) as f:
+
+
+def test_pieces_of_moved_rows(tmp_path):
+    """The pieces of 2^25 moved rows at head_dim 256 are more than 32 bits count: moves are counted."""
+    run_on_host("row_moves_check", tmp_path)
+    with open(os.path.join(ROOT, "paper_2604_06694_amd", "csrc", "evict_accumulated.hip")) as f:
         assert "listed[0] * per" not in f.read()
 
 
@@ -67,3 +73,17 @@ def test_accumulate_of_no_query_needs_neither_queries_nor_workspace(A):
     assert accumulate(A, [10, 7], [0, 0], k=None) == -1           # the rest is looked at
     assert accumulate(A, [10, 7], [1, 0], q=None) == -1
     assert accumulate(A, [10, 7], [1, 0], workspace=None) == -1
+
+
+@pytest.mark.parametrize("heads,lens,queries", [((32, 8), [131072] + [500] * 255, None), ((28, 4), [131072] + [300] * 255, [2000] + [300] * 255),
+                                                ((28, 4), [32768] * 28, None), ((1, 1), [1], None)])
+def test_accumulate_workspace_does_not_grow_with_ragged_items(A, heads, lens, queries):
+    """A norm per query, and what 256 workgroups at most find for the two blocks at most that each shares with others: a
+    (reference, sum) per row, a sum per key, of blocks of at most 448."""
+    queries = queries or lens
+    most = heads[0] * sum(queries) * 4 + 2 * 256 * 448 * (8 + 4) + 3 * 256
+    assert A.accumulate_workspace_bytes(A.Params(*heads, 128, 0), lens, queries) <= most
+
+
+def test_slots_of_shared_blocks(tmp_path):
+    run_on_host("accumulate_slots_check", tmp_path)
