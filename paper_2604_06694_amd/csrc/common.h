@@ -159,7 +159,8 @@ struct SharedPlan {
     long long slots = 0;                       // of chunks: every head leaves at most one empty
     int own_chunk = 0, own_chunks = 0;         // own rows: of a chunk, chunks of a head
     int logit_pitch = 0;
-    size_t stats_p = 0, stats_o = 0, after = 0, part_p = 0, part_o = 0, logits = 0, bytes = 0;    // offsets in the workspace
+    long long later_at = 0, own_at = 0;        // results of the prompts' later chunks, and of own rows
+    size_t stats = 0, after = 0, part = 0, logits = 0, bytes = 0;    // offsets in the workspace
 };
 struct SharedCall {
     const void *q, *k_prompt, *v_prompt;

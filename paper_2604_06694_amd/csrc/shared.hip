@@ -53,8 +53,13 @@ struct Shared {
     int capacity, max_own, own_chunk, own_chunks;
     const __bf16 *k_new, *v_new;
     const int32_t* pos_new;
-    float *part_p, *part_o;                   // [slot][max_seqs * G][D], [own head][chunk][G][D]
-    float2 *stats_p, *stats_o;                // (reference, sum) of the same
+    // What the chunks have found, by query: [D] sums and (reference, sum). A head's first chunk has a place per sequence, [KV head][seq][G];
+    // later ones begin in the row block (of a chunk's length, from the prompts' first row on) that no other chunk begins in, and have
+    // [row block - 1][max_seqs][G]; own rows' [own head][chunk][G]. So all of it follows the sequences that there are, not the widest
+    // item times the heads.
+    float* part;
+    float2* stats;
+    int64_t later_at, own_at;                 // where the second and third begin
     float* logits;                            // [own head][G][logit_pitch], base 2
     int logit_pitch;
     int32_t* after;                           // [own head]: 2 * rows after the step + whether one was appended
@@ -381,9 +386,9 @@ __global__ __launch_bounds__(kThreads, 2) void shared_partial_kernel(Shared a)
         rows.k = a.kp + row0 * D;
         rows.v = a.vp + row0 * D;
         rows.stride = D;
-        const int64_t base = (int64_t)slot * a.max_seqs * a.g.G;
-        part = a.part_p + base * D;
-        stats = a.stats_p + base;
+        const int64_t base = c == 0 ? ((int64_t)h * a.n_seqs + first_seq) * a.g.G : a.later_at + ((row0 >> a.log_r) - 1) * a.max_seqs * a.g.G;
+        part = a.part + base * D;
+        stats = a.stats + base;
     } else {
         const int id = blockIdx.x - prompt_blocks, own = id / a.own_chunks, c = id - own * a.own_chunks;
         const int x = own / a.g.H_kv;
@@ -409,34 +414,34 @@ __global__ __launch_bounds__(kThreads, 2) void shared_partial_kernel(Shared a)
             rows.k_dst = a.ko + at + rows.fresh * rows.stride;
             rows.v_dst = a.vo + at + rows.fresh * rows.stride;
         }
-        const int64_t base = ((int64_t)own * a.own_chunks + c) * a.g.G;
-        part = a.part_o + base * D;
-        stats = a.stats_o + base;
+        const int64_t base = a.own_at + ((int64_t)own * a.own_chunks + c) * a.g.G;
+        part = a.part + base * D;
+        stats = a.stats + base;
         if (a.weights) rows.logits = a.logits + (int64_t)own * a.g.G * a.logit_pitch + j0;
     }
     attend<D>(a, rows, first_seq, h, r_first, r_end, part, stats);
 }
 
-// The chunks that a query of sequence x has rows in: first those of the prompt, then its own
+// The chunks that a query of sequence x has rows in, first those of the prompt, then its own: where each has its result
 struct Chunks {
-    const float2 *sp, *so;     // statistics of the first of each, and the distance from chunk to chunk
-    int64_t step_p, step_o;
-    int np, no;
-    __device__ __forceinline__ float2 stat(int c) const { return c < np ? sp[c * step_p] : so[(c - np) * step_o]; }
+    int64_t first, later, own; // of the prompt's chunk 0, of its chunk c less c steps, of the first own one
+    int64_t step;
+    int np, no, G;
+    __device__ __forceinline__ int64_t at(int c) const { return c >= np ? own + (int64_t)(c - np) * G : c == 0 ? first : later + c * step; }
 };
 // after: of the sequence's own head h
 __device__ __forceinline__ Chunks chunks_of(const Shared& a, int x, ItemOf it, int h, int gq, int after) {
-    Chunks t{a.stats_p, a.stats_o, 0, 0, 0, 0};
+    Chunks t{0, 0, 0, 0, 0, 0, a.g.G};
     if (a.cu_seqs) {
         const int head = it.item * a.g.H_kv + h, begin = head_start(a, head), n = head_start(a, head + 1) - begin;
         t.np = n > 0 ? (n + (1 << a.log_r) - 1) >> a.log_r : 0;
-        t.step_p = (int64_t)a.max_seqs * a.g.G;
-        t.sp = a.stats_p + ((begin >> a.log_r) + head) * t.step_p + (int64_t)(x - it.first) * a.g.G + gq;
+        t.step = (int64_t)a.max_seqs * a.g.G;
+        t.first = ((int64_t)h * a.n_seqs + x) * a.g.G + gq;
+        t.later = a.later_at + ((begin >> a.log_r) - 1) * t.step + (int64_t)(x - it.first) * a.g.G + gq;
     }
     if (a.own_chunks > 0) {
         t.no = ((after >> 1) + a.own_chunk - 1) / a.own_chunk;
-        t.step_o = a.g.G;
-        t.so = a.stats_o + (int64_t)(x * a.g.H_kv + h) * a.own_chunks * a.g.G + gq;
+        t.own = a.own_at + (int64_t)(x * a.g.H_kv + h) * a.own_chunks * a.g.G + gq;
     }
     return t;
 }
@@ -464,7 +469,7 @@ __device__ __forceinline__ void add_weights(const Shared& a, int own, int j0)
         const Chunks t = chunks_of(a, x, it, h, gq, after);
         float m = -INFINITY, l = 0.f;
         for (int c = lane; c < t.np + t.no; c += 64) {
-            const float2 s = t.stat(c);
+            const float2 s = a.stats[t.at(c)];
             const float m2 = fmaxf(m, s.x), ref = m2 == -INFINITY ? 0.f : m2;
             l = l * fast_exp2(m - ref) + s.y * fast_exp2(s.x - ref);
             m = m2;
@@ -523,7 +528,7 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int wei
     const int nc = t.np + t.no;
     float m = -INFINITY, l = 0.f;
     for (int c = tid; c < nc; c += THREADS) {
-        const float2 s = t.stat(c);
+        const float2 s = a.stats[t.at(c)];
         const float m2 = fmaxf(m, s.x), ref = m2 == -INFINITY ? 0.f : m2;
         l = l * fast_exp2(m - ref) + s.y * fast_exp2(s.x - ref);
         m = m2;
@@ -549,12 +554,13 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(Shared a, int wei
     }
     // a thread has four channels of every (THREADS / (D / 4))-th chunk
     const int log_quads = 29 - __builtin_clz(D), quads = 1 << log_quads, groups = THREADS >> log_quads, ch = tid & (quads - 1), grp = tid >> log_quads;
-    const f32x4* pp = reinterpret_cast<const f32x4*>(a.part_p + (t.sp - a.stats_p) * D) + ch;
-    const f32x4* po = reinterpret_cast<const f32x4*>(a.part_o + (t.so - a.stats_o) * D) + ch;
+    const f32x4* part = reinterpret_cast<const f32x4*>(a.part) + ch;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int c = grp; c < nc; c += groups)
-        acc += (c < t.np ? pp[c * t.step_p * quads] : po[(c - t.np) * t.step_o * quads]) * fast_exp2(t.stat(c).x - ref);
+    for (int c = grp; c < nc; c += groups) {
+        const int64_t at = t.at(c);
+        acc += part[at * quads] * fast_exp2(a.stats[at].x - ref);
+    }
     if constexpr (WAVES > 1) {
         red[tid] = acc;
         __syncthreads();
@@ -594,7 +600,7 @@ constexpr int kWaveFloats = 4096;
 SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_seqs, int max_seqs, int max_own)
 {
     SharedPlan p;
-    long long slots = 0, chunks = 0;            // what the workspace is charged
+    long long later = 0, chunks = 0;            // what the workspace is charged
     if (n_items > 0) {
         p.row_block = max_row_block(g.D);
         p.row_blocks = (int)(((long long)max_seqs * g.G + p.row_block - 1) / p.row_block);
@@ -603,8 +609,10 @@ SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_s
         p.log_r = 7;
         while (p.log_r < 16 && (total_rows >> (p.log_r + 1)) >= wanted) ++p.log_r;
         p.slots = (total_rows >> p.log_r) + (long long)n_items * g.H_kv;
-        slots = p.slots;                        // where the chunks double, the slots halve
-        if (p.log_r > 7 && (total_rows >> p.log_r) < 2 * wanted - 1) slots = 2 * wanted - 1 + (long long)n_items * g.H_kv;
+        p.later_at = (long long)n_seqs * g.H_q;
+        p.own_at = p.later_at + (total_rows >> p.log_r) * max_seqs * g.G;
+        later = total_rows >> p.log_r;          // where the chunks double, their number halves
+        if (p.log_r > 7 && later < 2 * wanted - 1) later = 2 * wanted - 1;
     }
     if (max_own > 0) {
         const long long heads = (long long)n_seqs * g.H_kv;
@@ -617,12 +625,10 @@ SharedPlan shared_plan(const Geom& g, int n_items, long long total_rows, int n_s
     }
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
-    const size_t prompt = (size_t)slots * max_seqs * g.G, own = (size_t)n_seqs * g.H_kv * chunks * g.G;
-    p.stats_p = take(prompt * sizeof(float2));
-    p.stats_o = take(own * sizeof(float2));
+    const size_t parts = (size_t)p.later_at + (size_t)later * max_seqs * g.G + (size_t)n_seqs * g.H_q * chunks;
+    p.stats = take(parts * sizeof(float2));
     p.after = take((size_t)n_seqs * g.H_kv * sizeof(int32_t));
-    p.part_p = take(prompt * g.D * sizeof(float));
-    p.part_o = take(own * g.D * sizeof(float));
+    p.part = take(parts * g.D * sizeof(float));
     p.logits = take((size_t)n_seqs * g.H_q * p.logit_pitch * sizeof(float));
     p.bytes = at;
     return p;
@@ -665,11 +671,11 @@ hipError_t launch_shared(const Geom& g, const SharedPlan& p, const SharedCall& c
     a.k_new = static_cast<const __bf16*>(c.k_new);
     a.v_new = static_cast<const __bf16*>(c.v_new);
     a.pos_new = c.pos_new;
-    a.stats_p = reinterpret_cast<float2*>(ws + p.stats_p);
-    a.stats_o = reinterpret_cast<float2*>(ws + p.stats_o);
+    a.stats = reinterpret_cast<float2*>(ws + p.stats);
+    a.later_at = p.later_at;
+    a.own_at = p.own_at;
     a.after = reinterpret_cast<int32_t*>(ws + p.after);
-    a.part_p = reinterpret_cast<float*>(ws + p.part_p);
-    a.part_o = reinterpret_cast<float*>(ws + p.part_o);
+    a.part = reinterpret_cast<float*>(ws + p.part);
     a.logits = reinterpret_cast<float*>(ws + p.logits);
     a.logit_pitch = p.logit_pitch;
     a.out = static_cast<__bf16*>(c.out);

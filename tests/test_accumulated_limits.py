@@ -87,3 +87,12 @@ def test_accumulate_workspace_does_not_grow_with_ragged_items(A, heads, lens, qu
 
 def test_slots_of_shared_blocks(tmp_path):
     run_on_host("accumulate_slots_check", tmp_path)
+
+
+@pytest.mark.parametrize("items,rows,seqs,most", [(64, 64 * 4 * 5000, 512, 512), (500, 500 * 4 * 400, 999, 500), (1, 4 * 13107, 32, 32)])
+def test_decode_shared_workspace_follows_the_sequences(A, items, rows, seqs, most):
+    """A result per sequence, query head and first chunk, and per sequence of the widest item and later chunk, of which there are
+    less than twice as many as wanted: 384 workgroups, in blocks of 128 query rows."""
+    blocks = -(-most * 7 // 128)
+    results = seqs * 28 + 2 * -(-384 // blocks) * most * 7
+    assert A.decode_shared_workspace_bytes(A.Params(28, 4, 128, 0), items, rows, seqs, most, 0) <= results * (128 * 4 + 8) + seqs * 4 * 4 + 4 * 256
