@@ -128,7 +128,7 @@ __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int fi
     const int G = a.g.G;
     // waves over query rows, and, where these leave some and a tile has two, over its halves
     const int left = r_end - r_first, wq_n = left <= 32 ? 1 : left <= 64 || W::kRowWaves == 2 ? 2 : 4;
-    const int part_of = wave % W::kSplit, wq = wave / W::kSplit % wq_n, wk = wave / W::kSplit / wq_n;
+    const int part_of = wave % W::kSplit, wq = __builtin_amdgcn_readfirstlane(wave / W::kSplit % wq_n), wk = wave / W::kSplit / wq_n;
     const bool halves = kTile > 32 && wq_n < 4, works = wk < (halves ? 2 : 1);
     const int sub0 = halves ? wk : 0, sub1 = halves ? wk + 1 : kTile / 32;
     const int r_wave = r_first + wq * 32;
@@ -137,6 +137,15 @@ __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int fi
     const int chunk = piece_chunk<D>() * 8;
     const int64_t apart = piece_row<D>(0) * rows.stride + chunk;
     constexpr int kStep = kThreads / (D / 8);
+    // What only few tiles need is computed where they need it: kept from the start, addresses of the new row and the like took more
+    // registers than d = 256 has left (ten spilled, some in every tile: 24 sequences on eight prompts 47 us a pass instead of 37).
+    auto once = [](int x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+        asm volatile("" : "+v"(x));
+#endif
+        return x;
+    };
+    auto other_half = [&](int x) { return __builtin_amdgcn_ds_bpermute((once(lane) ^ 32) * 4, x); };
     u32x4 kpiece[N], vpiece[N];
     auto plain = [&](int t) { return t + kTile <= rows.n && (rows.fresh < t || rows.fresh >= t + kTile); };
     auto fetch = [&](int t) {
@@ -148,23 +157,25 @@ __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int fi
                 vpiece[u] = *reinterpret_cast<const u32x4*>(rows.v + first + apart);
             }
         } else {
+            const int here = once(chunk);
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const int j = t + piece_row<D>(u);
-                const int64_t at = min(j, rows.n - 1) * rows.stride + chunk;
-                kpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.k_new + chunk : rows.k + at);
-                vpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.v_new + chunk : rows.v + at);
+                const int64_t at = min(j, rows.n - 1) * rows.stride + here;
+                kpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.k_new + here : rows.k + at);
+                vpiece[u] = *reinterpret_cast<const u32x4*>(j == rows.fresh ? rows.v_new + here : rows.v + at);
             }
         }
     };
     auto put = [&](int t, int buffer) {
         if (!plain(t)) {
+            const int here = once(chunk);
 #pragma unroll
             for (int u = 0; u < N; ++u) {
                 const int j = t + piece_row<D>(u);
                 if (j == rows.fresh) {                        // the new row takes its slot
-                    *reinterpret_cast<u32x4*>(rows.k_dst + chunk) = kpiece[u];
-                    *reinterpret_cast<u32x4*>(rows.v_dst + chunk) = vpiece[u];
+                    *reinterpret_cast<u32x4*>(rows.k_dst + here) = kpiece[u];
+                    *reinterpret_cast<u32x4*>(rows.v_dst + here) = vpiece[u];
                 }
                 // rows past the end have weight 0, but 0 times an infinity is NaN
                 vpiece[u] = j < rows.n ? vpiece[u] : u32x4{0, 0, 0, 0};
@@ -223,7 +234,7 @@ __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int fi
             for (int ct = 0; ct < CT; ++ct) vf[ct] = values(vt, 0, ct);
             __builtin_amdgcn_sched_barrier(0);
             if (key0 + 32 > rows.n) {
-                const int most = rows.n - key0 - 4 * hf;
+                const int most = rows.n - key0 - 4 * once(hf);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) z[i] = key_of(i, 0) < most ? z[i] : -INFINITY;
             }
@@ -245,8 +256,8 @@ __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int fi
                 float top = z[0];
 #pragma unroll
                 for (int i = 1; i < 16; ++i) top = fmaxf(top, z[i]);
-                top = fmaxf(top, __shfl_xor(top, 32, 64));
-                const int theirs = __shfl_xor((int)far, 32, 64);       // (in front of the test: all lanes take part)
+                top = fmaxf(top, __int_as_float(other_half(__float_as_int(top))));
+                const int theirs = other_half((int)far);       // (in front of the test: all lanes take part)
                 const bool redo = far | (theirs != 0);
                 const float ref = redo ? fmaxf(m, top * a.g.c_log2) : m, ref0 = ref == -INFINITY ? 0.f : ref;
                 const float by = redo ? fast_exp2(m - ref0) : 1.f;
