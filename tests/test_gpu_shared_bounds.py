@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import audiokv_oracle as O
 from test_gpu_shared import A, Step
 
 pytestmark = pytest.mark.gpu
@@ -25,3 +26,27 @@ def test_ragged_items_and_a_loose_bound(A, H_q, H_kv, d, bound):
     ws = torch.full((A.decode_shared_workspace_bytes(t["p"], len(sharing), len(s.kp), n, most, s.max_own(True)),), 255, dtype=torch.uint8, device="cuda")
     s.call(A, t, max_seqs=most, workspace=ws)
     s.check(t)
+
+
+@pytest.mark.parametrize("stride_head,stride_tok", [((1 << 31) + 4096, 64), (64, 1 << 25)])
+def test_eviction_moves_rows_beyond_32_bits(A, stride_head, stride_tok):
+    """Rows further than 2^31 elements from the first, moved and left where they are: every slot against the oracle."""
+    rng = np.random.default_rng(21)
+    n, C, budget = [71, 67], 72, 40
+    rows = torch.from_numpy(rng.integers(-30000, 30000, (2, 2, C, 64)).astype(np.int16)).cuda().view(torch.bfloat16)       # K, V
+    weights = torch.from_numpy(rng.random((2, C)).astype(np.float32)).cuda()
+    span = stride_head + (C - 1) * stride_tok + 64
+    k, v = (torch.zeros(span, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    views = [x.as_strided((2, C, 64), (stride_head, stride_tok, 1)) for x in (k, v)]
+    views[0].copy_(rows[0]); views[1].copy_(rows[1])
+    slots = A.Slots(k, v, torch.tensor(n, dtype=torch.int32, device="cuda"), C, weights.clone())
+    A.evict_accumulated(A.Params(4, 2, 64, 0, kv_stride_item=8, kv_stride_head=stride_head, kv_stride_tok=stride_tok), slots, 1, budget, 0, C)
+    torch.cuda.synchronize()
+    assert slots.lengths.tolist() == [budget] * 2
+    for h in range(2):
+        w = weights[h, :n[h]].cpu().numpy()
+        src = torch.tensor(O.evict_accumulated(w, np.arange(n[h]), budget, 0) + list(range(budget, C)), device="cuda")
+        assert src[:budget].tolist() != list(range(budget))
+        assert torch.equal(slots.weights[h], weights[h, src])
+        for x, was in zip(views, rows):
+            assert torch.equal(x[h].view(torch.int16), was[h, src].view(torch.int16)), h
