@@ -296,15 +296,14 @@ __global__ __launch_bounds__(THREADS) void evict_rank_kernel(EvictAccum a)
             scan2<THREADS>(scan, holes, movers, moves, all_movers);
             at = equal;
             each([&](int t, unsigned r) {
-                const bool g = goes(r);
-                if (g && t < b) {
-                    if (listed) listed[1 + 2 * holes] = t; else holes_at[holes] = t;
-                    ++holes;
+                const bool g = goes(r), hole = g && t < b, mover = !g && t >= b;
+                if (hole || mover) {
+                    const int i = hole ? holes : movers;
+                    if (listed) listed[(hole ? 1 : 2) + 2 * i] = t;
+                    else (hole ? holes_at : movers_at)[i] = t;
                 }
-                if (!g && t >= b) {
-                    if (listed) listed[2 + 2 * movers] = t; else movers_at[movers] = t;
-                    ++movers;
-                }
+                holes += hole;
+                movers += mover;
             });
         }
         __syncthreads();                                          // (also: every rank has been read)
