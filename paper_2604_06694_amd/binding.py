@@ -104,27 +104,26 @@ class Slots:
     weights: Optional[torch.Tensor] = None   # fp32 [n_seqs * n_kv_heads, capacity]
     positions: Optional[torch.Tensor] = None # int32, the same
 
-    def _c(self, p: Params, n_seqs: int) -> _CSlots:
-        """The C struct, after a look at types and sizes (in one expression: a step is some twenty microseconds of the host's)."""
+    def _c(self, p: Params, n_seqs: int, at: int) -> _CSlots:
+        """The C struct, after a look at types, sizes and the device (in one expression: a step is some twenty microseconds of the host's)."""
         k, v, lengths, w, pos = self.k, self.v, self.lengths, self.weights, self.positions
         heads = n_seqs * p.n_kv_heads
         slots = heads * self.capacity
-        if (k.dtype is not _BF16 or v.dtype is not _BF16 or not k.is_cuda or not v.is_cuda
+        if (k.dtype is not _BF16 or v.dtype is not _BF16 or k.get_device() != at or v.get_device() != at
                 or p.kv_stride_tok == 0 and (not k.is_contiguous() or not v.is_contiguous() or k.numel() < slots * p.head_dim
                                              or v.numel() < slots * p.head_dim)):
-            raise ValueError(f"slots.k and slots.v must be device tensors of dtype {_BF16}, and contiguous with {slots * p.head_dim} values "
-                             "where params has no strides")
+            raise ValueError(f"slots.k and slots.v must be tensors of the current device, {at}, and dtype {_BF16}, and contiguous with "
+                             f"{slots * p.head_dim} values where params has no strides")
         if p.kv_stride_tok != 0 and n_seqs > 0:
             end = ((n_seqs - 1) * p.kv_stride_item + (p.n_kv_heads - 1) * p.kv_stride_head + (self.capacity - 1) * p.kv_stride_tok + p.head_dim)
             if _room(p, k) < end or _room(p, v) < end:
                 raise ValueError(f"slots.k or slots.v has room for {min(_room(p, k), _room(p, v))} values, {end} needed by the strides")
-        if lengths.dtype is not _I32 or not lengths.is_cuda or not lengths.is_contiguous() or lengths.numel() < heads:
-            raise ValueError(f"slots.lengths must be a contiguous device tensor of {heads} values of dtype {_I32}")
-        if w is not None and (w.dtype is not _F32 or not w.is_cuda or not w.is_contiguous() or w.numel() < slots):
-            raise ValueError(f"slots.weights must be a contiguous device tensor of {slots} values of dtype {_F32}")
-        if pos is not None and (pos.dtype is not _I32 or not pos.is_cuda or not pos.is_contiguous() or pos.numel() < slots):
-            raise ValueError(f"slots.positions must be a contiguous device tensor of {slots} values of dtype {_I32}")
-        _here("slots.k slots.v slots.lengths slots.weights slots.positions", k, v, lengths, w, pos)
+        if lengths.dtype is not _I32 or lengths.get_device() != at or not lengths.is_contiguous() or lengths.numel() < heads:
+            raise ValueError(f"slots.lengths must be a contiguous tensor of {heads} values of dtype {_I32} on the current device, {at}")
+        if w is not None and (w.dtype is not _F32 or w.get_device() != at or not w.is_contiguous() or w.numel() < slots):
+            raise ValueError(f"slots.weights must be a contiguous tensor of {slots} values of dtype {_F32} on the current device, {at}")
+        if pos is not None and (pos.dtype is not _I32 or pos.get_device() != at or not pos.is_contiguous() or pos.numel() < slots):
+            raise ValueError(f"slots.positions must be a contiguous tensor of {slots} values of dtype {_I32} on the current device, {at}")
         return _CSlots(_SLOTS_SIZE, self.capacity, k.data_ptr(), v.data_ptr(), lengths.data_ptr(), _ptr(w), _ptr(pos))
 
 
@@ -232,9 +231,26 @@ def _need(t: torch.Tensor, dtype, name: str) -> torch.Tensor:
     return t
 
 
-def _table(t: Optional[torch.Tensor], n: int, name: str) -> None:
+# Kernels go to the current stream of the current device: tensors of another one, or of the host, are refused.
+def _device() -> int:
+    return _raw_device() if _raw_device is not None else torch.cuda.current_device()
+
+
+def _need_at(t: torch.Tensor, dtype, at: int, name: str) -> torch.Tensor:
+    if t.dtype is not dtype or t.get_device() != at or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of dtype {dtype} on the current device, {at}")
+    return t
+
+
+def _workspace_at(t: torch.Tensor, at: int) -> torch.Tensor:
+    if t.get_device() != at or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on the current device, {at}")
+    return t
+
+
+def _table(t: Optional[torch.Tensor], n: int, at: int, name: str) -> None:
     """Exclusive prefix sums of n numbers, if given."""
-    if t is not None and _need(t, _I32, name).numel() < n + 1:
+    if t is not None and _need_at(t, _I32, at, name).numel() < n + 1:
         raise ValueError(f"{name} has {t.numel()} values, {n + 1} needed")
 
 
@@ -251,14 +267,6 @@ def _room(p: Params, t: torch.Tensor) -> int:
     if p.kv_stride_tok == 0:
         return t.numel()
     return t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
-
-
-def _here(names: str, *tensors: Optional[torch.Tensor]) -> None:
-    """Kernels go to the current stream of the current device: tensors of another one, or of the host, are refused."""
-    at = _raw_device() if _raw_device is not None else torch.cuda.current_device()
-    for i, t in enumerate(tensors):
-        if t is not None and t.get_device() != at:
-            raise ValueError(f"{names.split()[i]} is on {t.device}, the current device is {at}")
 
 
 def version() -> int:
@@ -504,8 +512,8 @@ def accumulate(p: Params, q: torch.Tensor, k: torch.Tensor, seqlens: Sequence[in
     """Adds the attention weight that every token receives from the last queries[i] positions of each item to `weights`
     (fp32; zeros of the scores' layout if not given) and returns it. `pitch`: distance between heads of `weights`, 0:
     packed like scores. `lse`: fp32, [n_q_heads][queries[i]] of item after item."""
-    _need(q, torch.bfloat16, "q"); _need(k, torch.bfloat16, "k")
-    _here("q k weights lse cu_seqlens cu_queries workspace", q, k, weights, lse, cu_seqlens, cu_queries, workspace)
+    at = _device()
+    _need_at(q, _BF16, at, "q"); _need_at(k, _BF16, at, "k")
     if len(queries) != len(seqlens):
         raise ValueError(f"{len(queries)} numbers of queries for {len(seqlens)} lengths")
     dev = k.device
@@ -513,21 +521,22 @@ def accumulate(p: Params, q: torch.Tensor, k: torch.Tensor, seqlens: Sequence[in
         raise ValueError("q is smaller than its queries")
     if _room(p, k) < _rows_end(p, seqlens):
         raise ValueError(f"k has room for {_room(p, k)} values, {_rows_end(p, seqlens)} needed")
-    _table(cu_seqlens, len(seqlens), "cu_seqlens"); _table(cu_queries, len(seqlens), "cu_queries")
+    _table(cu_seqlens, len(seqlens), at, "cu_seqlens"); _table(cu_queries, len(seqlens), at, "cu_queries")
     cu = cu_seqlens if cu_seqlens is not None else _cu(seqlens, dev)
     cu_q = cu_queries if cu_queries is not None else _cu(queries, dev)
     total = (pitch * len(seqlens) if pitch else sum(int(x) for x in seqlens)) * p.n_kv_heads
     if weights is None:
         weights = torch.zeros(total, dtype=torch.float32, device=dev)
-    _need(weights, torch.float32, "weights")
+    _need_at(weights, _F32, at, "weights")
     if weights.numel() < total:
         raise ValueError(f"weights has {weights.numel()} values, {total} needed")
     if lse is not None:
-        _need(lse, torch.float32, "lse")
+        _need_at(lse, _F32, at, "lse")
         if lse.numel() < sum(queries) * p.n_q_heads:
             raise ValueError("lse is smaller than its queries")
-    ws = workspace
-    if ws is None:
+    if workspace is not None:
+        ws = _workspace_at(workspace, at)
+    else:
         ws = torch.empty(max(accumulate_workspace_bytes(p, seqlens, queries), 256), dtype=torch.uint8, device=dev)
     cp = p.c()
     _check(_lib.audiokv_accumulate(C.byref(cp), _ptr(q), _ptr(k), _ptr(lse), _ptr(cu), _host_lens(seqlens), _ptr(cu_q),
@@ -550,16 +559,15 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
                   out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """One decoding step of q.shape[0] sequences (q: bf16 [n_seqs, n_q_heads, head_dim]) on the compacted caches that they
     share (`k_prompt` None: on none) and the rows that they own; bf16 output of q's shape. Updates `slots` in place."""
-    _need(q, _BF16, "q")
-    _here("q k_new v_new pos_new out workspace", q, k_new, v_new, pos_new, out, workspace)
+    at = _device()
+    _need_at(q, _BF16, at, "q")
     dev, n_seqs = q.device, q.shape[0]
     if q.numel() != n_seqs * p.n_q_heads * p.head_dim:
         raise ValueError("q must be [n_seqs, n_q_heads, head_dim]")
     n_items = 0
     if k_prompt is not None:
-        _need(k_prompt, _BF16, "k_prompt"); _need(v_prompt, _BF16, "v_prompt")
-        _need(cu_budgets, _I32, "cu_budgets"); _need(cu_seqs, _I32, "cu_seqs")
-        _here("k_prompt v_prompt cu_budgets cu_seqs", k_prompt, v_prompt, cu_budgets, cu_seqs)
+        _need_at(k_prompt, _BF16, at, "k_prompt"); _need_at(v_prompt, _BF16, at, "v_prompt")
+        _need_at(cu_budgets, _I32, at, "cu_budgets"); _need_at(cu_seqs, _I32, at, "cu_seqs")
         n_items = cu_seqs.numel() - 1
         if n_items < 1:                       # (the library's call without items lets every sequence take part)
             raise ValueError("cu_seqs must have an entry per item and one more; without prompts, k_prompt is None")
@@ -569,21 +577,22 @@ def decode_shared(p: Params, q: torch.Tensor, k_prompt: Optional[torch.Tensor], 
             raise ValueError(f"k_prompt or v_prompt holds fewer than {total_rows} rows")
     if k_new is not None:
         rows = n_seqs * p.n_kv_heads * p.head_dim
-        if _need(k_new, _BF16, "k_new").numel() < rows or v_new is None or _need(v_new, _BF16, "v_new").numel() < rows:
+        if _need_at(k_new, _BF16, at, "k_new").numel() < rows or v_new is None or _need_at(v_new, _BF16, at, "v_new").numel() < rows:
             raise ValueError("k_new and v_new must be [n_seqs, n_kv_heads, head_dim]")
     elif v_new is not None:
         raise ValueError("k_new and v_new come together")
-    if pos_new is not None and _need(pos_new, _I32, "pos_new").numel() < n_seqs:
+    if pos_new is not None and _need_at(pos_new, _I32, at, "pos_new").numel() < n_seqs:
         raise ValueError("pos_new must have a value per sequence")
     if out is None:
         out = torch.empty(q.shape, dtype=torch.bfloat16, device=dev)
-    elif _need(out, _BF16, "out").numel() < q.numel():
+    elif _need_at(out, _BF16, at, "out").numel() < q.numel():
         raise ValueError("out is smaller than q")
-    ws = workspace
-    if ws is None:
+    if workspace is not None:
+        ws = _workspace_at(workspace, at)
+    else:
         ws = torch.empty(max(decode_shared_workspace_bytes(p, n_items, total_rows, n_seqs, max_seqs, max_own if slots else 0), 256),
                          dtype=torch.uint8, device=dev)
-    cs = C.byref(slots._c(p, n_seqs)) if slots is not None else None
+    cs = C.byref(slots._c(p, n_seqs, at)) if slots is not None else None
     prompts = (k_prompt.data_ptr(), v_prompt.data_ptr(), cu_budgets.data_ptr()) if n_items > 0 else (None, None, None)
     _check(_lib.audiokv_decode_shared(C.byref(p.c()), q.data_ptr(), *prompts, n_items, int(total_rows),
                                       cu_seqs.data_ptr() if n_items > 0 else None, n_seqs, int(max_seqs), cs, int(max_own),
@@ -602,15 +611,17 @@ def evict_accumulated(p: Params, slots: Slots, n_seqs: int, budget: int, recent:
                       budgets: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """Cuts the rows of every head of `slots` to its budget (`budget`, or the larger of it and budgets[head]) in place, by
     recency and accumulated weight."""
-    _here("budgets workspace", budgets, workspace)
-    if budgets is not None and _need(budgets, torch.int32, "budgets").numel() < n_seqs * p.n_kv_heads:
+    at = _device()
+    if budgets is not None and _need_at(budgets, _I32, at, "budgets").numel() < n_seqs * p.n_kv_heads:
         raise ValueError(f"budgets has {budgets.numel()} values, {n_seqs * p.n_kv_heads} needed")
-    ws = workspace
-    if ws is None:
+    cs = slots._c(p, n_seqs, at)
+    if workspace is not None:
+        ws = _workspace_at(workspace, at)
+    else:
         ws = torch.empty(max(evict_accumulated_workspace_bytes(p, n_seqs, max_own, budget), 256), dtype=torch.uint8,
                          device=slots.lengths.device)
-    _check(_lib.audiokv_evict_accumulated(C.byref(p.c()), C.byref(slots._c(p, n_seqs)), int(n_seqs), int(budget), _ptr(budgets), int(recent), int(max_own),
-                                          _ptr(ws), ws.numel(), _stream()))
+    _check(_lib.audiokv_evict_accumulated(C.byref(p.c()), C.byref(cs), int(n_seqs), int(budget), _ptr(budgets), int(recent),
+                                          int(max_own), _ptr(ws), ws.numel(), _stream()))
 
 
 PROFILE_STAGES = ("allocate", "score_sweep1", "score_sweep2", "pool_smooth", "select", "compact")
