@@ -128,3 +128,24 @@ def test_nan_of_a_query_reaches_only_what_it_sees(A, H_q, H_kv, d, given):
         clean = c.run(A, lse=c.lse() if given else None)
         assert torch.equal(w[0, 0, seen:], clean[0, 0, seen:]) and torch.equal(w[0, 1:], clean[0, 1:]) and torch.equal(w[1:], clean[1:])
         c.q[0][0, at] = q
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_few_queries_on_a_long_prompt(A, given):
+    """One block of rows, or many of keys, cut between all workgroups: 256 parts of a row's statistics."""
+    c = Call(77, 7, 1, 128, [(131072, 3), (90000, 120)])
+    lens, queries = [131072, 90000], [3, 120]
+    k = c.k.clone()
+    k[1, :, 90000:] = float("nan")
+    p = A.Params(7, 1, 128, 0, kv_stride_item=c.T * 128, kv_stride_head=c.T * 128, kv_stride_tok=128)
+    w = A.accumulate(p, torch.cat([q.reshape(-1) for q in c.q]), k.view(-1), lens, queries, pitch=c.T, lse=c.lse() if given else None)
+    c.check(w.view(2, 1, c.T))
+
+
+@pytest.mark.parametrize("H_q,H_kv,d,L,Q", [(64, 1, 64, 300, 300), (100, 1, 128, 200, 170), (96, 2, 256, 500, 3)])
+def test_many_query_heads_a_head(A, H_q, H_kv, d, L, Q):
+    """More of them than a load's rows, and than a tile's."""
+    c = Call(H_q, H_q, H_kv, d, [(L, Q), (40, 40)])
+    p = A.Params(H_q, H_kv, d, 0, kv_stride_item=H_kv * c.T * d, kv_stride_head=c.T * d, kv_stride_tok=d)
+    w = A.accumulate(p, torch.cat([q.reshape(-1) for q in c.q]), c.k.view(-1), [L, 40], [Q, 40], pitch=c.T)
+    c.check(w.view(2, H_kv, c.T))

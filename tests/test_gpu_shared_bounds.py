@@ -28,6 +28,49 @@ def test_ragged_items_and_a_loose_bound(A, H_q, H_kv, d, bound):
     s.check(t)
 
 
+def test_a_captured_step_refilled_by_its_tables(A):
+    """A graph of eleven sequences on four items, replayed with other numbers of sequences per item, and of rows per head, than it was
+    captured with: results as of a call with those numbers."""
+    rng = np.random.default_rng(31)
+    p, n, capacity = A.Params(8, 2, 128, 0), 11, 70
+    draw = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).bfloat16().cuda()
+    q, kp, vp, k_new, v_new = draw(n, 8, 128), draw(3000, 128), draw(3000, 128), draw(n, 2, 128), draw(n, 2, 128)
+    ko, vo = draw(n, 2, capacity, 128), draw(n, 2, capacity, 128)
+    cu_s, cu_b, pos = (torch.zeros(m, dtype=torch.int32, device="cuda") for m in (5, 9, n))
+    length = torch.tensor(rng.integers(0, 65, n * 2), dtype=torch.int32, device="cuda")
+    state = [x.clone() for x in (ko, vo, length, torch.zeros(n * 2, capacity, device="cuda"), torch.full((n * 2, capacity), -1, dtype=torch.int32, device="cuda"))]
+    slots = A.Slots(state[0], state[1], state[2], capacity, state[3], state[4])
+    out = torch.empty_like(q)
+    ws = torch.empty(A.decode_shared_workspace_bytes(p, 4, 3000, n, n, capacity), dtype=torch.uint8, device="cuda")
+
+    def reset():
+        for x, y in zip(state, (ko, vo, length)):
+            x.copy_(y)
+        state[3].zero_(); state[4].fill_(-1); out.fill_(7); ws.fill_(255)
+
+    def call():
+        A.decode_shared(p, q, kp, vp, cu_b, 3000, cu_s, n, slots=slots, max_own=capacity, k_new=k_new, v_new=v_new, pos_new=pos, out=out, workspace=ws)
+    reset(); call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for sequences, budgets in (([2, 3, 1, 5], [100, 7, 0, 900, 300, 20, 1, 1000]), ([11, 0, 0, 0], [1500, 1500, 0, 0, 0, 0, 0, 0]),
+                               ([0, 0, 1, 1], [1, 2, 3, 4, 500, 600, 700, 800]), ([0, 0, 0, 0], [375] * 8)):
+        cu_s.copy_(torch.tensor(np.concatenate([[0], np.cumsum(sequences)]), dtype=torch.int32))
+        cu_b.copy_(torch.tensor(np.concatenate([[0], np.cumsum(budgets)]), dtype=torch.int32))
+        results = []
+        for step in (call, graph.replay, graph.replay):
+            reset(); step()
+            torch.cuda.synchronize()
+            results.append([x.clone() for x in (out, *state)])
+        for got in results[1:]:
+            assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(got, results[0])), sequences
+        active = sum(sequences)
+        assert (out[active:] == 7).all() and torch.equal(state[2][2 * active:], length[2 * active:]) and (out[:active] != 7).any(2).all()
+        assert torch.equal(state[2][:2 * active], length[:2 * active] + 1)
+
+
 @pytest.mark.parametrize("stride_head,stride_tok", [((1 << 31) + 4096, 64), (64, 1 << 25)])
 def test_eviction_moves_rows_beyond_32_bits(A, stride_head, stride_tok):
     """Rows further than 2^31 elements from the first, moved and left where they are: every slot against the oracle."""
