@@ -402,8 +402,8 @@ typedef struct audiokv_slots {
  * Sequences from cu_seqs[n_items] on, and those of an item beyond max_seqs, take
  * no part: their outputs, lengths and rows stay as they are, so that a batch of
  * fixed size can be captured into a graph and filled by cu_seqs.
- * Softmax statistics, weights and sums are fp32; each weight is rounded to bf16
- * for its product with V, and out is bf16. n_q_heads / n_kv_heads <= 32.
+ * Softmax statistics, weights and sums are fp32; for its product with V a weight is
+ * taken to 2^-15 of it, and out is bf16. n_q_heads / n_kv_heads <= 32.
  * The workspace never shrinks as total_rows or max_own grow. */
 int32_t audiokv_decode_shared_workspace_bytes(const audiokv_params* params, int32_t n_items, int64_t total_rows,
                                               int32_t n_seqs, int32_t max_seqs, int32_t max_own, size_t* out_bytes);

@@ -7,9 +7,11 @@
 // The queries of an item's sequences that read one KV head, S * G of them, are the rows of a product with the prompt's keys; a
 // sequence's own rows meet its G queries only. Both are the same work for a workgroup of four waves: up to 128 query rows
 // against a chunk of rows of K and V. C = K Q^T on v_mfma_f32_32x32x16_bf16 leaves a lane with one query row (mfma_tile.h):
-// exponentials and their sum stay in the lane, and four keys at a time its weights, rounded to bf16, are already the operand
-// of O^T = V^T P^T, whose other operand the transposing LDS read fetches from V as it lies. Weights are rounded to bf16 (half a
-// step is 2^-8 of each at most) because V and the result are bf16; the sums that divide them are of the unrounded fp32 values.
+// exponentials and their sum stay in the lane, and four keys at a time its weights, as bf16, are already the operand of
+// O^T = V^T P^T, whose other operand the transposing LDS read fetches from V as it lies. A weight is the sum of two bf16 values, good
+// to 2^-15, and the product with V is taken twice: rounded to one, weights add as much error as the bf16 output's own rounding
+// (against 64 bits 1.7e-3 -> 1.9e-3 to 2.5e-3 of the output). The second product costs 32 sequences on 13107 rows a head 29.2 -> 32.3 us
+// a pass, 24 on eight prompts at d = 256 36.6 -> 38.0, and nothing where HBM or latency bounds. The sums that divide are of fp32 weights.
 // 32 query rows a wave. Up to 64 rows the tile's keys are split over two (groups of) waves, joined at the end through LDS.
 // A row's exponentials are taken against a reference, the maximum of the first tile: where a later sum leaves the safe range,
 // accumulators and sum are rescaled (see score_impl.h; here the two halves of a wave share their row's reference, since the
@@ -116,6 +118,12 @@ struct Rows {
     __bf16 *k_dst, *v_dst;
     float* logits;             // of the chunk's first row and the group's first query, or nullptr
 };
+
+// The upper part of a weight: itself with the lower half of its bits cleared, a bf16 value, and below the weight also where that half
+// is clear (unless the weight is zero). The rest is then above zero: times an infinity both parts have its sign.
+__device__ __forceinline__ float upper_part(float x) {
+    return __uint_as_float(__builtin_elementwise_sub_sat(__float_as_uint(x), 1u) & 0xffff0000u);
+}
 
 template <int D>
 __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int first_seq, int h, int r_first, int r_end, float* part, float2* stats)
@@ -277,12 +285,21 @@ __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int fi
             l += sum;
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                bf16x8 pf;
+                bf16x8 low;
+                u32x4 pairs;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) pf[e] = (__bf16)p[kb * 8 + e];
+                for (int e = 0; e < 8; e += 2) {
+                    const float p0 = p[kb * 8 + e], p1 = p[kb * 8 + e + 1], top0 = upper_part(p0), top1 = upper_part(p1);
+                    pairs[e / 2] = __builtin_amdgcn_perm(__float_as_uint(top1), __float_as_uint(top0), 0x07060302);
+                    low[e] = (__bf16)(p0 - top0);
+                    low[e + 1] = (__bf16)(p1 - top1);
+                }
+                const bf16x8 high = __builtin_bit_cast(bf16x8, pairs);
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) acc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ct], low, acc[ct], 0, 0, 0);
 #pragma unroll
                 for (int ct = 0; ct < CT; ++ct) {
-                    acc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ct], pf, acc[ct], 0, 0, 0);
+                    acc[ct] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[ct], high, acc[ct], 0, 0, 0);
                     if (kb == 0) vf[ct] = values(vt, 16, ct);
                     __builtin_amdgcn_sched_barrier(0);
                 }
