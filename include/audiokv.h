@@ -398,7 +398,10 @@ typedef struct audiokv_slots {
  *             what the group's queries gave it.
  * max_own (host): no head has more own rows than this after the step, at most
  * slots->capacity and below 2^30. Rows beyond it are not read, and a head that has
- * max_own rows before the step appends none. max_seqs (host): no item has more sequences.
+ * max_own rows before the step appends none. max_seqs (host): no item has more
+ * sequences. The prompts are cut into fewer and longer chunks the more it is, and
+ * the workspace has room for it in every chunk but a head's first: a bound far
+ * above what items have costs time and memory, not exactness.
  * Sequences from cu_seqs[n_items] on, and those of an item beyond max_seqs, take
  * no part: their outputs, lengths and rows stay as they are, so that a batch of
  * fixed size can be captured into a graph and filled by cu_seqs.
@@ -421,10 +424,13 @@ int32_t audiokv_decode_shared(const audiokv_params* params, const void* q_dev,
  * order, until the budget is full:
  *   1. rows at positions > newest - recent, newest being the head's largest;
  *   2. rows by slots->weights, the largest first, NaN last (-0 equals +0);
- * equal ones by slot, the lower first. Kept rows stay where they are, but those in
- * slots from the budget on move, in order, into the lower slots that became free:
- * K, V, weight and position; the length becomes the budget. Slots from the budget
- * on keep their contents. The next audiokv_decode_shared appends behind.
+ * equal ones by slot, the lower first: where `recent` is more than the budget, the
+ * rows that stay are the recent ones of the lowest slots, which need not be the
+ * newest. Keep `recent` within the budget for a window of the newest.
+ * Kept rows stay where they are, but those in slots from the budget on move, in
+ * order, into the lower slots that became free: K, V, weight and position; the
+ * length becomes the budget. Slots from the budget on keep their contents. The
+ * next audiokv_decode_shared appends behind.
  * The budget of head (x, h) is `budget`, or the larger of it and
  * budgets_dev[x * n_kv_heads + h] where budgets_dev (int32, device) is not NULL.
  * recent >= 0; slots->weights is needed, slots->positions where recent > 0.

@@ -610,7 +610,7 @@ def evict_accumulated_workspace_bytes(p: Params, n_seqs: int, max_own: int, budg
 def evict_accumulated(p: Params, slots: Slots, n_seqs: int, budget: int, recent: int, max_own: int, *,
                       budgets: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
     """Cuts the rows of every head of `slots` to its budget (`budget`, or the larger of it and budgets[head]) in place, by
-    recency and accumulated weight."""
+    recency and accumulated weight. (More recent rows than the budget: those of the lowest slots stay, not the newest.)"""
     at = _device()
     if budgets is not None and _need_at(budgets, _I32, at, "budgets").numel() < n_seqs * p.n_kv_heads:
         raise ValueError(f"budgets has {budgets.numel()} values, {n_seqs * p.n_kv_heads} needed")
