@@ -319,8 +319,8 @@ __device__ __forceinline__ void attend(const Shared& a, const Rows& rows, int fi
     auto group = [&](int ct, int i) { return col * kGroups + ((ct * 8 + i / 2 + hf) ^ (col & 15)); };
     l += __shfl_xor(l, 32, 64);
     // At d = 128 both waves' shares go there and all threads join and store them: one wave took 5000 cycles for it, a third of a short
-    // workgroup's time (48 caches of up to 4096 rows 39.5 -> 36.4 us). At d = 64 this takes 182 registers instead of 150 (1024
-    // sequences with few rows 34 -> 44 us).
+    // workgroup's time (48 caches of up to 4096 rows 39.5 -> 36.4 us). Not at d = 64: 1024 sequences
+    // with few rows 24.5 -> 23.8 us, but 48 caches of up to 4096 31.6 -> 33.1.
     if constexpr (D == 128) {
         if (halves) {                                         // uniform
             if (works) {
@@ -613,14 +613,14 @@ inline size_t up(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 }  // namespace
 
 // Workgroups that a call's prompts, and own rows, are cut for at least, where they are long enough. A prompt's chunk costs a result per
-// query, 512 bytes written and read at d = 128: few, long ones (32 sequences on 13107 rows, 4 heads: chunks of 128, 256 and 512 rows
-// 32 + 13, 24 + 10 and 23 + 8 us). At d = 128, from three blocks of query rows on, the products are most of it and two workgroups
-// share a CU: 64 sequences on the same rows 35 + 7 us with one, 30 + 9 with two; 512 on eight prompts 87 + 20 and 79 + 21 (at d = 64
-// 35 + 14 and 36 + 15, at d = 256 79 + 10 and 86 + 14: not there). Own rows: 48 caches of up to 4096 rows, 4 heads, 1024 workgroups 43 us, 2048 39.
+// query, 512 bytes written and read at d = 128: few, long ones. Both kernels, us: 32 sequences on 13107 rows, 4 heads, 42 with 96
+// workgroups, 30.3 with 192. At d = 128, from three blocks of query rows on, the products are most of it and two workgroups share a CU:
+// 64 sequences on the same rows 43.9 with 192, 39.4 with 384, 47.9 with 768; 512 on eight prompts 82 and 85 (at d = 64 55 and 56,
+// at d = 256 56 and 65: not there). Own rows: 48 caches of up to 4096 rows, 4 heads, 1024 workgroups 53.6, 2048 50.5.
 constexpr int kPromptBlocks = 192, kOwnBlocks = 2048;
-// What one wave joins per query: four channels to a lane, 256 floats at a time. Both kernels' weights included: 48 caches of 11 chunks
-// at d = 128 8.8 us by a wave and 10.5 by a workgroup per query, 64 sequences on 9 chunks of eight prompts 19 and 42; at d = 256
-// with 18 chunks 7.0 and 6.2.
+// What one wave joins per query: four channels to a lane, 256 floats at a time. Both kernels: 48 caches of 11 chunks at d = 128 50.5 us
+// by a wave and 51.2 by a workgroup per query, 512 sequences on 9 chunks of eight prompts 85 and 101; at d = 256 32 sequences on 13107
+// rows with caches of up to 4096 67.9 and 59.5.
 constexpr int kWaveFloats = 4096;
 
 // How a call is cut. Pure function of its sizes, so that the workspace query and the launch agree. The workspace never shrinks as
