@@ -657,9 +657,12 @@ hipError_t launch_accumulate(const Geom& g, const AccumPlan& p, const void* q, c
     a.cu_seq = cu_seqlens;
     a.cu_q = cu_queries;
     a.lse = lse;
-    a.norms = reinterpret_cast<float*>(ws);
-    a.stats = reinterpret_cast<float2*>(ws + up((size_t)p.rows_total * sizeof(float)));
-    a.parts = reinterpret_cast<float*>(ws + (lse ? 0 : accumulate_stats_bytes(p)));
+    if (!lse) {                                // (otherwise there may be no workspace at all)
+        a.norms = reinterpret_cast<float*>(ws);
+        a.stats = reinterpret_cast<float2*>(ws + up((size_t)p.rows_total * sizeof(float)));
+        ws += accumulate_stats_bytes(p);
+    }
+    a.parts = reinterpret_cast<float*>(ws);
     a.weights = weights;
     a.pitch = pitch;
     a.div_g = g.G > 1 ? (unsigned)((0x100000000ULL + g.G - 1) / g.G) : 0;

@@ -28,6 +28,7 @@ def A(monkeypatch):
     library = Library()
     monkeypatch.setattr(A.binding, "_lib", library)
     monkeypatch.setattr(A.binding, "_raw_device", lambda: 0)
+    monkeypatch.setattr(A.binding, "_SIZE_CACHE", {})         # (sizes that this library answers are not the real one's)
     monkeypatch.setattr(A.binding, "_stream", lambda: 0)
     A.reached = library.reached
     with FakeTensorMode(), warnings.catch_warnings():

@@ -149,3 +149,16 @@ def test_many_query_heads_a_head(A, H_q, H_kv, d, L, Q):
     p = A.Params(H_q, H_kv, d, 0, kv_stride_item=H_kv * c.T * d, kv_stride_head=c.T * d, kv_stride_tok=d)
     w = A.accumulate(p, torch.cat([q.reshape(-1) for q in c.q]), c.k.view(-1), [L, 40], [Q, 40], pitch=c.T)
     c.check(w.view(2, H_kv, c.T))
+
+
+def test_given_lse_needs_no_workspace_where_no_block_is_shared(A):
+    """No queries but of one item, one block of keys, one workgroup: the library takes a workspace of no bytes, and of no address."""
+    import ctypes as C
+    c = Call(5, 4, 2, 64, [(60, 8)])
+    p = A.Params(4, 2, 64, 0, kv_stride_item=2 * c.T * 64, kv_stride_head=c.T * 64, kv_stride_tok=64)
+    cu, cu_q = (torch.tensor([0, n], dtype=torch.int32, device="cuda") for n in (60, 8))
+    w, lse, one = torch.zeros(2 * c.T, device="cuda"), c.lse(), lambda n: (C.c_int32 * 1)(n)
+    rc = A.binding._lib.audiokv_accumulate(C.byref(p.c()), c.q[0].data_ptr(), c.k.data_ptr(), lse.data_ptr(), cu.data_ptr(), one(60), cu_q.data_ptr(),
+                                           one(8), 1, w.data_ptr(), c.T, None, 0, torch.cuda.current_stream().cuda_stream)
+    assert rc == 0, A.binding._lib.audiokv_last_error()
+    c.check(w.view(1, 2, c.T))

@@ -61,3 +61,18 @@ def test_infinite_values_that_have_weight(A, d):
         assert (out[:, :2, 3] == np.inf).all() and (out[:, 2:, 9] == -np.inf).all() and (out[1, :2, d - 1] == np.inf).all()
         out[:, :2, 3] = out[:, 2:, 9] = out[1, :2, d - 1] = 0
         assert np.isfinite(out).all()
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+def test_nan_stays_where_it_is(A, d):
+    """A query of NaN gives NaN, and NaN weights to the rows that its group owns; a value of NaN makes its channel that. Nothing else is."""
+    s = Step(np.random.default_rng(d), 6, 2, d, [40, 64], [3], [[23, 5]] * 3, 24)
+    s.q[1, 4], s.vp[70, 11] = np.nan, np.nan                  # query head 4 of sequence 1, in the group of KV head 1; a row of head 1
+    t = s.tensors(A)
+    s.call(A, t)
+    torch.cuda.synchronize()
+    out, w = f64(t["out"]), t["slots"].weights.cpu().numpy()
+    assert np.isnan(out[1, 4]).all() and np.isnan(out[:, 3:, 11]).all() and np.isnan(w[1, 1, :6]).all()
+    out[1, 4] = out[:, 3:, 11] = 0
+    w[1, 1, :6] = 0
+    assert np.isfinite(out).all() and np.isfinite(w).all()
