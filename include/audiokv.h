@@ -12,6 +12,8 @@
  * (step 1 with all queries instead of a window), audiokv_decode_attend and
  * audiokv_decode_shared (decoding steps on the packed cache, the latter with rows
  * that the sequences add) and audiokv_evict_accumulated (those kept at a budget).
+ * And a cache in 4 bits and in pages of a pool: audiokv_pages_append (instead of
+ * step 5, and for new rows), _attend, _fork, _keep and _read.
  *
  * Conventions common to every entry point
  * ---------------------------------------
@@ -107,7 +109,7 @@ typedef struct audiokv_params {
      * moved as 16-byte vectors), kv_stride_tok >= head_dim, and kv_stride_item > 0 when n_items > 1. Rows of
      * different (item, head, token) must not overlap. This is how a padded prefill cache [B][H_kv][L_max][d]
      * (kv_stride_item = H_kv*L_max*d, kv_stride_head = L_max*d, kv_stride_tok = d) or a slice of a larger
-     * buffer is passed without a copy. Used by score, compact, evict (and their variants), accumulate, and for the
+     * buffer is passed without a copy. Used by score, compact, evict (and their variants), accumulate, pages_append, and for the
      * rows in audiokv_slots (a sequence is the item there); q_win, the outputs
      * and the compacted cache read by decode_attend are always packed. */
     int64_t  kv_stride_item;
@@ -441,6 +443,125 @@ int32_t audiokv_evict_accumulated_workspace_bytes(const audiokv_params* params, 
 int32_t audiokv_evict_accumulated(const audiokv_params* params, const audiokv_slots* slots, int32_t n_seqs,
                                   int32_t budget, const int32_t* budgets_dev, int32_t recent, int32_t max_own,
                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* A cache in 4 bits and in pages: the compacted cache (paper Sec. 1 and Sec. 4.6: its
+ * size is what eviction is for) at 17/64 of bf16's bytes, for heads whose budgets
+ * differ (Sec. 3.1) and grow, and for sequences that share rows.
+ *
+ * What is held. A row's channels are blocks of 32. A block stands for code * 2^(e - 127):
+ * one byte e, and 32 codes of four bits, a sign and one of the magnitudes 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 (codes 0 to 7; 8 to 15 with the sign). e is the smallest number with
+ * max|x| <= 7 * 2^(e - 127), within 2 and 252 (2 for zeros only). A value x / 2^(e - 127)
+ * goes to the nearest magnitude, in the middle between two to the even code, beyond 6 to
+ * 6. A block with an infinity or NaN has e = 255 and codes 0; e = 255 stands for NaN.
+ *
+ * Where. A page holds `page_rows` rows P of one KV head: K's codes [P][head_dim / 2], the
+ * even channel in the low half of a byte, V's codes, K's e [P][head_dim / 32], V's e;
+ * audiokv_page_bytes bytes. Head (x, h), x a sequence and h a KV head, has row r in page
+ * table[x * n_kv_heads + h][r / P] at r % P, for r < lengths[x * n_kv_heads + h]; entries
+ * behind that have no meaning. refs[p] says how many heads have page p in their tables;
+ * state[0] how many pages have none, and are free; state[1] where the search for free
+ * pages begins. Pages are taken in ascending order from there, after the last one from
+ * the first again, and state[1] becomes the one behind the last that was taken.
+ * lengths, refs and state[1] zero and state[0] = n_pages is an empty cache. All pointers
+ * are device memory. The calls below keep the numbers in step; none of them looks
+ * for numbers that are not (a page number outside the pool is never followed, a length
+ * beyond a table row is cut). "Sequences" may be (sequence, layer) pairs.
+ * Calls that change a cache (append, fork, keep) must be ordered after each other and
+ * after and before others on it, by a stream or events. n_seqs * n_kv_heads <= 2^20,
+ * and n_seqs * n_kv_heads * max_pages * page_rows / 32 < 2^31. */
+typedef struct audiokv_pages {
+    uint32_t size;           /* sizeof(audiokv_pages)                                  */
+    int32_t  page_rows;      /* P: 32, 64, 128 or 256                                  */
+    int32_t  n_pages;        /* pages of the pool, >= 1                                */
+    int32_t  max_pages;      /* entries of a head's table row, >= 1                    */
+    void    *pool;           /* [n_pages][audiokv_page_bytes], 16-byte aligned         */
+    int32_t *table;          /* [n_seqs * n_kv_heads][max_pages]                       */
+    int32_t *lengths;        /* [n_seqs * n_kv_heads]                                  */
+    int32_t *refs;           /* [n_pages]                                              */
+    int32_t *state;          /* [2]                                                    */
+} audiokv_pages;
+
+/* Host-only: bytes of a page, page_rows * head_dim * 17 / 16. */
+int32_t audiokv_page_bytes(const audiokv_params* params, int32_t page_rows, size_t* out_bytes);
+
+/* Rounds rows of K and V to 4 bits and puts them behind the rows that their heads have.
+ * k, v, cu_seqlens_dev, seqlens_host, n_items: as for audiokv_compact (the kv_layout or
+ * the strides of params; lengths L_i >= 1). Head h of item i gets rows indices[cu_budgets[g]
+ * + t] of it, g = i * n_kv_heads + h, as audiokv_select / _evict write them; indices and
+ * cu_budgets NULL: all L_i rows (a step's new row per sequence: n_items of length 1).
+ * total_rows (host): the sum of the budgets, or of L_i * n_kv_heads; without indices the
+ * call computes it and the argument is not used.
+ * seqs_dev: the sequence of every item (int32 [n_items]), or NULL: item i is sequence i,
+ * n_items <= n_seqs. An item takes no part where that is outside [0, n_seqs), or a
+ * sequence that an item before it has named: a batch of fixed size can be captured into
+ * a graph and filled by seqs.
+ * A head needs a page for every P rows that it begins, in the order of the items and
+ * their heads; one more where its last page is begun and refs says that others have
+ * it as well, too: its rows are copied first, and the others keep the page. (Two heads
+ * that share such a page and grow in one call both get copies, and the page is free for
+ * calls after this one.) Items are served while the free pages last: an item that needs
+ * pages, with which the needed ones of it and all before it (served or not, but for those
+ * that max_pages refuses) are more than there are free, gets no rows, and neither does
+ * one of which a head would need more than max_pages. Their heads stay as they are;
+ * refused_dev (int32, or NULL) becomes the number of heads that should have got rows so
+ * and did not. */
+int32_t audiokv_pages_append_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,
+                                             int32_t n_items, int64_t total_rows, size_t* out_bytes);
+int32_t audiokv_pages_append(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,
+                             const void* k, const void* v, const int32_t* indices_dev, const int32_t* cu_budgets_dev,
+                             int64_t total_rows, const int32_t* cu_seqlens_dev, const int32_t* seqlens_host, int32_t n_items,
+                             const int32_t* seqs_dev, int32_t* refused_dev,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* One decoding step of all sequences on the cache:
+ *   out[x][q] = sum over the rows r of q's KV head of softmax_r(scale * <q, K_r>) * V_r,
+ * K_r and V_r the values that the cache holds. q_dev, out_dev: bf16 [n_seqs][n_q_heads]
+ * [head_dim]. lse_dev: NULL, or fp32 [n_seqs][n_q_heads], the natural logarithm of the
+ * softmax's denominator (two parts of a cache are joined by it). A query without rows,
+ * or whose logits are all -infinity, gives zeros and -infinity. Products, statistics and
+ * sums are fp32; for its product with V a weight is taken to 2^-16 of it, and out is
+ * bf16. n_q_heads / n_kv_heads <= 16. The pages may be read by several calls at once. */
+int32_t audiokv_pages_attend_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,
+                                             size_t* out_bytes);
+int32_t audiokv_pages_attend(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, const void* q_dev,
+                             void* out_dev, float* lse_dev, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Sequence x becomes what sequence parents[x] was before the call, without its last
+ * drop[x] rows in every head: a beam that goes on from another, a sample of a prompt, a
+ * sequence whose rejected rows go, or one that ends (parents[x] outside [0, n_seqs): no
+ * rows). parents_dev, drop_dev: int32 [n_seqs] or NULL (itself; 0; drop < 0 is 0). No row
+ * is copied: pages are shared, and what append does to a shared one it does to a copy. */
+int32_t audiokv_pages_fork_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,
+                                           size_t* out_bytes);
+int32_t audiokv_pages_fork(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,
+                           const int32_t* parents_dev, const int32_t* drop_dev,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Every head keeps the rows that are listed: head g keeps rows indices[cu_budgets[g] + t],
+ * ascending and none twice (an index outside its rows is cut to the nearest), which become
+ * rows t; a head that keeps as many rows as it has, or more, stays as it is, its indices
+ * unread. Rows move as they are held. cu_budgets_dev: int32 [n_seqs * n_kv_heads + 1];
+ * total_rows (host): the sum of the budgets.
+ * Whole pages of a head whose rows are all kept, from its first row on, stay; the others'
+ * kept rows go to new pages, taken in the order of the heads, and the old ones lose a
+ * head. Pages that become free so can be had from the next call on. Heads are
+ * served while the free pages last, as items are by audiokv_pages_append; the others
+ * stay as they are and are counted in refused_dev (int32, or NULL). */
+int32_t audiokv_pages_keep_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,
+                                           int64_t total_rows, size_t* out_bytes);
+int32_t audiokv_pages_keep(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,
+                           const int32_t* indices_dev, const int32_t* cu_budgets_dev, int64_t total_rows, int32_t* refused_dev,
+                           void* workspace, size_t workspace_bytes, void* stream);
+
+/* Rows of the cache as bf16, exactly what is held: rows first[g] .. of head g (first_dev
+ * NULL: from row 0) go to rows cu_rows[g] .. cu_rows[g+1] - 1 of k_out / v_out (bf16
+ * [total_rows][head_dim]), packed as audiokv_compact packs them: what decode_attend reads,
+ * and, where the heads of a sequence have as many rows each, K and V of a head-major
+ * batch for score or accumulate. Rows that a head does not have read as zeros.
+ * cu_rows_dev: int32 [n_seqs * n_kv_heads + 1], from 0; total_rows (host): its last. */
+int32_t audiokv_pages_read(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, const int32_t* first_dev,
+                           const int32_t* cu_rows_dev, int64_t total_rows, void* k_out, void* v_out, void* stream);
 
 /* Measurement aid, not part of the method (used by the benchmark to time the
  * kernels of audiokv_evict where they run). While enabled, audiokv_evict records

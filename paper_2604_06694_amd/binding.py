@@ -60,6 +60,20 @@ class _CSlots(C.Structure):
     ]
 
 
+class _CPages(C.Structure):
+    _fields_ = [
+        ("size", C.c_uint32),
+        ("page_rows", C.c_int32),
+        ("n_pages", C.c_int32),
+        ("max_pages", C.c_int32),
+        ("pool", C.c_void_p),
+        ("table", C.c_void_p),
+        ("lengths", C.c_void_p),
+        ("refs", C.c_void_p),
+        ("state", C.c_void_p),
+    ]
+
+
 @dataclass
 class Params:
     n_q_heads: int
@@ -127,6 +141,59 @@ class Slots:
         return _CSlots(_SLOTS_SIZE, self.capacity, k.data_ptr(), v.data_ptr(), lengths.data_ptr(), _ptr(w), _ptr(pos))
 
 
+_PAGES_SIZE = C.sizeof(_CPages)
+_U8 = torch.uint8
+
+
+@dataclass
+class Pages:
+    """A cache in 4 bits and in pages: device tensors, see audiokv_pages. `empty` makes one."""
+    pool: torch.Tensor                       # uint8, n_pages * page_bytes
+    table: torch.Tensor                      # int32 [n_seqs * n_kv_heads, max_pages]
+    lengths: torch.Tensor                    # int32 [n_seqs * n_kv_heads]
+    refs: torch.Tensor                       # int32 [n_pages]
+    state: torch.Tensor                      # int32 [2]: free pages, where the search for them begins
+    page_rows: int
+
+    @classmethod
+    def empty(cls, p: Params, n_seqs: int, n_pages: int, max_pages: int, page_rows: int = 64, device="cuda") -> "Pages":
+        """An empty cache of n_seqs sequences; a head can have max_pages pages."""
+        heads = n_seqs * p.n_kv_heads
+
+        def zeros(*shape):
+            return torch.zeros(shape, dtype=_I32, device=device)
+        state = zeros(2)
+        state[0] = n_pages
+        return cls(torch.empty(n_pages * page_bytes(p, page_rows), dtype=_U8, device=device), zeros(heads, max_pages), zeros(heads),
+                   zeros(n_pages), state, page_rows)
+
+    def n_seqs(self, p: Params) -> int:
+        return self.lengths.numel() // p.n_kv_heads
+
+    def _c(self, p: Params, at: int) -> _CPages:
+        """The C struct, after a look at types, sizes and the device."""
+        pool, table, lengths, refs, state = self.pool, self.table, self.lengths, self.refs, self.state
+        heads, n_pages = lengths.numel(), refs.numel()
+        if heads % p.n_kv_heads:
+            raise ValueError(f"pages.lengths has {heads} values, which is no number of sequences of {p.n_kv_heads} KV heads")
+        for t, name in ((table, "table"), (lengths, "lengths"), (refs, "refs"), (state, "state")):
+            if t.dtype is not _I32 or t.get_device() != at or not t.is_contiguous():
+                raise ValueError(f"pages.{name} must be a contiguous tensor of dtype {_I32} on the current device, {at}")
+        if table.dim() != 2 or table.shape[0] != heads:
+            raise ValueError(f"pages.table must be [{heads}, entries], one row per head in pages.lengths")
+        if state.numel() != 2:
+            raise ValueError("pages.state must have two values")
+        if pool.dtype is not _U8 or pool.get_device() != at or not pool.is_contiguous() or pool.numel() < n_pages * self.page_rows * p.head_dim * 17 // 16:
+            raise ValueError(f"pages.pool must be a contiguous tensor of {n_pages} pages, {n_pages * self.page_rows * p.head_dim * 17 // 16} values of "
+                             f"dtype {_U8}, on the current device, {at}")
+        return _CPages(_PAGES_SIZE, self.page_rows, n_pages, table.shape[1], pool.data_ptr(), table.data_ptr(), lengths.data_ptr(),
+                       refs.data_ptr(), state.data_ptr())
+
+    def _sizes(self) -> _CPages:
+        """The C struct of a size query, which looks at no pointer."""
+        return _CPages(_PAGES_SIZE, self.page_rows, self.refs.numel(), self.table.shape[1], None, None, None, None, None)
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -166,6 +233,17 @@ def _load() -> C.CDLL:
                                           C.c_size_t, vp]
     lib.audiokv_evict_accumulated_workspace_bytes.argtypes = [pp, i32, i32, i32, C.POINTER(C.c_size_t)]
     lib.audiokv_evict_accumulated.argtypes = [pp, C.POINTER(_CSlots), i32, i32, vp, i32, i32, vp, C.c_size_t, vp]
+    gp, sz = C.POINTER(_CPages), C.POINTER(C.c_size_t)
+    lib.audiokv_page_bytes.argtypes = [pp, i32, sz]
+    lib.audiokv_pages_append_workspace_bytes.argtypes = [pp, gp, i32, i32, i64, sz]
+    lib.audiokv_pages_append.argtypes = [pp, gp, i32, vp, vp, vp, vp, i64, vp, vp, i32, vp, vp, vp, C.c_size_t, vp]
+    lib.audiokv_pages_attend_workspace_bytes.argtypes = [pp, gp, i32, sz]
+    lib.audiokv_pages_attend.argtypes = [pp, gp, i32, vp, vp, vp, vp, C.c_size_t, vp]
+    lib.audiokv_pages_fork_workspace_bytes.argtypes = [pp, gp, i32, sz]
+    lib.audiokv_pages_fork.argtypes = [pp, gp, i32, vp, vp, vp, C.c_size_t, vp]
+    lib.audiokv_pages_keep_workspace_bytes.argtypes = [pp, gp, i32, i64, sz]
+    lib.audiokv_pages_keep.argtypes = [pp, gp, i32, vp, vp, i64, vp, vp, C.c_size_t, vp]
+    lib.audiokv_pages_read.argtypes = [pp, gp, i32, vp, vp, i64, vp, vp, vp]
     lib.audiokv_profile_enable.argtypes = [i32]
     lib.audiokv_profile_enable.restype = i32
     lib.audiokv_profile_read.argtypes = [C.POINTER(C.c_float)]
@@ -173,7 +251,9 @@ def _load() -> C.CDLL:
     for name in ("total_kept", "workspace_bytes", "score", "allocate", "smooth", "smooth_cutoffs", "select", "compact", "evict",
                  "decode_workspace_bytes", "decode_attend", "score_lse", "evict_lse", "evict_noalloc",
                  "accumulate_workspace_bytes", "accumulate", "decode_shared_workspace_bytes", "decode_shared",
-                 "evict_accumulated_workspace_bytes", "evict_accumulated"):
+                 "evict_accumulated_workspace_bytes", "evict_accumulated", "page_bytes", "pages_append_workspace_bytes", "pages_append",
+                 "pages_attend_workspace_bytes", "pages_attend", "pages_fork_workspace_bytes", "pages_fork",
+                 "pages_keep_workspace_bytes", "pages_keep", "pages_read"):
         getattr(lib, "audiokv_" + name).restype = i32
     return lib
 
@@ -622,6 +702,130 @@ def evict_accumulated(p: Params, slots: Slots, n_seqs: int, budget: int, recent:
                          device=slots.lengths.device)
     _check(_lib.audiokv_evict_accumulated(C.byref(p.c()), C.byref(cs), int(n_seqs), int(budget), _ptr(budgets), int(recent),
                                           int(max_own), _ptr(ws), ws.numel(), _stream()))
+
+
+def _size_of(name: str, p: Params, *args) -> int:
+    out = C.c_size_t(0)
+    _check(getattr(_lib, name)(C.byref(p.c()), *args, C.byref(out)))
+    return out.value
+
+
+def _workspace_of(workspace: Optional[torch.Tensor], at: int, needed) -> torch.Tensor:
+    if workspace is not None:
+        return _workspace_at(workspace, at)
+    return torch.empty(max(needed(), 256), dtype=_U8, device=torch.device("cuda", at))
+
+
+def _values(t: Optional[torch.Tensor], n: int, dtype, at: int, name: str) -> Optional[int]:
+    """The address of a tensor of n values or more, if given."""
+    if t is None:
+        return None
+    if _need_at(t, dtype, at, name).numel() < n:
+        raise ValueError(f"{name} has {t.numel()} values, {n} needed")
+    return t.data_ptr()
+
+
+def page_bytes(p: Params, page_rows: int) -> int:
+    return _size_of("audiokv_page_bytes", p, int(page_rows))
+
+
+def pages_append_workspace_bytes(p: Params, pages: Pages, n_items: int, total_rows: int) -> int:
+    return _size_of("audiokv_pages_append_workspace_bytes", p, C.byref(pages._sizes()), pages.n_seqs(p), int(n_items), int(total_rows))
+
+
+def pages_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, seqlens: Sequence[int], *,
+                 indices: Optional[torch.Tensor] = None, cu_budgets: Optional[torch.Tensor] = None, total_rows: int = 0,
+                 seqs: Optional[torch.Tensor] = None, cu_seqlens: Optional[torch.Tensor] = None,
+                 refused: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """Rows of K and V (all of every item's, or those that indices and cu_budgets name; then total_rows is the sum of the budgets)
+    behind the rows that the heads of their sequences have, in 4 bits. `seqs`: the sequence of every item, otherwise item i is
+    sequence i. `refused` (int32, one value) becomes the number of heads that there were no pages for."""
+    at = _device()
+    cg = pages._c(p, at)
+    n_seqs, n_items, heads = pages.n_seqs(p), len(seqlens), len(seqlens) * p.n_kv_heads
+    _need_at(k, _BF16, at, "k"); _need_at(v, _BF16, at, "v")
+    if min(_room(p, k), _room(p, v)) < _rows_end(p, seqlens):
+        raise ValueError(f"k or v has room for {min(_room(p, k), _room(p, v))} values, {_rows_end(p, seqlens)} needed")
+    _table(cu_seqlens, n_items, at, "cu_seqlens"); _table(cu_budgets, heads, at, "cu_budgets")
+    if indices is None:
+        total_rows = sum(int(x) for x in seqlens) * p.n_kv_heads
+    idx, to, no = (_values(indices, total_rows, _I32, at, "indices"), _values(seqs, n_items, _I32, at, "seqs"),
+                   _values(refused, 1, _I32, at, "refused"))
+    ws = _workspace_of(workspace, at, lambda: pages_append_workspace_bytes(p, pages, n_items, total_rows))
+    cu = cu_seqlens if cu_seqlens is not None else _cu(seqlens, k.device)
+    _check(_lib.audiokv_pages_append(C.byref(p.c()), C.byref(cg), n_seqs, k.data_ptr(), v.data_ptr(), idx, _ptr(cu_budgets),
+                                     int(total_rows), cu.data_ptr(), _host_lens(seqlens), n_items, to, no, ws.data_ptr(), ws.nbytes,
+                                     _stream()))
+
+
+def pages_attend_workspace_bytes(p: Params, pages: Pages) -> int:
+    return _size_of("audiokv_pages_attend_workspace_bytes", p, C.byref(pages._sizes()), pages.n_seqs(p))
+
+
+def pages_attend(p: Params, pages: Pages, q: torch.Tensor, *, out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                 workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One decoding step of all sequences (q: bf16 [n_seqs, n_q_heads, head_dim]); bf16 output of q's shape. `lse` (fp32 [n_seqs,
+    n_q_heads]) becomes the log-sum-exp of the logits."""
+    at = _device()
+    cg = pages._c(p, at)
+    n_seqs = pages.n_seqs(p)
+    _need_at(q, _BF16, at, "q")
+    if q.numel() != n_seqs * p.n_q_heads * p.head_dim:
+        raise ValueError(f"q must be [n_seqs = {n_seqs}, n_q_heads, head_dim]")
+    if out is None:
+        out = torch.empty(q.shape, dtype=_BF16, device=q.device)
+    to, ls = _values(out, q.numel(), _BF16, at, "out"), _values(lse, n_seqs * p.n_q_heads, _F32, at, "lse")
+    ws = _workspace_of(workspace, at, lambda: pages_attend_workspace_bytes(p, pages))
+    _check(_lib.audiokv_pages_attend(C.byref(p.c()), C.byref(cg), n_seqs, q.data_ptr(), to, ls, ws.data_ptr(), ws.nbytes, _stream()))
+    return out
+
+
+def pages_fork_workspace_bytes(p: Params, pages: Pages) -> int:
+    return _size_of("audiokv_pages_fork_workspace_bytes", p, C.byref(pages._sizes()), pages.n_seqs(p))
+
+
+def pages_fork(p: Params, pages: Pages, parents: Optional[torch.Tensor] = None, *, drop: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None) -> None:
+    """Sequence x becomes what sequence parents[x] (int32; -1: none) was, without its last drop[x] rows. Pages are shared."""
+    at = _device()
+    cg = pages._c(p, at)
+    n_seqs = pages.n_seqs(p)
+    pa, dr = _values(parents, n_seqs, _I32, at, "parents"), _values(drop, n_seqs, _I32, at, "drop")
+    ws = _workspace_of(workspace, at, lambda: pages_fork_workspace_bytes(p, pages))
+    _check(_lib.audiokv_pages_fork(C.byref(p.c()), C.byref(cg), n_seqs, pa, dr, ws.data_ptr(), ws.nbytes, _stream()))
+
+
+def pages_keep_workspace_bytes(p: Params, pages: Pages, total_rows: int) -> int:
+    return _size_of("audiokv_pages_keep_workspace_bytes", p, C.byref(pages._sizes()), pages.n_seqs(p), int(total_rows))
+
+
+def pages_keep(p: Params, pages: Pages, indices: Optional[torch.Tensor], cu_budgets: torch.Tensor, total_rows: int, *,
+               refused: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """Every head keeps its rows indices[cu_budgets[head] ..], ascending, moved together; a head that has no more rows than its
+    budget stays as it is."""
+    at = _device()
+    cg = pages._c(p, at)
+    n_seqs = pages.n_seqs(p)
+    idx, no = _values(indices, total_rows, _I32, at, "indices"), _values(refused, 1, _I32, at, "refused")
+    cu = _values(cu_budgets, n_seqs * p.n_kv_heads + 1, _I32, at, "cu_budgets")
+    ws = _workspace_of(workspace, at, lambda: pages_keep_workspace_bytes(p, pages, total_rows))
+    _check(_lib.audiokv_pages_keep(C.byref(p.c()), C.byref(cg), n_seqs, idx, cu, int(total_rows), no, ws.data_ptr(), ws.nbytes, _stream()))
+
+
+def pages_read(p: Params, pages: Pages, cu_rows: torch.Tensor, total_rows: int, *, first: Optional[torch.Tensor] = None,
+               k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rows first[head] (0) .. of every head, cu_rows[head + 1] - cu_rows[head] of them, as bf16 [total_rows, head_dim], K and V."""
+    at = _device()
+    cg = pages._c(p, at)
+    n_seqs, shape = pages.n_seqs(p), (int(total_rows), p.head_dim)
+    cu, fi = _values(cu_rows, n_seqs * p.n_kv_heads + 1, _I32, at, "cu_rows"), _values(first, n_seqs * p.n_kv_heads, _I32, at, "first")
+    if k_out is None:
+        k_out = torch.empty(shape, dtype=_BF16, device=cu_rows.device)
+    if v_out is None:
+        v_out = torch.empty(shape, dtype=_BF16, device=cu_rows.device)
+    ko, vo = _values(k_out, shape[0] * shape[1], _BF16, at, "k_out"), _values(v_out, shape[0] * shape[1], _BF16, at, "v_out")
+    _check(_lib.audiokv_pages_read(C.byref(p.c()), C.byref(cg), n_seqs, fi, cu, shape[0], ko, vo, _stream()))
+    return k_out, v_out
 
 
 PROFILE_STAGES = ("allocate", "score_sweep1", "score_sweep2", "pool_smooth", "select", "compact")

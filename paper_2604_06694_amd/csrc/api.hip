@@ -9,6 +9,7 @@
 #include "accumulate_plan.h"
 #include "common.h"
 #include "conv.h"
+#include "pages.h"
 #include "select_head.h"
 
 using namespace audiokv;
@@ -875,6 +876,230 @@ int32_t audiokv_evict_accumulated(const audiokv_params* params, const audiokv_sl
     c.budget = budget;
     c.recent = recent;
     AUDIOKV_HIP(launch_evict_accumulated(g, c, workspace, static_cast<hipStream_t>(stream)), "evict_accumulated kernels");
+    return AUDIOKV_OK;
+}
+
+// sizes of a cache in pages; its pointers where they are used
+static int32_t check_pages(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, bool pointers, PageView* pv)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (!pages) return fail(AUDIOKV_E_INVALID_ARG, "pages is NULL");
+    if (pages->size != sizeof(audiokv_pages))
+        return fail(AUDIOKV_E_INVALID_ARG, "pages.size = %u, this library expects %zu", pages->size, sizeof(audiokv_pages));
+    const int P = pages->page_rows;
+    if (P != 32 && P != 64 && P != 128 && P != 256) return fail(AUDIOKV_E_INVALID_ARG, "page_rows %d: 32, 64, 128 or 256", P);
+    if (pages->n_pages < 1 || pages->max_pages < 1 || n_seqs < 1)
+        return fail(AUDIOKV_E_INVALID_ARG, "n_pages %d, max_pages %d and n_seqs %d must be at least 1", pages->n_pages, pages->max_pages, n_seqs);
+    const long long heads = (long long)n_seqs * params->n_kv_heads;
+    // (entries of a table, and units of 32 rows over all heads, are counted in 32 bits; so are the rows of a head)
+    if (heads > (1 << 20) || heads * pages->max_pages > INT32_MAX / (P / 32) || (long long)pages->max_pages * P > INT32_MAX)
+        return fail(AUDIOKV_E_UNSUPPORTED, "%lld heads of %d pages of %d rows are too many for one call", heads, pages->max_pages, P);
+    if (pointers) {
+        if (!pages->pool || !pages->table || !pages->lengths || !pages->refs || !pages->state)
+            return fail(AUDIOKV_E_INVALID_ARG, "pages: pool, table, lengths, refs or state is NULL");
+        if (!aligned16(pages->pool)) return fail(AUDIOKV_E_INVALID_ARG, "pages: pool must be 16-byte aligned");
+    }
+    pv->pool = static_cast<char*>(pages->pool);
+    pv->table = pages->table;
+    pv->lengths = pages->lengths;
+    pv->refs = pages->refs;
+    pv->state = pages->state;
+    pv->n_pages = pages->n_pages;
+    pv->width = pages->max_pages;
+    pv->log_p = P == 32 ? 5 : P == 64 ? 6 : P == 128 ? 7 : 8;
+    pv->n_heads = (int)heads;
+    pv->H = params->n_kv_heads;
+    pv->D = params->head_dim;
+    return AUDIOKV_OK;
+}
+
+static int32_t check_workspace(const void* workspace, size_t has, size_t need)
+{
+    if (!workspace) return fail(AUDIOKV_E_INVALID_ARG, "workspace is NULL");
+    if (!aligned16(workspace)) return fail(AUDIOKV_E_INVALID_ARG, "the workspace must be 16-byte aligned");
+    if (has < need) return fail(AUDIOKV_E_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, %zu needed", has, need);
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_page_bytes(const audiokv_params* params, int32_t page_rows, size_t* out_bytes)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (!out_bytes) return fail(AUDIOKV_E_INVALID_ARG, "out_bytes is NULL");
+    if (page_rows != 32 && page_rows != 64 && page_rows != 128 && page_rows != 256)
+        return fail(AUDIOKV_E_INVALID_ARG, "page_rows %d: 32, 64, 128 or 256", page_rows);
+    *out_bytes = (size_t)page_rows * params->head_dim * 17 / 16;
+    return AUDIOKV_OK;
+}
+
+// items of an append, but for their lengths
+static int32_t check_append(const PageView& pv, int32_t n_items, int64_t total_rows)
+{
+    if (n_items < 1 || total_rows < 0 || total_rows > (int64_t)INT32_MAX)
+        return fail(AUDIOKV_E_INVALID_ARG, "n_items %d or total_rows %lld out of range", n_items, (long long)total_rows);
+    if ((long long)n_items * pv.H > (1 << 20)) return fail(AUDIOKV_E_UNSUPPORTED, "too many heads in one call");
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_pages_append_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, int32_t n_items,
+                                             int64_t total_rows, size_t* out_bytes)
+{
+    PageView pv;
+    AUDIOKV_TRY(check_params(params, 0));
+    if (!out_bytes) return fail(AUDIOKV_E_INVALID_ARG, "out_bytes is NULL");
+    if (n_items == 0 || n_seqs == 0) { *out_bytes = 0; return AUDIOKV_OK; }
+    AUDIOKV_TRY(check_pages(params, pages, n_seqs, false, &pv));
+    AUDIOKV_TRY(check_append(pv, n_items, total_rows));
+    *out_bytes = pages_append_bytes(pv, n_seqs, n_items, total_rows);
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_pages_append(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, const void* k, const void* v,
+                             const int32_t* indices_dev, const int32_t* cu_budgets_dev, int64_t total_rows,
+                             const int32_t* cu_seqlens_dev, const int32_t* seqlens_host, int32_t n_items, const int32_t* seqs_dev,
+                             int32_t* refused_dev, void* workspace, size_t workspace_bytes, void* stream)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (n_items == 0 || n_seqs == 0) return AUDIOKV_OK;
+    PageView pv;
+    AUDIOKV_TRY(check_pages(params, pages, n_seqs, true, &pv));
+    Batch b;
+    audiokv_params any_window = *params;
+    any_window.window = 0;
+    AUDIOKV_TRY(check_batch(&any_window, n_items, seqlens_host, &b));
+    if ((indices_dev == nullptr) != (cu_budgets_dev == nullptr))
+        return fail(AUDIOKV_E_INVALID_ARG, "indices and cu_budgets come together");
+    if (!indices_dev) total_rows = b.total_tokens * params->n_kv_heads;
+    AUDIOKV_TRY(check_append(pv, n_items, total_rows));
+    if (total_rows > b.total_tokens * params->n_kv_heads)
+        return fail(AUDIOKV_E_INVALID_ARG, "total_rows %lld: the items have %lld", (long long)total_rows, b.total_tokens * params->n_kv_heads);
+    if (!k || !v || !cu_seqlens_dev) return fail(AUDIOKV_E_INVALID_ARG, "audiokv_pages_append: NULL pointer argument");
+    if (!aligned16(k) || !aligned16(v)) return fail(AUDIOKV_E_INVALID_ARG, "k and v must be 16-byte aligned");
+    if (!seqs_dev && n_items > n_seqs) return fail(AUDIOKV_E_INVALID_ARG, "%d items for %d sequences need seqs", n_items, n_seqs);
+    AUDIOKV_TRY(check_workspace(workspace, workspace_bytes, pages_append_bytes(pv, n_seqs, n_items, total_rows)));
+    AppendCall c{};
+    c.k = k;
+    c.v = v;
+    c.indices = indices_dev;
+    c.cu_budgets = cu_budgets_dev;
+    c.cu_seqlens = cu_seqlens_dev;
+    c.seqs = seqs_dev;
+    c.n_items = n_items;
+    c.n_seqs = n_seqs;
+    c.same_length = b.uniform ? b.max_L : 0;
+    c.total_rows = total_rows;
+    c.refused = refused_dev;
+    AUDIOKV_HIP(launch_pages_append(make_geom(params, n_items), pv, c, workspace, static_cast<hipStream_t>(stream)), "pages_append kernels");
+    return AUDIOKV_OK;
+}
+
+static int32_t check_attend(const audiokv_params* p)
+{
+    if (p->n_q_heads / p->n_kv_heads > 16)
+        return fail(AUDIOKV_E_UNSUPPORTED, "pages_attend: %d query heads per KV head > 16", p->n_q_heads / p->n_kv_heads);
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_pages_attend_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, size_t* out_bytes)
+{
+    PageView pv;
+    AUDIOKV_TRY(check_params(params, 0));
+    if (!out_bytes) return fail(AUDIOKV_E_INVALID_ARG, "out_bytes is NULL");
+    if (n_seqs == 0) { *out_bytes = 0; return AUDIOKV_OK; }
+    AUDIOKV_TRY(check_pages(params, pages, n_seqs, false, &pv));
+    AUDIOKV_TRY(check_attend(params));
+    *out_bytes = pages_attend_bytes(make_geom(params, n_seqs), pv);
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_pages_attend(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, const void* q_dev, void* out_dev,
+                             float* lse_dev, void* workspace, size_t workspace_bytes, void* stream)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (n_seqs == 0) return AUDIOKV_OK;
+    PageView pv;
+    AUDIOKV_TRY(check_pages(params, pages, n_seqs, true, &pv));
+    AUDIOKV_TRY(check_attend(params));
+    if (!q_dev || !out_dev) return fail(AUDIOKV_E_INVALID_ARG, "audiokv_pages_attend: NULL pointer argument");
+    if (!aligned16(q_dev) || !aligned16(out_dev)) return fail(AUDIOKV_E_INVALID_ARG, "q and out must be 16-byte aligned");
+    const Geom g = make_geom(params, n_seqs);
+    AUDIOKV_TRY(check_workspace(workspace, workspace_bytes, pages_attend_bytes(g, pv)));
+    AUDIOKV_HIP(launch_pages_attend(g, pv, q_dev, out_dev, lse_dev, workspace, static_cast<hipStream_t>(stream)), "pages_attend kernels");
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_pages_fork_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, size_t* out_bytes)
+{
+    PageView pv;
+    AUDIOKV_TRY(check_params(params, 0));
+    if (!out_bytes) return fail(AUDIOKV_E_INVALID_ARG, "out_bytes is NULL");
+    if (n_seqs == 0) { *out_bytes = 0; return AUDIOKV_OK; }
+    AUDIOKV_TRY(check_pages(params, pages, n_seqs, false, &pv));
+    *out_bytes = pages_fork_bytes(pv);
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_pages_fork(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, const int32_t* parents_dev,
+                           const int32_t* drop_dev, void* workspace, size_t workspace_bytes, void* stream)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (n_seqs == 0) return AUDIOKV_OK;
+    PageView pv;
+    AUDIOKV_TRY(check_pages(params, pages, n_seqs, true, &pv));
+    AUDIOKV_TRY(check_workspace(workspace, workspace_bytes, pages_fork_bytes(pv)));
+    if (!parents_dev && !drop_dev) return AUDIOKV_OK;          // nobody changes
+    AUDIOKV_HIP(launch_pages_fork(pv, parents_dev, drop_dev, workspace, static_cast<hipStream_t>(stream)), "pages_fork kernels");
+    return AUDIOKV_OK;
+}
+
+static int32_t check_rows(int64_t total_rows)
+{
+    if (total_rows < 0 || total_rows > (int64_t)INT32_MAX)
+        return fail(AUDIOKV_E_INVALID_ARG, "total_rows %lld must lie in [0, 2^31)", (long long)total_rows);
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_pages_keep_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, int64_t total_rows,
+                                           size_t* out_bytes)
+{
+    PageView pv;
+    AUDIOKV_TRY(check_params(params, 0));
+    if (!out_bytes) return fail(AUDIOKV_E_INVALID_ARG, "out_bytes is NULL");
+    if (n_seqs == 0) { *out_bytes = 0; return AUDIOKV_OK; }
+    AUDIOKV_TRY(check_pages(params, pages, n_seqs, false, &pv));
+    AUDIOKV_TRY(check_rows(total_rows));
+    *out_bytes = pages_keep_bytes(pv, total_rows);
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_pages_keep(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, const int32_t* indices_dev,
+                           const int32_t* cu_budgets_dev, int64_t total_rows, int32_t* refused_dev, void* workspace,
+                           size_t workspace_bytes, void* stream)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (n_seqs == 0) return AUDIOKV_OK;
+    PageView pv;
+    AUDIOKV_TRY(check_pages(params, pages, n_seqs, true, &pv));
+    AUDIOKV_TRY(check_rows(total_rows));
+    if (!cu_budgets_dev || (!indices_dev && total_rows > 0))
+        return fail(AUDIOKV_E_INVALID_ARG, "audiokv_pages_keep: NULL pointer argument");
+    AUDIOKV_TRY(check_workspace(workspace, workspace_bytes, pages_keep_bytes(pv, total_rows)));
+    AUDIOKV_HIP(launch_pages_keep(pv, indices_dev, cu_budgets_dev, total_rows, refused_dev, workspace, static_cast<hipStream_t>(stream)),
+                "pages_keep kernels");
+    return AUDIOKV_OK;
+}
+
+int32_t audiokv_pages_read(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, const int32_t* first_dev,
+                           const int32_t* cu_rows_dev, int64_t total_rows, void* k_out, void* v_out, void* stream)
+{
+    AUDIOKV_TRY(check_params(params, 0));
+    if (n_seqs == 0) return AUDIOKV_OK;
+    PageView pv;
+    AUDIOKV_TRY(check_pages(params, pages, n_seqs, true, &pv));
+    AUDIOKV_TRY(check_rows(total_rows));
+    if (total_rows == 0) return AUDIOKV_OK;
+    if (!cu_rows_dev || !k_out || !v_out) return fail(AUDIOKV_E_INVALID_ARG, "audiokv_pages_read: NULL pointer argument");
+    if (!aligned16(k_out) || !aligned16(v_out)) return fail(AUDIOKV_E_INVALID_ARG, "k_out and v_out must be 16-byte aligned");
+    AUDIOKV_HIP(launch_pages_read(pv, first_dev, cu_rows_dev, total_rows, k_out, v_out, static_cast<hipStream_t>(stream)), "pages_read kernel");
     return AUDIOKV_OK;
 }
 

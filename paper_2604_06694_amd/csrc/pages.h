@@ -1,0 +1,162 @@
+// The cache in 4 bits and in pages (audiokv_pages): where things lie, and how rows are rounded and read. A header of its own
+// because the limits and the walk over segments are checked on the host as well (tests/pages_check.cpp).
+//
+// A page holds P rows of one KV head: K's codes [P][D / 2], V's codes, K's scales [P][D / 32], V's scales. Rows of codes are 32 to
+// 128 bytes, so that sections begin at multiples of 16 bytes whatever P (a multiple of 32) is.
+#pragma once
+
+#include "common.h"
+
+namespace audiokv {
+
+struct PageView {
+    char* pool;
+    int32_t *table, *lengths, *refs, *state;
+    int n_pages, width, log_p;      // pages of the pool; entries of a head's table row; log2 of a page's rows
+    int n_heads, H, D;
+
+    __host__ __device__ int rows() const { return 1 << log_p; }
+    __host__ __device__ size_t page_bytes() const { return (size_t)(D + D / 16) << log_p; }
+    __host__ __device__ int pages_of(int n) const { return (int)(((long long)n + rows() - 1) >> log_p); }
+    // Sections of a page, from its first byte
+    __host__ __device__ size_t k_codes(int row) const { return (size_t)row * (D / 2); }
+    __host__ __device__ size_t v_codes(int row) const { return ((size_t)(D / 2) << log_p) + (size_t)row * (D / 2); }
+    __host__ __device__ size_t k_scales(int row) const { return ((size_t)D << log_p) + (size_t)row * (D / 32); }
+    __host__ __device__ size_t v_scales(int row) const { return ((size_t)(D + D / 32) << log_p) + (size_t)row * (D / 32); }
+    __host__ __device__ char* page(int p) const { return pool + (size_t)p * page_bytes(); }
+    __host__ __device__ bool is_page(int p) const { return (unsigned)p < (unsigned)n_pages; }
+    // Rows of a head. A length that its table row cannot hold is a caller's error; cut so that nothing is read past the row
+    __device__ __forceinline__ int length(int head) const { return min(max(lengths[head], 0), width << log_p); }
+};
+
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+// The scale byte of a block whose largest magnitude has the bits `top` (bf16 without the sign): the smallest power of two s with
+// top <= 7 s. 7 is in the middle of 6 and 8 and goes to 6, so that no value is further off than half a step of its neighbours.
+// Added 0x1f carries into the exponent where the mantissa is beyond 1.75 = 7 / 4. Within 2 and 252, so that every value that codes
+// stand for is a normal number of bf16 or zero; 255 with an infinity or NaN in the block.
+__host__ __device__ __forceinline__ int scale_of(unsigned top) {
+    const int e = (int)((top + 0x1f) >> 7) - 2;
+    return top >= 0x7f80 ? 255 : e < 2 ? 2 : e > 252 ? 252 : e;
+}
+
+// Rows of queues: largest g with cu[g] * times <= p (cu is a non-decreasing exclusive scan; p uniform). Every round probes 64 entries
+// at equal distances, one per lane: one load latency for up to 64 of them, two up to 4096.
+__device__ __forceinline__ int owner_of_row(const int32_t* __restrict__ cu, int n, int times, long long p) {
+    int head = 0;
+    for (int span = n; span > 1;) {
+        const int step = (span + 63) >> 6;
+        const int probe = head + (int)(threadIdx.x & 63) * step;
+        const bool at_or_before = probe < head + span && (long long)cu[min(probe, n - 1)] * times <= p;
+        const int k = __builtin_popcountll(__builtin_amdgcn_ballot_w64(at_or_before));   // a prefix of the lanes
+        const int skip = k > 0 ? (k - 1) * step : 0;
+        head += skip;
+        span = min(step, span - skip);
+    }
+    return __builtin_amdgcn_readfirstlane(head);
+}
+
+// Sum over the lanes before this one and, in `total`, over the workgroup, whose waves' sums go through `sums` (a barrier before
+// and after).
+template <int THREADS>
+__device__ __forceinline__ int exclusive_sum(int x, int* sums, int& total) {
+    const int incl = wave_incl(x), wave = threadIdx.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 63) sums[wave] = incl;
+    __syncthreads();
+    int before = 0;
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+        const int s = sums[w];
+        before += w < wave ? s : 0;
+        total += s;
+    }
+    return before + incl - x;
+}
+
+// What append and keep plan on the device, by one workgroup: which pages the heads get.
+// The first `want` pages with refs 0 from state[1] upwards and round, in that order, to found[]. Returns how many there were, and in
+// `next` where the following search begins. (sums: (4 * THREADS / 64) ints of LDS)
+template <int THREADS>
+__device__ int find_pages(const PageView& pv, int want, int32_t* __restrict__ found, int* sums, int& next) {
+    constexpr int U = 4, WAVES = THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int begin = min(max(pv.state[1], 0), pv.n_pages - 1);
+    int have = 0;
+    next = begin;
+    __shared__ int last;
+    for (int base = 0; base < pv.n_pages && have < want; base += THREADS * U) {
+        int page[U];
+        unsigned long long free_in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const long long i = (long long)base + u * THREADS + threadIdx.x;
+            long long p = begin + i;
+            if (p >= pv.n_pages) p -= pv.n_pages;
+            page[u] = (int)p;
+            free_in[u] = __builtin_amdgcn_ballot_w64(i < pv.n_pages && pv.refs[min(p, (long long)pv.n_pages - 1)] == 0);
+        }
+        __syncthreads();
+        if (lane == 0)
+#pragma unroll
+            for (int u = 0; u < U; ++u) sums[u * WAVES + wave] = __builtin_popcountll(free_in[u]);
+        __syncthreads();
+        int before = have;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            for (int w = 0; w < WAVES; ++w) {
+                if (w == wave) {
+                    const int at = before + __builtin_popcountll(free_in[u] & ((1ull << lane) - 1));
+                    if ((free_in[u] >> lane & 1) && at < want) {
+                        found[at] = page[u];
+                        if (at == want - 1) last = page[u];
+                    }
+                }
+                before += sums[u * WAVES + w];
+            }
+        have = before;
+    }
+    have = min(have, want);
+    __syncthreads();
+    // (fewer than wanted: the state said that there were more. The search ends where it began)
+    if (want > 0 && have == want) next = last + 1 == pv.n_pages ? 0 : last + 1;
+    for (int i = have + threadIdx.x; i < want; i += THREADS) found[i] = -1;
+    return have;
+}
+
+inline size_t up256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }    // parts of a workspace begin at multiples of 256 bytes
+
+// CALL with kD, the head's channels, a constant
+#define AUDIOKV_FOR_DIM(D, CALL)                                 \
+    switch (D) {                                                 \
+        case 64: { constexpr int kD = 64; CALL; break; }         \
+        case 128: { constexpr int kD = 128; CALL; break; }       \
+        case 256: { constexpr int kD = 256; CALL; break; }       \
+        default: return hipErrorInvalidValue;                    \
+    }
+
+// ---- launchers ---------------------------------------------------------------------------------------------------------------------
+
+struct AppendCall {
+    const void *k, *v;
+    const int32_t *indices, *cu_budgets, *cu_seqlens, *seqs;
+    int n_items, n_seqs, same_length;       // same_length: tokens of every item, 0: they differ
+    long long total_rows;
+    int32_t* refused;
+};
+size_t pages_append_bytes(const PageView& pv, int n_seqs, int n_items, long long total_rows);
+hipError_t launch_pages_append(const Geom& g, const PageView& pv, const AppendCall& c, void* workspace, hipStream_t s);
+hipError_t launch_pages_read(const PageView& pv, const int32_t* first, const int32_t* cu_rows, long long total_rows, void* k_out,
+                             void* v_out, hipStream_t s);
+size_t pages_fork_bytes(const PageView& pv);
+hipError_t launch_pages_fork(const PageView& pv, const int32_t* parents, const int32_t* drop, void* workspace, hipStream_t s);
+size_t pages_keep_bytes(const PageView& pv, long long total_rows);
+hipError_t launch_pages_keep(const PageView& pv, const int32_t* indices, const int32_t* cu_budgets, long long total_rows,
+                             int32_t* refused, void* workspace, hipStream_t s);
+size_t pages_attend_bytes(const Geom& g, const PageView& pv);
+hipError_t launch_pages_attend(const Geom& g, const PageView& pv, const void* q, void* out, float* lse, void* workspace, hipStream_t s);
+
+}  // namespace audiokv

@@ -1,0 +1,442 @@
+// One decoding step on the cache in 4 bits and in pages (audiokv_pages_attend): every query head attends to its KV head's rows.
+//
+// Bound: the rows' bytes, 17/16 per channel of K and V together, each read once for all G query heads of the group. A row of D channels
+// costs 2 G D products and G exponentials; on the vector units its conversion, about one instruction per channel of K and V and 64 rows.
+//
+// Heads have lengths of their own, known on the device only, so the work is cut there: the units of 32 rows of all heads one behind
+// the other, and workgroup w of W takes units [T w / W, T (w + 1) / W), which may end one head, hold several and begin another. Every
+// workgroup adds up the lengths for itself. A head that lies within one workgroup is finished there; what the others find for a part of
+// a head goes to the workspace (at most two parts a workgroup, its first and its last) and a second launch joins it. No atomics;
+// every sum has a fixed order.
+//
+// A wave takes every fourth unit. Both products are 16 x 16 x 32 on the matrix cores, with the query heads as columns, padded to 16:
+//   C[key][query] = K Q^T       lane (c = lane & 15, r = lane >> 4) holds row c of K, channels of scale block r: its codes are one load,
+//                               its scale one byte, and the conversion to bf16 is exact (a magnitude of e2m1 has two bits)
+//   O[channel][query] += V^T P  the lane's C, keys 4 r .. 4 r + 3 of two tiles, is its column of P as it is: the product runs over keys in
+//                               that order, and V's rows are loaded so
+// The running reference of the softmax moves only where a logit exceeds it by 2^8: a wave-wide test per unit instead of a maximum over
+// lanes and a rescaling. P goes to the second product as two bf16 numbers (16 bits of it), V in bf16 is exact.
+#include "pages.h"
+
+namespace audiokv {
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4, kUnit = 32;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
+
+constexpr float kSlack = 8.f;       // octaves that a logit may lie above the reference
+
+struct AttendSpace {
+    int2* heads;            // [heads]: slot of the first part, parts (0: nothing to join)
+    float* stats;           // [slot][G][2]: reference in base-2 units, sum
+    float* parts;           // [slot][G][D]
+};
+
+// how the channels of a row lie over the lanes: k-step `s` of lane group r begins at this channel
+template <int D> __device__ __forceinline__ constexpr int channel_of(int s, int r) {
+    return D == 64 ? r * 16 + s * 8 : (s >> 2) * 128 + r * 32 + (s & 3) * 8;
+}
+
+template <int D> struct Rows32 {         // one unit on its way: what a lane holds of it
+    static constexpr int KW = D / 32;    // dwords of K's codes per tile of 16 rows
+    unsigned k[2][KW], ks[2], v[8][(D + 127) / 128], vs[8];
+};
+
+__device__ __forceinline__ float exponent_of(unsigned word, int byte) {     // 2^(e - 127) of a byte (the conversions read no other bits)
+    return __uint_as_float(__builtin_amdgcn_alignbit(word, word, (9 + 8 * byte) & 31));
+}
+
+template <int D>
+__device__ __forceinline__ void load_unit(Rows32<D>& u, const PageView& pv, int page, int row0) {
+    const int lane = threadIdx.x & 63, c = lane & 15, r = lane >> 4;
+    const char* base = pv.page(page);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        const int row = row0 + t * 16 + c;
+        const char* k = base + pv.k_codes(row);
+        const unsigned char* e = reinterpret_cast<const unsigned char*>(base + pv.k_scales(row));
+        if constexpr (D == 64) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(k + r * 8);
+            u.k[t][0] = w[0];
+            u.k[t][1] = w[1];
+            u.ks[t] = e[r >> 1];
+        } else {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(k + r * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u.k[t][i] = w[i];
+            u.ks[t] = e[r];
+            if constexpr (D == 256) {
+                const u32x4 w2 = *reinterpret_cast<const u32x4*>(k + 64 + r * 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u.k[t][4 + i] = w2[i];
+                u.ks[t] |= (unsigned)e[4 + r] << 8;
+            }
+        }
+    }
+    // V: rows 4 r + i of either tile, channels c * D / 16 ..
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = row0 + t * 16 + r * 4 + i, n = t * 4 + i;
+            const char* v = base + pv.v_codes(row) + c * (D / 32);
+            if constexpr (D == 64) u.v[n][0] = *reinterpret_cast<const unsigned short*>(v);
+            else if constexpr (D == 128) u.v[n][0] = *reinterpret_cast<const unsigned*>(v);
+            else {
+                const u32x2 w = *reinterpret_cast<const u32x2*>(v);
+                u.v[n][0] = w[0];
+                u.v[n][1] = w[1];
+            }
+        }
+    const char* e = base + pv.v_scales(row0 + r * 4);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        if constexpr (D == 128) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(e + t * 64);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u.vs[t * 4 + i] = w[i];
+        } else if constexpr (D == 64) {                                       // two rows to a dword
+            const u32x2 w = *reinterpret_cast<const u32x2*>(e + t * 32);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u.vs[t * 4 + i] = w[i >> 1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u.vs[t * 4 + i] = *reinterpret_cast<const unsigned*>(e + t * 128 + i * 8 + (c >> 3) * 4);
+        }
+    }
+}
+// which byte of u.vs[n] is the scale of the lane's channels of V
+template <int D> __device__ __forceinline__ int scale_byte(int n, int c) {
+    return D == 64 ? (n & 1) * 2 + (c >> 3) : D == 128 ? c >> 2 : (c >> 1) & 3;
+}
+
+#if defined(__HIP_DEVICE_COMPILE__)
+__device__ __forceinline__ unsigned pair_of(unsigned codes, float scale, int byte) {
+    switch (byte) {
+        case 0: return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
+        case 1: return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
+        case 2: return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
+        default: return __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
+    }
+}
+#else
+__device__ __forceinline__ unsigned pair_of(unsigned, float, int) { return 0; }
+#endif
+
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {             // nearest even
+    bf16x2 x;
+    x[0] = (__bf16)a;
+    x[1] = (__bf16)b;
+    return __builtin_bit_cast(unsigned, x);
+}
+
+// What a wave knows of a head so far. Column c = lane & 15 is a query; `sum` is the lane's share of it.
+template <int D> struct Running {
+    f32x4 out[D / 16];      // out[ct][i]: channel (4 r + i) * D / 16 + ct
+    float ref, sum;
+};
+
+template <int D>
+__device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, const bf16x8 (&q)[D / 32], float c_log2, int rows) {
+    const int lane = threadIdx.x & 63, c = lane & 15, r = lane >> 4;
+    float z[8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            const float scale = __uint_as_float(D == 256 && s >= 4 ? u.ks[t] << 15 : u.ks[t] << 23);
+            u32x4_t f;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) f[b] = pair_of(u.k[t][s], scale, b);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), q[s], acc, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[t * 4 + i] = acc[i] * c_log2;
+    }
+    unsigned vs[8];
+#pragma unroll
+    for (int n = 0; n < 8; ++n) vs[n] = u.vs[n];
+    if (rows < kUnit) {                                    // wave-uniform: a head's last unit
+#pragma unroll
+        for (int n = 0; n < 8; ++n) {
+            const bool there = (n >> 2) * 16 + r * 4 + (n & 3) < rows;
+            z[n] = there ? z[n] : -INFINITY;
+            vs[n] = there ? vs[n] : 0x7f7f7f7f;            // what lies behind the last row may say NaN, which zero times is NaN
+        }
+    }
+    float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
+    if (__builtin_amdgcn_ballot_w64(top > o.ref + kSlack) != 0) {
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float ref = fmaxf(o.ref, top);
+        const float shrink = o.ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(o.ref - ref);
+        o.ref = ref;
+        o.sum *= shrink;
+#pragma unroll
+        for (int ct = 0; ct < D / 16; ++ct) o.out[ct] *= shrink;
+    }
+    const float ref = o.ref == -INFINITY ? 0.f : o.ref;
+    u32x4_t hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = __builtin_amdgcn_exp2f(z[2 * i] - ref), b = __builtin_amdgcn_exp2f(z[2 * i + 1] - ref);
+        o.sum += a + b;
+        hi[i] = pack_bf16(a, b);
+        lo[i] = pack_bf16(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xffff0000u));
+    }
+#pragma unroll
+    for (int w = 0; w < (D + 127) / 128; ++w)
+#pragma unroll
+        for (int b = 0; b < (D == 64 ? 2 : 4); ++b) {
+            u32x4_t even, odd;                             // channels 8 w + 2 b and 2 b + 1 of the lane's, keys by twos
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const unsigned x = pair_of(u.v[2 * i][w], exponent_of(vs[2 * i], scale_byte<D>(2 * i, c)), b);
+                const unsigned y = pair_of(u.v[2 * i + 1][w], exponent_of(vs[2 * i + 1], scale_byte<D>(2 * i + 1, c)), b);
+                even[i] = __builtin_amdgcn_perm(y, x, 0x05040100);
+                odd[i] = __builtin_amdgcn_perm(y, x, 0x07060302);
+            }
+            const int ct = w * 8 + b * 2;
+            o.out[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), __builtin_bit_cast(bf16x8, hi), o.out[ct], 0, 0, 0);
+            o.out[ct + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), __builtin_bit_cast(bf16x8, hi), o.out[ct + 1], 0, 0, 0);
+            o.out[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), __builtin_bit_cast(bf16x8, lo), o.out[ct], 0, 0, 0);
+            o.out[ct + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), __builtin_bit_cast(bf16x8, lo), o.out[ct + 1], 0, 0, 0);
+        }
+}
+
+// First of 64 heads or more, from `head` on, that has rows; n_heads if none has. (wave-uniform)
+__device__ __forceinline__ int next_with_rows(const PageView& pv, int head) {
+    for (; head < pv.n_heads; head += 64) {
+        const int g = head + (int)(threadIdx.x & 63);
+        const unsigned long long m = __builtin_amdgcn_ballot_w64(g < pv.n_heads && pv.length(min(g, pv.n_heads - 1)) > 0);
+        if (m) return head + __builtin_ctzll(m);
+    }
+    return pv.n_heads;
+}
+
+__device__ __forceinline__ int units_of(int rows) { return (rows + kUnit - 1) / kUnit; }
+
+// first unit of workgroup w, and the workgroup that has a unit
+__device__ __forceinline__ long long first_unit(long long units, int w, int W) { return units * w / W; }
+__device__ __forceinline__ int workgroup_of(long long units, long long u, int W) { return (int)(((u + 1) * W - 1) / units); }
+
+// dynamic LDS: [wave][G][D + 4]
+template <int D>
+__global__ __launch_bounds__(kThreads) void attend_kernel(Geom g, PageView pv, const __bf16* __restrict__ q, __bf16* __restrict__ out,
+                                                          float* __restrict__ lse, AttendSpace a)
+{
+    extern __shared__ __attribute__((aligned(16))) float merge[];
+    __shared__ int sums[kWaves];
+    __shared__ float ref_of[kWaves][16], sum_of[kWaves][16];
+    __shared__ int begin_head, begin_unit;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, r = lane >> 4;
+    const int G = g.G, PITCH = D + 4;
+
+    // all units, and where this workgroup's first one is
+    const int each = (pv.n_heads + kThreads - 1) / kThreads, h0 = min(tid * each, pv.n_heads), h1 = min(h0 + each, pv.n_heads);
+    int mine = 0;
+    for (int h = h0; h < h1; ++h) mine += units_of(pv.length(h));
+    int total;
+    const int before = exclusive_sum<kThreads>(mine, sums, total);
+    const int W = min((int)gridDim.x, max(1, (total + kWaves - 1) / kWaves));
+    if ((int)blockIdx.x >= W || total == 0) return;
+    const int u0 = (int)first_unit(total, blockIdx.x, W), u1 = (int)first_unit(total, blockIdx.x + 1, W);
+    if (mine > 0 && u0 >= before && u0 < before + mine) {
+        int h = h0, at = before;
+        for (;; ++h) {
+            const int n = units_of(pv.length(h));
+            if (u0 < at + n) break;
+            at += n;
+        }
+        begin_head = h;
+        begin_unit = at;
+    }
+    __syncthreads();
+    int head = __builtin_amdgcn_readfirstlane(begin_head), start = __builtin_amdgcn_readfirstlane(begin_unit);
+
+    for (int u = u0; u < u1;) {
+        const int rows = __builtin_amdgcn_readfirstlane(pv.length(head)), units = units_of(rows);
+        const int from = u - start, to = min(units, u1 - start);           // units of this head
+        const int x = head / g.H_kv, h = head - x * g.H_kv;
+        const int32_t* table = pv.table + (size_t)head * pv.width;
+        const int log_u = pv.log_p - 5;                                    // units to a page
+        bf16x8 qf[D / 32];
+        {
+            const __bf16* src = q + ((size_t)x * g.H_q + (size_t)h * G + min(c, G - 1)) * D;    // (columns from G on: copies, unused)
+#pragma unroll
+            for (int s = 0; s < D / 32; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(src + channel_of<D>(s, r));
+        }
+        Running<D> o;
+#pragma unroll
+        for (int ct = 0; ct < D / 16; ++ct) o.out[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+        o.ref = -INFINITY;
+        o.sum = 0.f;
+        for (int i = from + wave; i < to; i += kWaves) {
+            const int page = __builtin_amdgcn_readfirstlane(table[i >> log_u]);
+            const bool good = pv.is_page(page);                            // (rows of none take no part)
+            Rows32<D> unit;
+            load_unit<D>(unit, pv, good ? page : 0, (i & ((1 << log_u) - 1)) * kUnit);
+            add_unit<D>(o, unit, qf, g.c_log2, good ? min(kUnit, rows - i * kUnit) : 0);
+        }
+        // the four waves' findings
+        float sum = o.sum;
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        if (r == 0) {
+            ref_of[wave][c] = o.ref;
+            sum_of[wave][c] = sum;
+        }
+        __syncthreads();
+        const float all = fmaxf(fmaxf(ref_of[0][c], ref_of[1][c]), fmaxf(ref_of[2][c], ref_of[3][c]));
+        const float shrink = o.ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(o.ref - all);
+        if (c < G) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int ct = 0; ct < D / 16; ct += 4)
+                    *reinterpret_cast<f32x4*>(&merge[(wave * G + c) * PITCH + (r * 4 + i) * (D / 16) + ct]) =
+                        f32x4{o.out[ct][i], o.out[ct + 1][i], o.out[ct + 2][i], o.out[ct + 3][i]} * shrink;
+        }
+        __syncthreads();
+        const bool whole = from == 0 && to == units;
+        const int slot = 2 * blockIdx.x + (u != u0);
+        if (tid == 0) {
+            if (whole) a.heads[head] = int2{0, 0};
+            else if (from == 0) a.heads[head] = int2{slot, workgroup_of(total, start + units - 1, W) - (int)blockIdx.x + 1};
+        }
+        auto sums_of = [&](int n, float& m) {
+            m = fmaxf(fmaxf(ref_of[0][n], ref_of[1][n]), fmaxf(ref_of[2][n], ref_of[3][n]));
+            float l = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) l += sum_of[w][n] * (ref_of[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref_of[w][n] - m));   // (NaN stays NaN)
+            return l;
+        };
+        for (int e = tid * 4; e < G * D; e += kThreads * 4) {
+            const int n = e / D, ch = e % D;
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(&merge[(w * G + n) * PITCH + ch]);
+            if (whole) {
+                float m;
+                const float l = sums_of(n, m);
+                if (l != 0.f) v /= l;                                     // (no weight at all: zeros)
+                *reinterpret_cast<u32x2*>(out + ((size_t)x * g.H_q + (size_t)h * G + n) * D + ch) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+            } else {
+                *reinterpret_cast<f32x4*>(a.parts + ((size_t)slot * G + n) * D + ch) = v;
+            }
+        }
+        if (tid < G) {
+            float m;
+            const float l = sums_of(tid, m);
+            if (!whole) {
+                a.stats[((size_t)slot * G + tid) * 2] = m;
+                a.stats[((size_t)slot * G + tid) * 2 + 1] = l;
+            } else if (lse) {
+                lse[(size_t)x * g.H_q + (size_t)h * G + tid] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+            }
+        }
+        u = start + to;
+        start += units;
+        if (u < u1) head = next_with_rows(pv, head + 1);
+        __syncthreads();                                                   // the LDS is free again
+    }
+}
+
+// One workgroup per query head: the parts of its KV head, in order. A head without rows gives zeros.
+template <int D>
+__global__ __launch_bounds__(kThreads) void join_kernel(Geom g, PageView pv, __bf16* __restrict__ out, float* __restrict__ lse, AttendSpace a)
+{
+    constexpr int QUADS = D / 4, GROUPS = kThreads / QUADS;                // threads on four channels each, parts at a time
+    const int G = g.G, head = blockIdx.x / G, n = blockIdx.x - head * G, tid = threadIdx.x;
+    const int x = head / g.H_kv, h = head - x * g.H_kv;
+    const size_t row = (size_t)x * g.H_q + (size_t)h * G + n;
+    if (pv.length(head) == 0) {
+        if (tid < QUADS) *reinterpret_cast<u32x2*>(out + row * D + tid * 4) = u32x2{0, 0};
+        if (lse && tid == 0) lse[row] = -INFINITY;
+        return;
+    }
+    const int2 from = a.heads[head];
+    if (from.y == 0) return;
+    __shared__ float wave_m[kThreads / 64], wave_l[kThreads / 64];
+    __shared__ __attribute__((aligned(16))) f32x4 red[kThreads];
+    // part p of the head: the first where the head began, the others the first of the workgroups behind
+    auto slot_of = [&](int p) { return p == 0 ? from.x : (from.x & ~1) + 2 * p; };
+    auto stat = [&](int p) { return *reinterpret_cast<const float2*>(&a.stats[((size_t)slot_of(p) * G + n) * 2]); };
+    float m = -INFINITY;
+    for (int p = tid; p < from.y; p += kThreads) m = fmaxf(m, stat(p).x);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    if ((tid & 63) == 0) wave_m[tid >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
+    auto weight = [&](float ref) { return ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - m); };
+    float l = 0.f;
+    for (int p = tid; p < from.y; p += kThreads) {
+        const float2 s = stat(p);
+        l += weight(s.x) * s.y;
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
+    if ((tid & 63) == 0) wave_l[tid >> 6] = l;
+    const int ch = tid % QUADS * 4, grp = tid / QUADS;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int p = grp; p < from.y; p += GROUPS)
+        acc += *reinterpret_cast<const f32x4*>(a.parts + ((size_t)slot_of(p) * G + n) * D + ch) * weight(stat(p).x);
+    red[tid] = acc;
+    __syncthreads();
+    l = ((wave_l[0] + wave_l[1]) + wave_l[2]) + wave_l[3];
+    if (grp == 0) {
+        for (int k = 1; k < GROUPS; ++k) acc += red[k * QUADS + tid];
+        if (l != 0.f) acc /= l;
+        *reinterpret_cast<u32x2*>(out + row * D + ch) = u32x2{pack_bf16(acc[0], acc[1]), pack_bf16(acc[2], acc[3])};
+        if (lse && tid == 0) lse[row] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    }
+}
+
+// Workgroups: as many as the registers let run at once, so that equal shares end together
+int workgroups(const Geom& g, const PageView& pv) {
+    const long long most = ((long long)pv.n_heads * pv.width << pv.log_p) / (kUnit * kWaves) + pv.n_heads;
+    const int w = 256 * (g.D == 256 ? 2 : 4);
+    return (int)(most < w ? most : w);
+}
+
+AttendSpace attend_space(const Geom& g, const PageView& pv, void* workspace, size_t* bytes) {
+    AttendSpace a;
+    const size_t slots = 2 * (size_t)workgroups(g, pv);
+    char* at = static_cast<char*>(workspace);
+    a.heads = reinterpret_cast<int2*>(at);
+    size_t off = up256((size_t)pv.n_heads * sizeof(int2));
+    a.stats = reinterpret_cast<float*>(at + off);
+    off += up256(slots * g.G * 2 * sizeof(float));
+    a.parts = reinterpret_cast<float*>(at + off);
+    off += slots * g.G * g.D * sizeof(float);
+    if (bytes) *bytes = off;
+    return a;
+}
+
+}  // namespace
+
+size_t pages_attend_bytes(const Geom& g, const PageView& pv) {
+    size_t bytes;
+    attend_space(g, pv, nullptr, &bytes);
+    return bytes;
+}
+
+hipError_t launch_pages_attend(const Geom& g, const PageView& pv, const void* q, void* out, float* lse, void* workspace, hipStream_t s)
+{
+    const AttendSpace a = attend_space(g, pv, workspace, nullptr);
+    const dim3 grid((unsigned)workgroups(g, pv)), join((unsigned)(pv.n_heads * g.G));
+    const unsigned lds = (unsigned)(sizeof(float) * kWaves * g.G * (g.D + 4));
+    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL(attend_kernel<kD>, grid, dim3(kThreads), lds, s, g, pv, (const __bf16*)q, (__bf16*)out, lse, a))
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL(join_kernel<kD>, join, dim3(kThreads), 0, s, g, pv, (__bf16*)out, lse, a))
+    return hipGetLastError();
+}
+
+}  // namespace audiokv

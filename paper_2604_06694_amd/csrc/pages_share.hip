@@ -1,0 +1,252 @@
+// Pages that sequences take over, share and give back (audiokv_pages_fork), and heads cut to given rows (audiokv_pages_keep).
+// No arithmetic: table entries and counts, and for keep the kept rows' bytes.
+//
+// fork is two launches over the table, because a sequence may take over pages of one whose own entries change in the same call: the
+// first lists every new entry in the workspace and counts the pages' new owners, the second takes away the old owners and writes the
+// table. A page is free when its last owner goes, which only the second launch can bring about, once for every page: what it adds to
+// state[0] does not depend on the order. Entries that stay as they are touch no count (after a reorder of beams that share their
+// prompt nearly all do), which spares the atomics on pages that many sequences have.
+//
+// keep is three launches: one workgroup decides who gets which pages; the kept rows are copied into them, the table still as it was;
+// the table and the counts change. Whole pages whose rows are all kept, from the first on, stay (and stay shared).
+#include "pages.h"
+
+namespace audiokv {
+
+namespace {
+
+constexpr int kThreads = 256, kPlanThreads = 1024;
+
+// ---- fork --------------------------------------------------------------------------------------------------------------------------
+
+struct ForkSpace {
+    int32_t* rows;          // [heads]: length after the call
+    int32_t* entries;       // [heads][width]: table after the call, as far as it is not what it was
+};
+ForkSpace fork_space(const PageView& pv, void* workspace, size_t* bytes) {
+    ForkSpace f;
+    f.rows = static_cast<int32_t*>(workspace);
+    const size_t at = up256((size_t)pv.n_heads * 4);
+    f.entries = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + at);
+    if (bytes) *bytes = at + up256((size_t)pv.n_heads * pv.width * 4);
+    return f;
+}
+
+// One workgroup per head, in both launches.
+__global__ __launch_bounds__(kThreads) void fork_take_kernel(PageView pv, const int32_t* __restrict__ parents,
+                                                             const int32_t* __restrict__ drop, int n_seqs, ForkSpace f)
+{
+    const int head = blockIdx.x, x = head / pv.H, h = head - x * pv.H;
+    const int parent = parents ? parents[x] : x;
+    const bool taken = (unsigned)parent < (unsigned)n_seqs;
+    const int from = taken ? parent * pv.H + h : head;
+    const int rows = taken ? max(pv.length(from) - (drop ? max(drop[x], 0) : 0), 0) : 0;
+    if (threadIdx.x == 0) f.rows[head] = rows;
+    if (from == head) return;                              // its own pages, or none
+    const int had = pv.pages_of(pv.length(head)), has = pv.pages_of(rows);
+    const int32_t *mine = pv.table + (size_t)head * pv.width, *theirs = pv.table + (size_t)from * pv.width;
+    for (int j = threadIdx.x; j < has; j += kThreads) {
+        const int page = theirs[j];
+        f.entries[(size_t)head * pv.width + j] = page;
+        if (pv.is_page(page) && (j >= had || mine[j] != page)) atomicAdd(&pv.refs[page], 1);
+    }
+}
+
+__global__ __launch_bounds__(kThreads) void fork_give_kernel(PageView pv, const int32_t* __restrict__ parents, int n_seqs, ForkSpace f)
+{
+    const int head = blockIdx.x, x = head / pv.H;
+    const int parent = parents ? parents[x] : x;
+    const bool same = parent == x || (unsigned)parent >= (unsigned)n_seqs;      // no entry changes, some may go
+    const int rows = f.rows[head], was = pv.length(head);
+    const int had = pv.pages_of(was), has = pv.pages_of(rows);
+    int32_t* mine = pv.table + (size_t)head * pv.width;
+    int freed = 0;
+    for (int j = threadIdx.x; j < max(had, has); j += kThreads) {
+        const int now = j < has ? same ? mine[j] : f.entries[(size_t)head * pv.width + j] : -1;
+        if (j < had) {
+            const int page = mine[j];
+            if (page != now && pv.is_page(page)) freed += atomicSub(&pv.refs[page], 1) == 1;
+        }
+        if (j < has && !same) mine[j] = now;
+    }
+    if (rows != was && threadIdx.x == 0) pv.lengths[head] = rows;
+    freed = wave_incl(freed);
+    if ((threadIdx.x & 63) == 63 && freed > 0) atomicAdd(&pv.state[0], freed);
+}
+
+// ---- keep --------------------------------------------------------------------------------------------------------------------------
+
+struct KeepJob {
+    int rows;               // kept: the length after the call; -1: the head stays as it is
+    int same;               // whole pages that stay
+    int first;              // where its new pages begin in the list
+    int had;                // rows before
+};
+struct KeepSpace {
+    KeepJob* jobs;
+    int32_t* found;
+    int most;
+};
+KeepSpace keep_space(const PageView& pv, long long total_rows, void* workspace, size_t* bytes) {
+    KeepSpace a;
+    a.jobs = static_cast<KeepJob*>(workspace);
+    const size_t at = up256((size_t)pv.n_heads * sizeof(KeepJob));
+    a.found = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + at);
+    const long long n = (total_rows >> pv.log_p) + pv.n_heads;       // a head's last page may be begun
+    a.most = (int)(n < pv.n_pages ? n : pv.n_pages);
+    if (bytes) *bytes = at + up256((size_t)a.most * 4);
+    return a;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void keep_plan_kernel(PageView pv, const int32_t* __restrict__ indices,
+                                                                 const int32_t* __restrict__ cu_b, int total_rows, KeepSpace a,
+                                                                 int32_t* __restrict__ refused)
+{
+    __shared__ int sums[4 * kPlanThreads / 64];
+    __shared__ int served_pages, lost;
+    const int tid = threadIdx.x, P = pv.rows();
+    if (tid == 0) served_pages = lost = 0;
+    const int n_free = min(max(pv.state[0], 0), a.most), really_free = max(pv.state[0], 0);
+    int running = 0;
+    for (int base = 0; base < pv.n_heads; base += kPlanThreads) {
+        const int head = base + tid;
+        KeepJob job{-1, 0, 0, 0};
+        int need = 0;
+        if (head < pv.n_heads) {
+            const int begin = min(max(cu_b[head], 0), total_rows), rows = max(min(cu_b[head + 1], total_rows) - begin, 0);
+            job.had = pv.length(head);
+            if (rows < job.had) {
+                job.rows = rows;
+                // Rows come in order, none twice: where row r is index r, the ones before are theirs, too.
+                const int32_t* mine = indices + begin;
+                int lo = 0, hi = rows >> pv.log_p;
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (mine[mid * P - 1] == mid * P - 1) lo = mid;
+                    else hi = mid - 1;
+                }
+                job.same = lo;
+                need = pv.pages_of(rows) - lo;
+            }
+        }
+        int total;
+        job.first = running + exclusive_sum<kPlanThreads>(need, sums, total);
+        running += total;
+        // Heads are served while the free pages last.
+        if (job.first + need <= n_free) {
+            if (need > 0) atomicMax(&served_pages, job.first + need);
+        } else if (need > 0) {
+            job.rows = -1;
+            atomicAdd(&lost, 1);
+        }
+        if (head < pv.n_heads) a.jobs[head] = job;
+    }
+    __syncthreads();
+    const int want = served_pages;
+    int next;
+    const int have = find_pages<kPlanThreads>(pv, want, a.found, sums, next);
+    __syncthreads();
+    if (tid == 0) {
+        pv.state[0] = really_free - have;
+        pv.state[1] = next;
+        if (refused) *refused = lost;
+    }
+}
+
+// The kept rows into the new pages: consecutive rows to a workgroup, D / 32 lanes a row, each a block's codes and scale of K and V.
+// A workgroup's rows are in new pages or in pages that stay row by row; the latter have nothing to do.
+template <int D>
+__global__ __launch_bounds__(kThreads) void keep_move_kernel(PageView pv, const int32_t* __restrict__ indices,
+                                                             const int32_t* __restrict__ cu_b, long long first_row,
+                                                             long long total_rows, KeepSpace a)
+{
+    constexpr int LANES = D / 32, ROWS = kThreads / LANES;
+    const int lane = threadIdx.x % LANES;
+    const long long row0 = first_row + (long long)blockIdx.x * ROWS;
+    const long long r = row0 + threadIdx.x / LANES;
+    int head = owner_of_row(cu_b, pv.n_heads, 1, row0);
+    const long long rc = min(r, total_rows - 1);
+    while (head + 1 < pv.n_heads && cu_b[head + 1] <= rc) ++head;
+    const KeepJob job = a.jobs[head];
+    const int t = (int)(rc - cu_b[head]), slot = t >> pv.log_p;
+    if (r >= total_rows || t < 0 || t >= job.rows || slot < job.same) return;
+    const int at = min(max(indices[rc], 0), job.had - 1);              // an index outside is a caller error; cut
+    const int from = pv.table[(size_t)head * pv.width + (at >> pv.log_p)], to = a.found[job.first + slot - job.same];
+    if (!pv.is_page(from) || !pv.is_page(to)) return;
+    const int src = at & (pv.rows() - 1), dst = t & (pv.rows() - 1);
+    const char* s = pv.page(from);
+    char* d = pv.page(to);
+    *reinterpret_cast<u32x4*>(d + pv.k_codes(dst) + lane * 16) = *reinterpret_cast<const u32x4*>(s + pv.k_codes(src) + lane * 16);
+    *reinterpret_cast<u32x4*>(d + pv.v_codes(dst) + lane * 16) = *reinterpret_cast<const u32x4*>(s + pv.v_codes(src) + lane * 16);
+    d[pv.k_scales(dst) + lane] = s[pv.k_scales(src) + lane];
+    d[pv.v_scales(dst) + lane] = s[pv.v_scales(src) + lane];
+}
+
+__global__ __launch_bounds__(kThreads) void keep_table_kernel(PageView pv, KeepSpace a)
+{
+    const int head = blockIdx.x;
+    const KeepJob job = a.jobs[head];
+    if (job.rows < 0) return;
+    int32_t* mine = pv.table + (size_t)head * pv.width;
+    const int had = pv.pages_of(job.had), has = pv.pages_of(job.rows);
+    int freed = 0;
+    for (int j = job.same + threadIdx.x; j < had; j += kThreads) {
+        const int page = mine[j];
+        if (pv.is_page(page)) freed += atomicSub(&pv.refs[page], 1) == 1;
+        if (j < has) {
+            const int now = a.found[job.first + j - job.same];
+            mine[j] = now;
+            if (pv.is_page(now)) pv.refs[now] = 1;
+        }
+    }
+    if (threadIdx.x == 0) pv.lengths[head] = job.rows;
+    freed = wave_incl(freed);
+    if ((threadIdx.x & 63) == 63 && freed > 0) atomicAdd(&pv.state[0], freed);
+}
+
+}  // namespace
+
+size_t pages_fork_bytes(const PageView& pv) {
+    size_t bytes;
+    fork_space(pv, nullptr, &bytes);
+    return bytes;
+}
+
+hipError_t launch_pages_fork(const PageView& pv, const int32_t* parents, const int32_t* drop, void* workspace, hipStream_t s)
+{
+    const ForkSpace f = fork_space(pv, workspace, nullptr);
+    const int n_seqs = pv.n_heads / pv.H;
+    hipLaunchKernelGGL(fork_take_kernel, dim3(pv.n_heads), dim3(kThreads), 0, s, pv, parents, drop, n_seqs, f);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(fork_give_kernel, dim3(pv.n_heads), dim3(kThreads), 0, s, pv, parents, n_seqs, f);
+    return hipGetLastError();
+}
+
+size_t pages_keep_bytes(const PageView& pv, long long total_rows) {
+    size_t bytes;
+    keep_space(pv, total_rows, nullptr, &bytes);
+    return bytes;
+}
+
+hipError_t launch_pages_keep(const PageView& pv, const int32_t* indices, const int32_t* cu_budgets, long long total_rows,
+                             int32_t* refused, void* workspace, hipStream_t s)
+{
+    const KeepSpace a = keep_space(pv, total_rows, workspace, nullptr);
+    hipLaunchKernelGGL(keep_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, pv, indices, cu_budgets, (int)total_rows, a, refused);
+    hipError_t e = hipGetLastError();
+    const int rows_per_block = kThreads / (pv.D / 32);
+    const long long slab = (long long)rows_per_block << 22;
+    for (long long first = 0; first < total_rows && e == hipSuccess; first += slab) {
+        const long long rows = total_rows - first < slab ? total_rows - first : slab;
+        const dim3 grid((unsigned)((rows + rows_per_block - 1) / rows_per_block));
+        AUDIOKV_FOR_DIM(pv.D, hipLaunchKernelGGL(keep_move_kernel<kD>, grid, dim3(kThreads), 0, s, pv, indices, cu_budgets, first,
+                                                 total_rows, a))
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(keep_table_kernel, dim3(pv.n_heads), dim3(kThreads), 0, s, pv, a);
+    return hipGetLastError();
+}
+
+}  // namespace audiokv
