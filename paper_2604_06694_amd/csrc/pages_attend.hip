@@ -42,73 +42,82 @@ template <int D> __device__ __forceinline__ constexpr int channel_of(int s, int 
 
 template <int D> struct Rows32 {         // one unit on its way: what a lane holds of it
     static constexpr int KW = D / 32;    // dwords of K's codes per tile of 16 rows
-    unsigned k[2][KW], ks[2], v[8][(D + 127) / 128], vs[8];
+    static constexpr int VS = D == 64 ? 4 : 8;      // dwords with the scales of its eight rows of V (two rows in one at D = 64)
+    unsigned k[2][KW], ks[2], v[8][(D + 127) / 128], vs[VS];
 };
 
 __device__ __forceinline__ float exponent_of(unsigned word, int byte) {     // 2^(e - 127) of a byte (the conversions read no other bits)
     return __uint_as_float(__builtin_amdgcn_alignbit(word, word, (9 + 8 * byte) & 31));
 }
 
+// Where a lane's share of a unit lies behind the unit's first row in each section: the same for all units, so that a load's address is
+// a scalar (page, section, row) and one of these, with the tile and the row in the instruction.
+template <int D> struct LaneOffsets {
+    unsigned k, ks, v, vs;
+    __device__ __forceinline__ LaneOffsets() {
+        const unsigned lane = threadIdx.x & 63, c = lane & 15, r = lane >> 4;
+        k = c * (D / 2) + r * (D == 64 ? 8 : 16);
+        ks = c * (D / 32) + (D == 64 ? r >> 1 : r);
+        v = r * 4 * (D / 2) + c * (D / 32);
+        vs = r * 4 * (D / 32) + (D == 256 ? (c >> 3) * 4 : 0);
+    }
+};
+
+template <class T> __device__ __forceinline__ T at(const char* base, unsigned lane_offset, int offset) {
+    return *reinterpret_cast<const T*>(base + offset + lane_offset);
+}
+
 template <int D>
-__device__ __forceinline__ void load_unit(Rows32<D>& u, const PageView& pv, int page, int row0) {
-    const int lane = threadIdx.x & 63, c = lane & 15, r = lane >> 4;
+__device__ __forceinline__ void load_unit(Rows32<D>& u, const PageView& pv, const LaneOffsets<D>& of, int page, int row0) {
     const char* base = pv.page(page);
+    const char *k = base + pv.k_codes(row0), *v = base + pv.v_codes(row0), *ks = base + pv.k_scales(row0), *vs = base + pv.v_scales(row0);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int row = row0 + t * 16 + c;
-        const char* k = base + pv.k_codes(row);
-        const unsigned char* e = reinterpret_cast<const unsigned char*>(base + pv.k_scales(row));
         if constexpr (D == 64) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(k + r * 8);
+            const u32x2 w = at<u32x2>(k, of.k, t * 16 * (D / 2));
             u.k[t][0] = w[0];
             u.k[t][1] = w[1];
-            u.ks[t] = e[r >> 1];
         } else {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(k + r * 16);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u.k[t][i] = w[i];
-            u.ks[t] = e[r];
-            if constexpr (D == 256) {
-                const u32x4 w2 = *reinterpret_cast<const u32x4*>(k + 64 + r * 16);
+            for (int b = 0; b < D / 128; ++b) {
+                const u32x4 w = at<u32x4>(k, of.k, t * 16 * (D / 2) + b * 64);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) u.k[t][4 + i] = w2[i];
-                u.ks[t] |= (unsigned)e[4 + r] << 8;
+                for (int i = 0; i < 4; ++i) u.k[t][b * 4 + i] = w[i];
             }
         }
+        u.ks[t] = at<unsigned char>(ks, of.ks, t * 16 * (D / 32));
+        if constexpr (D == 256) u.ks[t] |= (unsigned)at<unsigned char>(ks, of.ks, t * 16 * (D / 32) + 4) << 8;
     }
     // V: rows 4 r + i of either tile, channels c * D / 16 ..
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = row0 + t * 16 + r * 4 + i, n = t * 4 + i;
-            const char* v = base + pv.v_codes(row) + c * (D / 32);
-            if constexpr (D == 64) u.v[n][0] = *reinterpret_cast<const unsigned short*>(v);
-            else if constexpr (D == 128) u.v[n][0] = *reinterpret_cast<const unsigned*>(v);
-            else {
-                const u32x2 w = *reinterpret_cast<const u32x2*>(v);
-                u.v[n][0] = w[0];
-                u.v[n][1] = w[1];
-            }
+    for (int n = 0; n < 8; ++n) {
+        const int row = (n >> 2) * 16 + (n & 3);
+        if constexpr (D == 64) u.v[n][0] = at<unsigned short>(v, of.v, row * (D / 2));
+        else if constexpr (D == 128) u.v[n][0] = at<unsigned>(v, of.v, row * (D / 2));
+        else {
+            const u32x2 w = at<u32x2>(v, of.v, row * (D / 2));
+            u.v[n][0] = w[0];
+            u.v[n][1] = w[1];
         }
-    const char* e = base + pv.v_scales(row0 + r * 4);
+        if constexpr (D == 256) u.vs[n] = at<unsigned>(vs, of.vs, row * (D / 32));
+    }
+    if constexpr (D == 128) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        if constexpr (D == 128) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(e + t * 64);
+        for (int t = 0; t < 2; ++t) {
+            const u32x4 w = at<u32x4>(vs, of.vs, t * 64);
 #pragma unroll
             for (int i = 0; i < 4; ++i) u.vs[t * 4 + i] = w[i];
-        } else if constexpr (D == 64) {                                       // two rows to a dword
-            const u32x2 w = *reinterpret_cast<const u32x2*>(e + t * 32);
+        }
+    } else if constexpr (D == 64) {                                           // two rows to a dword
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u.vs[t * 4 + i] = w[i >> 1];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) u.vs[t * 4 + i] = *reinterpret_cast<const unsigned*>(e + t * 128 + i * 8 + (c >> 3) * 4);
+        for (int t = 0; t < 2; ++t) {
+            const u32x2 w = at<u32x2>(vs, of.vs, t * 32);
+            u.vs[t * 2] = w[0];
+            u.vs[t * 2 + 1] = w[1];
         }
     }
 }
-// which byte of u.vs[n] is the scale of the lane's channels of V
+// which byte of the dword is the scale of the lane's channels of V in its row n
 template <int D> __device__ __forceinline__ int scale_byte(int n, int c) {
     return D == 64 ? (n & 1) * 2 + (c >> 3) : D == 128 ? c >> 2 : (c >> 1) & 3;
 }
@@ -142,33 +151,31 @@ template <int D> struct Running {
 template <int D>
 __device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, const bf16x8 (&q)[D / 32], float c_log2, int rows) {
     const int lane = threadIdx.x & 63, c = lane & 15, r = lane >> 4;
-    float z[8];
+    f32x4 z[2];                                            // products, keys 4 r + i of either tile
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        z[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) {
             const float scale = __uint_as_float(D == 256 && s >= 4 ? u.ks[t] << 15 : u.ks[t] << 23);
             u32x4_t f;
 #pragma unroll
             for (int b = 0; b < 4; ++b) f[b] = pair_of(u.k[t][s], scale, b);
-            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), q[s], acc, 0, 0, 0);
+            z[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, f), q[s], z[t], 0, 0, 0);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) z[t * 4 + i] = acc[i] * c_log2;
     }
-    unsigned vs[8];
+    float vs[8];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) vs[n] = u.vs[n];
+    for (int n = 0; n < 8; ++n) vs[n] = exponent_of(u.vs[D == 64 ? n >> 1 : n], scale_byte<D>(n, c));
     if (rows < kUnit) {                                    // wave-uniform: a head's last unit
 #pragma unroll
         for (int n = 0; n < 8; ++n) {
             const bool there = (n >> 2) * 16 + r * 4 + (n & 3) < rows;
-            z[n] = there ? z[n] : -INFINITY;
-            vs[n] = there ? vs[n] : 0x7f7f7f7f;            // what lies behind the last row may say NaN, which zero times is NaN
+            z[n >> 2][n & 3] = there ? z[n >> 2][n & 3] : -INFINITY;
+            vs[n] = there ? vs[n] : 1.f;                   // what lies behind the last row may say NaN, which zero times is NaN
         }
     }
-    float top = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
+    float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3]))) * c_log2;
     if (__builtin_amdgcn_ballot_w64(top > o.ref + kSlack) != 0) {
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
@@ -183,7 +190,7 @@ __device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, cons
     u32x4_t hi, lo;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float a = __builtin_amdgcn_exp2f(z[2 * i] - ref), b = __builtin_amdgcn_exp2f(z[2 * i + 1] - ref);
+        const float a = __builtin_amdgcn_exp2f(fmaf(z[i >> 1][2 * i & 3], c_log2, -ref)), b = __builtin_amdgcn_exp2f(fmaf(z[i >> 1][(2 * i & 3) + 1], c_log2, -ref));
         o.sum += a + b;
         hi[i] = pack_bf16(a, b);
         lo[i] = pack_bf16(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xffff0000u));
@@ -195,8 +202,7 @@ __device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, cons
             u32x4_t even, odd;                             // channels 8 w + 2 b and 2 b + 1 of the lane's, keys by twos
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const unsigned x = pair_of(u.v[2 * i][w], exponent_of(vs[2 * i], scale_byte<D>(2 * i, c)), b);
-                const unsigned y = pair_of(u.v[2 * i + 1][w], exponent_of(vs[2 * i + 1], scale_byte<D>(2 * i + 1, c)), b);
+                const unsigned x = pair_of(u.v[2 * i][w], vs[2 * i], b), y = pair_of(u.v[2 * i + 1][w], vs[2 * i + 1], b);
                 even[i] = __builtin_amdgcn_perm(y, x, 0x05040100);
                 odd[i] = __builtin_amdgcn_perm(y, x, 0x07060302);
             }
@@ -220,21 +226,26 @@ __device__ __forceinline__ int next_with_rows(const PageView& pv, int head) {
 
 __device__ __forceinline__ int units_of(int rows) { return (rows + kUnit - 1) / kUnit; }
 
-// first unit of workgroup w, and the workgroup that has a unit
-__device__ __forceinline__ long long first_unit(long long units, int w, int W) { return units * w / W; }
-__device__ __forceinline__ int workgroup_of(long long units, long long u, int W) { return (int)(((u + 1) * W - 1) / units); }
+// First unit of workgroup w, and the workgroup that has unit u. In float64, where both are exact: numerators are below 2^42, and a quotient
+// that is no whole number is at least 2^-31 away from one. (Divisions of 64-bit integers took 130 instructions each.)
+__device__ __forceinline__ int first_unit(int units, int w, int W) { return (int)((double)units * w / W); }
+__device__ __forceinline__ int workgroup_of(int units, int u, int W) { return (int)((((double)u + 1) * W - 1) / units); }
 
 // dynamic LDS: [wave][G][D + 4]
+// waves of a SIMD: what two units on their way leave registers for
+template <int D> constexpr int kResident = D == 64 ? 4 : D == 128 ? 3 : 2;
+
 template <int D>
-__global__ __launch_bounds__(kThreads) void attend_kernel(Geom g, PageView pv, const __bf16* __restrict__ q, __bf16* __restrict__ out,
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kResident<D>, kResident<D>))) void attend_kernel(Geom g, PageView pv, const __bf16* __restrict__ q, __bf16* __restrict__ out,
                                                           float* __restrict__ lse, AttendSpace a)
 {
     extern __shared__ __attribute__((aligned(16))) float merge[];
     __shared__ int sums[kWaves];
     __shared__ float ref_of[kWaves][16], sum_of[kWaves][16];
-    __shared__ int begin_head, begin_unit;
+    __shared__ int begin_head, begin_unit, begin_rows;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, r = lane >> 4;
     const int G = g.G, PITCH = D + 4;
+    const LaneOffsets<D> offsets;
 
     // all units, and where this workgroup's first one is
     const int each = (pv.n_heads + kThreads - 1) / kThreads, h0 = min(tid * each, pv.n_heads), h1 = min(h0 + each, pv.n_heads);
@@ -244,22 +255,24 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(Geom g, PageView pv, c
     const int before = exclusive_sum<kThreads>(mine, sums, total);
     const int W = min((int)gridDim.x, max(1, (total + kWaves - 1) / kWaves));
     if ((int)blockIdx.x >= W || total == 0) return;
-    const int u0 = (int)first_unit(total, blockIdx.x, W), u1 = (int)first_unit(total, blockIdx.x + 1, W);
+    const int u0 = __builtin_amdgcn_readfirstlane(first_unit(total, blockIdx.x, W));
+    const int u1 = __builtin_amdgcn_readfirstlane(first_unit(total, blockIdx.x + 1, W));
     if (mine > 0 && u0 >= before && u0 < before + mine) {
-        int h = h0, at = before;
-        for (;; ++h) {
-            const int n = units_of(pv.length(h));
-            if (u0 < at + n) break;
-            at += n;
+        int h = h0, at = before, rows = pv.length(h0);
+        while (u0 >= at + units_of(rows)) {
+            at += units_of(rows);
+            rows = pv.length(++h);
         }
         begin_head = h;
         begin_unit = at;
+        begin_rows = rows;
     }
     __syncthreads();
     int head = __builtin_amdgcn_readfirstlane(begin_head), start = __builtin_amdgcn_readfirstlane(begin_unit);
+    int rows = __builtin_amdgcn_readfirstlane(begin_rows);
 
     for (int u = u0; u < u1;) {
-        const int rows = __builtin_amdgcn_readfirstlane(pv.length(head)), units = units_of(rows);
+        const int units = units_of(rows);
         const int from = u - start, to = min(units, u1 - start);           // units of this head
         const int x = head / g.H_kv, h = head - x * g.H_kv;
         const int32_t* table = pv.table + (size_t)head * pv.width;
@@ -275,14 +288,42 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(Geom g, PageView pv, c
         for (int ct = 0; ct < D / 16; ++ct) o.out[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
         o.ref = -INFINITY;
         o.sum = 0.f;
-        for (int i = from + wave; i < to; i += kWaves) {
-            const int page = __builtin_amdgcn_readfirstlane(table[i >> log_u]);
-            const bool good = pv.is_page(page);                            // (rows of none take no part)
-            Rows32<D> unit;
-            load_unit<D>(unit, pv, good ? page : 0, (i & ((1 << log_u) - 1)) * kUnit);
-            add_unit<D>(o, unit, qf, g.c_log2, good ? min(kUnit, rows - i * kUnit) : 0);
+        // Two units on their way: while one is worked on, the next is loaded (the last one again behind it, so that every step waits
+        // for as many loads), and the page of the one after that is looked up.
+        if (from + wave < to) {
+            const int last = from + wave + (to - 1 - from - wave) / kWaves * kWaves;
+            auto page_of = [&](int i) { return __builtin_amdgcn_readfirstlane(table[min(i, last) >> log_u]); };
+            auto load = [&](Rows32<D>& unit, int i, int page) {
+                load_unit<D>(unit, pv, offsets, pv.is_page(page) ? page : 0, (min(i, last) & ((1 << log_u) - 1)) * kUnit);
+            };
+            auto add = [&](const Rows32<D>& unit, int i, int page) {       // (rows of no page take no part)
+                add_unit<D>(o, unit, qf, g.c_log2, pv.is_page(page) ? min(kUnit, rows - i * kUnit) : 0);
+            };
+            Rows32<D> a0, a1;
+            int i = from + wave, p0 = page_of(i), p1 = page_of(i + kWaves);
+            load(a0, i, p0);
+            for (;;) {
+                int p2 = page_of(i + 2 * kWaves);
+                load(a1, i + kWaves, p1);
+                __builtin_amdgcn_sched_barrier(0);
+                add(a0, i, p0);
+                i += kWaves;
+                if (i > last) break;
+                p0 = page_of(i + 2 * kWaves);
+                load(a0, i + kWaves, p2);
+                __builtin_amdgcn_sched_barrier(0);
+                add(a1, i, p1);
+                i += kWaves;
+                if (i > last) break;
+                p1 = p0;
+                p0 = p2;
+            }
         }
-        // the four waves' findings
+        // The four waves' findings. (The thread's number goes through an asm, so that no address below is worked out ahead of the loop
+        // and held in registers during it.)
+        int me = tid;
+        asm volatile("" : "+v"(me));
+        const int c = me & 15, r = (me & 63) >> 4;
         float sum = o.sum;
         sum += __shfl_xor(sum, 16, 64);
         sum += __shfl_xor(sum, 32, 64);
@@ -304,7 +345,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(Geom g, PageView pv, c
         __syncthreads();
         const bool whole = from == 0 && to == units;
         const int slot = 2 * blockIdx.x + (u != u0);
-        if (tid == 0) {
+        if (me == 0) {
             if (whole) a.heads[head] = int2{0, 0};
             else if (from == 0) a.heads[head] = int2{slot, workgroup_of(total, start + units - 1, W) - (int)blockIdx.x + 1};
         }
@@ -315,7 +356,7 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(Geom g, PageView pv, c
             for (int w = 0; w < kWaves; ++w) l += sum_of[w][n] * (ref_of[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref_of[w][n] - m));   // (NaN stays NaN)
             return l;
         };
-        for (int e = tid * 4; e < G * D; e += kThreads * 4) {
+        for (int e = me * 4; e < G * D; e += kThreads * 4) {
             const int n = e / D, ch = e % D;
             f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -329,64 +370,84 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(Geom g, PageView pv, c
                 *reinterpret_cast<f32x4*>(a.parts + ((size_t)slot * G + n) * D + ch) = v;
             }
         }
-        if (tid < G) {
+        if (me < G) {
             float m;
-            const float l = sums_of(tid, m);
+            const float l = sums_of(me, m);
             if (!whole) {
-                a.stats[((size_t)slot * G + tid) * 2] = m;
-                a.stats[((size_t)slot * G + tid) * 2 + 1] = l;
+                a.stats[((size_t)slot * G + me) * 2] = m;
+                a.stats[((size_t)slot * G + me) * 2 + 1] = l;
             } else if (lse) {
-                lse[(size_t)x * g.H_q + (size_t)h * G + tid] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+                lse[(size_t)x * g.H_q + (size_t)h * G + me] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
             }
         }
         u = start + to;
         start += units;
-        if (u < u1) head = next_with_rows(pv, head + 1);
+        if (u < u1) {
+            head = next_with_rows(pv, head + 1);
+            rows = __builtin_amdgcn_readfirstlane(pv.length(head));
+        }
         __syncthreads();                                                   // the LDS is free again
     }
 }
 
-// One workgroup per query head: the parts of its KV head, in order. A head without rows gives zeros.
+// One workgroup per query head: the parts of its KV head, in order. A head without rows gives zeros. A chain of loads from end to end:
+// the first parts are on their way with the statistics.
+constexpr int kMaxWorkgroups = 256 * 4, kEarly = 2;
+
 template <int D>
 __global__ __launch_bounds__(kThreads) void join_kernel(Geom g, PageView pv, __bf16* __restrict__ out, float* __restrict__ lse, AttendSpace a)
 {
-    constexpr int QUADS = D / 4, GROUPS = kThreads / QUADS;                // threads on four channels each, parts at a time
+    constexpr int QUADS = D / 4, GROUPS = kThreads / QUADS, WAVES = kThreads / 64;     // threads on four channels each, parts at a time
     const int G = g.G, head = blockIdx.x / G, n = blockIdx.x - head * G, tid = threadIdx.x;
     const int x = head / g.H_kv, h = head - x * g.H_kv;
     const size_t row = (size_t)x * g.H_q + (size_t)h * G + n;
+    const int2 from = a.heads[head];
     if (pv.length(head) == 0) {
         if (tid < QUADS) *reinterpret_cast<u32x2*>(out + row * D + tid * 4) = u32x2{0, 0};
         if (lse && tid == 0) lse[row] = -INFINITY;
         return;
     }
-    const int2 from = a.heads[head];
-    if (from.y == 0) return;
-    __shared__ float wave_m[kThreads / 64], wave_l[kThreads / 64];
+    const int parts = min(from.y, kMaxWorkgroups);
+    if (parts == 0) return;
+    __shared__ float weight[kMaxWorkgroups], wave_m[WAVES], wave_l[WAVES];
     __shared__ __attribute__((aligned(16))) f32x4 red[kThreads];
     // part p of the head: the first where the head began, the others the first of the workgroups behind
     auto slot_of = [&](int p) { return p == 0 ? from.x : (from.x & ~1) + 2 * p; };
-    auto stat = [&](int p) { return *reinterpret_cast<const float2*>(&a.stats[((size_t)slot_of(p) * G + n) * 2]); };
+    const int ch = tid % QUADS * 4, grp = tid / QUADS;
+    auto part = [&](int p) { return *reinterpret_cast<const f32x4*>(a.parts + ((size_t)slot_of(p) * G + n) * D + ch); };
+    f32x4 early[kEarly];
+#pragma unroll
+    for (int u = 0; u < kEarly; ++u) early[u] = part(min(grp + u * GROUPS, parts - 1));
+    float2 stat[kMaxWorkgroups / kThreads];
     float m = -INFINITY;
-    for (int p = tid; p < from.y; p += kThreads) m = fmaxf(m, stat(p).x);
+#pragma unroll
+    for (int u = 0; u < kMaxWorkgroups / kThreads; ++u) {
+        stat[u] = float2{-INFINITY, 0.f};
+        if (tid + u * kThreads < parts) stat[u] = *reinterpret_cast<const float2*>(&a.stats[((size_t)slot_of(tid + u * kThreads) * G + n) * 2]);
+        m = fmaxf(m, stat[u].x);
+    }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
     if ((tid & 63) == 0) wave_m[tid >> 6] = m;
     __syncthreads();
     m = fmaxf(fmaxf(wave_m[0], wave_m[1]), fmaxf(wave_m[2], wave_m[3]));
-    auto weight = [&](float ref) { return ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref - m); };
     float l = 0.f;
-    for (int p = tid; p < from.y; p += kThreads) {
-        const float2 s = stat(p);
-        l += weight(s.x) * s.y;
+#pragma unroll
+    for (int u = 0; u < kMaxWorkgroups / kThreads; ++u) {
+        const float w = stat[u].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(stat[u].x - m);
+        if (tid + u * kThreads < parts) weight[tid + u * kThreads] = w;
+        l += w * stat[u].y;
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) l += __shfl_xor(l, o, 64);
     if ((tid & 63) == 0) wave_l[tid >> 6] = l;
-    const int ch = tid % QUADS * 4, grp = tid / QUADS;
+    __syncthreads();
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < kEarly; ++u)
+        if (grp + u * GROUPS < parts) acc += early[u] * weight[grp + u * GROUPS];
 #pragma unroll 4
-    for (int p = grp; p < from.y; p += GROUPS)
-        acc += *reinterpret_cast<const f32x4*>(a.parts + ((size_t)slot_of(p) * G + n) * D + ch) * weight(stat(p).x);
+    for (int p = grp + kEarly * GROUPS; p < parts; p += GROUPS) acc += part(p) * weight[p];
     red[tid] = acc;
     __syncthreads();
     l = ((wave_l[0] + wave_l[1]) + wave_l[2]) + wave_l[3];
@@ -401,7 +462,8 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Geom g, PageView pv, __b
 // Workgroups: as many as the registers let run at once, so that equal shares end together
 int workgroups(const Geom& g, const PageView& pv) {
     const long long most = ((long long)pv.n_heads * pv.width << pv.log_p) / (kUnit * kWaves) + pv.n_heads;
-    const int w = 256 * (g.D == 256 ? 2 : 4);
+    const int w = 256 * (g.D == 64 ? kResident<64> : g.D == 128 ? kResident<128> : kResident<256>);
+    static_assert(256 * kResident<64> <= kMaxWorkgroups, "join_kernel holds the statistics of as many parts");
     return (int)(most < w ? most : w);
 }
 
