@@ -742,19 +742,21 @@ def pages_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, seql
     sequence i. `refused` (int32, one value) becomes the number of heads that there were no pages for."""
     at = _device()
     cg = pages._c(p, at)
-    n_seqs, n_items, heads = pages.n_seqs(p), len(seqlens), len(seqlens) * p.n_kv_heads
+    n_seqs, n_items, heads, lens = pages.n_seqs(p), len(seqlens), len(seqlens) * p.n_kv_heads, _host_lens(seqlens)
     _need_at(k, _BF16, at, "k"); _need_at(v, _BF16, at, "v")
-    if min(_room(p, k), _room(p, v)) < _rows_end(p, seqlens):
-        raise ValueError(f"k or v has room for {min(_room(p, k), _room(p, v))} values, {_rows_end(p, seqlens)} needed")
+    rows = sum(lens) * p.n_kv_heads
+    end = rows * p.head_dim if p.kv_stride_tok == 0 else _rows_end(p, seqlens)
+    if _room(p, k) < end or _room(p, v) < end:
+        raise ValueError(f"k or v has room for {min(_room(p, k), _room(p, v))} values, {end} needed")
     _table(cu_seqlens, n_items, at, "cu_seqlens"); _table(cu_budgets, heads, at, "cu_budgets")
     if indices is None:
-        total_rows = sum(int(x) for x in seqlens) * p.n_kv_heads
+        total_rows = rows
     idx, to, no = (_values(indices, total_rows, _I32, at, "indices"), _values(seqs, n_items, _I32, at, "seqs"),
                    _values(refused, 1, _I32, at, "refused"))
     ws = _workspace_of(workspace, at, lambda: pages_append_workspace_bytes(p, pages, n_items, total_rows))
     cu = cu_seqlens if cu_seqlens is not None else _cu(seqlens, k.device)
     _check(_lib.audiokv_pages_append(C.byref(p.c()), C.byref(cg), n_seqs, k.data_ptr(), v.data_ptr(), idx, _ptr(cu_budgets),
-                                     int(total_rows), cu.data_ptr(), _host_lens(seqlens), n_items, to, no, ws.data_ptr(), ws.nbytes,
+                                     int(total_rows), cu.data_ptr(), lens, n_items, to, no, ws.data_ptr(), ws.nbytes,
                                      _stream()))
 
 

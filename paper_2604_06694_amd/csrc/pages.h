@@ -78,54 +78,72 @@ __device__ __forceinline__ int exclusive_sum(int x, int* sums, int& total) {
 }
 
 // What append and keep plan on the device, by one workgroup: which pages the heads get.
-// The first `want` pages with refs 0 from state[1] upwards and round, in that order, to found[]. Returns how many there were, and in
-// `next` where the following search begins. (sums: (4 * THREADS / 64) ints of LDS)
-template <int THREADS>
-__device__ int find_pages(const PageView& pv, int want, int32_t* __restrict__ found, int* sums, int& next) {
-    constexpr int U = 4, WAVES = THREADS / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int begin = min(max(pv.state[1], 0), pv.n_pages - 1);
-    int have = 0;
-    next = begin;
-    __shared__ int last;
-    for (int base = 0; base < pv.n_pages && have < want; base += THREADS * U) {
-        int page[U];
-        unsigned long long free_in[U];
+//
+// A round of the search for pages with refs 0 looks at U * THREADS of them, a wave at U * 64 in a row, and begins at state[1]. The first
+// round's counts are loaded ahead (PageSearch), since where it begins is known before how many are wanted.
+template <int THREADS, int U>
+struct PageSearch {
+    int begin, page[U];
+    bool free[U];
+
+    __device__ __forceinline__ void load(const PageView& pv, int base) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const long long i = (long long)base + u * THREADS + threadIdx.x;
+            const long long i = (long long)base + ((threadIdx.x >> 6) * U + u) * 64 + (threadIdx.x & 63);
             long long p = begin + i;
             if (p >= pv.n_pages) p -= pv.n_pages;
-            page[u] = (int)p;
-            free_in[u] = __builtin_amdgcn_ballot_w64(i < pv.n_pages && pv.refs[min(p, (long long)pv.n_pages - 1)] == 0);
+            page[u] = (int)min(p, (long long)pv.n_pages - 1);
+            free[u] = i < pv.n_pages && pv.refs[page[u]] == 0;
+        }
+    }
+    __device__ __forceinline__ PageSearch(const PageView& pv, int from) : begin(min(max(from, 0), pv.n_pages - 1)) { load(pv, 0); }
+
+    // The first `want` free pages, in the order in which they are looked at, to found[]. Returns how many there were, and in `next`
+    // where the following search begins. sums: THREADS / 64 + 1 ints of LDS. (A barrier before the first and after the last use of LDS.)
+    __device__ int find(const PageView& pv, int want, int32_t* __restrict__ found, int* sums, int& next) {
+        constexpr int WAVES = THREADS / 64;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        int have = 0;
+        for (int base = 0; have < want; ) {
+            unsigned long long free_in[U];
+            int mine = 0;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                free_in[u] = __builtin_amdgcn_ballot_w64(free[u]);
+                mine += __builtin_popcountll(free_in[u]);
+            }
+            __syncthreads();
+            if (lane == 0) sums[wave] = mine;
+            __syncthreads();
+            int at = have, total = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) {
+                const int n = sums[w];
+                at += w < wave ? n : 0;
+                total += n;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int to = at + __builtin_popcountll(free_in[u] & ((1ull << lane) - 1));
+                if (free[u] && to < want) {
+                    found[to] = page[u];
+                    if (to == want - 1) sums[WAVES] = page[u];
+                }
+                at += __builtin_popcountll(free_in[u]);
+            }
+            have += total;
+            if (pv.n_pages - base <= THREADS * U) break;
+            base += THREADS * U;
+            if (have < want) load(pv, base);
         }
         __syncthreads();
-        if (lane == 0)
-#pragma unroll
-            for (int u = 0; u < U; ++u) sums[u * WAVES + wave] = __builtin_popcountll(free_in[u]);
-        __syncthreads();
-        int before = have;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            for (int w = 0; w < WAVES; ++w) {
-                if (w == wave) {
-                    const int at = before + __builtin_popcountll(free_in[u] & ((1ull << lane) - 1));
-                    if ((free_in[u] >> lane & 1) && at < want) {
-                        found[at] = page[u];
-                        if (at == want - 1) last = page[u];
-                    }
-                }
-                before += sums[u * WAVES + w];
-            }
-        have = before;
+        next = begin;
+        // (fewer than wanted: the state said that there were more. The next search begins where this one did)
+        if (want > 0 && have >= want) next = sums[WAVES] + 1 == pv.n_pages ? 0 : sums[WAVES] + 1;
+        for (int i = have + threadIdx.x; i < want; i += THREADS) found[i] = -1;
+        return min(have, want);
     }
-    have = min(have, want);
-    __syncthreads();
-    // (fewer than wanted: the state said that there were more. The search ends where it began)
-    if (want > 0 && have == want) next = last + 1 == pv.n_pages ? 0 : last + 1;
-    for (int i = have + threadIdx.x; i < want; i += THREADS) found[i] = -1;
-    return have;
-}
+};
 
 inline size_t up256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }    // parts of a workspace begin at multiples of 256 bytes
 

@@ -74,6 +74,47 @@ __global__ __launch_bounds__(kThreads) void fork_give_kernel(PageView pv, const 
     if ((threadIdx.x & 63) == 63 && freed > 0) atomicAdd(&pv.state[0], freed);
 }
 
+// Both for small tables, U entries a thread of one workgroup: what the first launch lists is in registers here.
+constexpr int kForkEntries = 4;       // 4096 entries: 16 heads of 17 pages 3.6 + 3.4 us by the two kernels, 4.6 by this one
+
+__global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageView pv, const int32_t* __restrict__ parents,
+                                                                  const int32_t* __restrict__ drop, int n_seqs)
+{
+    const int entries = pv.n_heads * pv.width;
+    int rows[kForkEntries], was[kForkEntries], before[kForkEntries], now[kForkEntries];
+#pragma unroll
+    for (int u = 0; u < kForkEntries; ++u) {
+        const int e = min((int)threadIdx.x + u * kPlanThreads, entries - 1), head = e / pv.width, j = e - head * pv.width;
+        const int x = head / pv.H, h = head - x * pv.H;
+        const int parent = parents ? parents[x] : x;
+        const bool taken = (unsigned)parent < (unsigned)n_seqs;
+        const int from = taken ? parent * pv.H + h : head;
+        was[u] = pv.length(head);
+        rows[u] = taken ? max(pv.length(from) - (drop ? max(drop[x], 0) : 0), 0) : 0;
+        const int mine = pv.table[e], theirs = pv.table[(size_t)from * pv.width + j];
+        before[u] = j < pv.pages_of(was[u]) ? mine : -1;
+        now[u] = j < pv.pages_of(rows[u]) ? theirs : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kForkEntries; ++u)
+        if ((int)threadIdx.x + u * kPlanThreads < entries && now[u] != before[u] && pv.is_page(now[u])) atomicAdd(&pv.refs[now[u]], 1);
+    __syncthreads();          // all new owners are counted, and all of the table is read
+    int freed = 0;
+#pragma unroll
+    for (int u = 0; u < kForkEntries; ++u) {
+        const int e = threadIdx.x + u * kPlanThreads;
+        if (e >= entries) break;
+        const int head = e / pv.width, j = e - head * pv.width;
+        if (now[u] != before[u]) {
+            if (pv.is_page(before[u])) freed += atomicSub(&pv.refs[before[u]], 1) == 1;
+            if (j < pv.pages_of(rows[u])) pv.table[e] = now[u];
+        }
+        if (j == 0 && rows[u] != was[u]) pv.lengths[head] = rows[u];
+    }
+    freed = wave_incl(freed);
+    if ((threadIdx.x & 63) == 63 && freed > 0) atomicAdd(&pv.state[0], freed);
+}
+
 // ---- keep --------------------------------------------------------------------------------------------------------------------------
 
 struct KeepJob {
@@ -102,11 +143,12 @@ __global__ __launch_bounds__(kPlanThreads) void keep_plan_kernel(PageView pv, co
                                                                  const int32_t* __restrict__ cu_b, int total_rows, KeepSpace a,
                                                                  int32_t* __restrict__ refused)
 {
-    __shared__ int sums[4 * kPlanThreads / 64];
+    __shared__ int sums[kPlanThreads / 64 + 1];
     __shared__ int served_pages, lost;
     const int tid = threadIdx.x, P = pv.rows();
+    PageSearch<kPlanThreads, 8> search(pv, pv.state[1]);
     if (tid == 0) served_pages = lost = 0;
-    const int n_free = min(max(pv.state[0], 0), a.most), really_free = max(pv.state[0], 0);
+    const int n_free = min(max(pv.state[0], 0), a.most);
     int running = 0;
     for (int base = 0; base < pv.n_heads; base += kPlanThreads) {
         const int head = base + tid;
@@ -144,10 +186,10 @@ __global__ __launch_bounds__(kPlanThreads) void keep_plan_kernel(PageView pv, co
     __syncthreads();
     const int want = served_pages;
     int next;
-    const int have = find_pages<kPlanThreads>(pv, want, a.found, sums, next);
+    const int have = search.find(pv, want, a.found, sums, next);
     __syncthreads();
     if (tid == 0) {
-        pv.state[0] = really_free - have;
+        pv.state[0] -= have;
         pv.state[1] = next;
         if (refused) *refused = lost;
     }
@@ -216,6 +258,10 @@ hipError_t launch_pages_fork(const PageView& pv, const int32_t* parents, const i
 {
     const ForkSpace f = fork_space(pv, workspace, nullptr);
     const int n_seqs = pv.n_heads / pv.H;
+    if ((long long)pv.n_heads * pv.width <= kForkEntries * kPlanThreads) {
+        hipLaunchKernelGGL(fork_small_kernel, dim3(1), dim3(kPlanThreads), 0, s, pv, parents, drop, n_seqs);
+        return hipGetLastError();
+    }
     hipLaunchKernelGGL(fork_take_kernel, dim3(pv.n_heads), dim3(kThreads), 0, s, pv, parents, drop, n_seqs, f);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;

@@ -16,6 +16,7 @@ namespace audiokv {
 namespace {
 
 constexpr int kThreads = 256, kPlanThreads = 1024;
+constexpr long long kStreamBytes = 64LL << 20;      // of bf16 rows that pass the memory-side cache by
 
 struct AppendJob {
     int start, rows;        // where the head's new rows begin, how many (0: nothing to do)
@@ -64,9 +65,10 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(
     PageView pv, const int32_t* __restrict__ cu_b, const int32_t* __restrict__ cu_seq, const int32_t* __restrict__ seqs, int n_items,
     int n_seqs, int total_rows, AppendSpace a, int32_t* __restrict__ refused)
 {
-    __shared__ int sums[4 * kPlanThreads / 64];
+    __shared__ int sums[kPlanThreads / 64 + 1];
     __shared__ int served_pages, lost, freed;
     const int tid = threadIdx.x, H = pv.H, heads = n_items * H;
+    PageSearch<kPlanThreads, 8> search(pv, pv.state[1]);
     if (tid == 0) served_pages = lost = freed = 0;
     for (int i = tid; i < n_items; i += kPlanThreads) a.bad[i] = 0;
     if (seqs) {
@@ -122,7 +124,6 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(
     __syncthreads();
     // Items are served while the free pages last: the ends of their pages do not fall.
     const int n_free = min(max(pv.state[0], 0), a.most);
-    const int really_free = max(pv.state[0], 0);
     auto end_of = [&](int item) { return item + 1 < n_items ? a.jobs[(item + 1) * H].first : running; };
     auto served = [&](int item) {
         const int end = end_of(item);
@@ -133,7 +134,7 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(
     __syncthreads();
     const int want = served_pages;
     int next;
-    const int have = find_pages<kPlanThreads>(pv, want, a.found, sums, next);
+    const int have = search.find(pv, want, a.found, sums, next);
     // lengths, and what shared pages lose: after the search, so that a page which is still to be copied is not handed out
     __syncthreads();
     for (int g = tid; g < heads; g += kPlanThreads) {
@@ -151,7 +152,90 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(
     for (int g = tid; g < heads; g += kPlanThreads)
         if (a.bad[g / H]) a.jobs[g].rows = 0;
     if (tid == 0) {
-        pv.state[0] = really_free - have + freed;
+        pv.state[0] += freed - have;
+        pv.state[1] = next;
+        if (refused) *refused = lost;
+    }
+}
+
+// The same for up to THREADS heads, one a thread, and up to kSmallSeqs sequences: what is a pass over the workspace there is a register
+// or LDS here, and the counts of the first pages that the search looks at are loaded beside the rest. What is left is the chain item ->
+// sequence -> length -> table -> refs and the barriers. (192 heads: 12.2 us by the kernel above, 7.3 so.)
+constexpr int kSmallSeqs = 4096;
+
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void append_plan_small_kernel(
+    PageView pv, const int32_t* __restrict__ cu_b, const int32_t* __restrict__ cu_seq, const int32_t* __restrict__ seqs, int n_items,
+    int n_seqs, int total_rows, AppendSpace a, int32_t* __restrict__ refused)
+{
+    __shared__ int sums[THREADS / 64 + 1], begins[THREADS + 1], bad[THREADS], owner[kSmallSeqs];
+    __shared__ int want, lost;
+    const int tid = threadIdx.x, H = pv.H, heads = n_items * H;
+    const bool mine = tid < heads;
+    const int item = mine ? tid / H : 0, h = tid - item * H;
+    const int state = pv.state[0];
+    int x = mine ? (seqs ? seqs[item] : item) : -1;
+    const int rows = mine ? rows_of(cu_b, cu_seq, H, tid, total_rows) : 0;
+    PageSearch<THREADS, THREADS == 256 ? 4 : 8> search(pv, pv.state[1]);
+    if (tid == 0) want = lost = 0;
+    if (mine) bad[item] = 0;
+    if (seqs) {
+        for (int i = tid; i < n_seqs; i += THREADS) owner[i] = INT_MAX;
+        __syncthreads();
+        const bool is_sequence = (unsigned)x < (unsigned)n_seqs;
+        if (is_sequence && h == 0) atomicMin(&owner[x], item);
+        __syncthreads();
+        x = is_sequence && owner[x] == item ? x : -1;
+    } else {
+        __syncthreads();
+    }
+    const int head = x * H + h;
+    const bool asks = x >= 0 && rows > 0;
+    AppendJob job{0, 0, -1, 0};
+    int need = 0;
+    if (asks) {
+        const int start = pv.length(head);
+        const long long end = (long long)start + rows;
+        if (end > (long long)pv.width << pv.log_p) {
+            bad[item] = 1;
+        } else {
+            int first = pv.pages_of(start);
+            if (start & (pv.rows() - 1)) {
+                const int page = pv.table[(size_t)head * pv.width + (start >> pv.log_p)];
+                if (pv.is_page(page) && pv.refs[page] > 1) {
+                    job.copy_from = page;
+                    --first;
+                }
+            }
+            job.start = start;
+            need = pv.pages_of((int)end) - first;
+        }
+    }
+    __syncthreads();
+    const bool fits = mine && !bad[item];
+    int total;
+    job.first = exclusive_sum<THREADS>(fits ? need : 0, sums, total);
+    begins[tid] = job.first;
+    if (tid == 0) begins[THREADS] = total;
+    __syncthreads();
+    // Items are served while the free pages last: the ends of their pages do not fall.
+    const int n_free = min(max(state, 0), a.most);
+    const int last = (item + 1) * H, end = last < THREADS ? begins[last] : total;
+    const bool served = fits && (end <= n_free || end == begins[item * H]);
+    if (served && need > 0) atomicMax(&want, end);
+    if (asks && !served) atomicAdd(&lost, 1);
+    __syncthreads();
+    int next;
+    const int have = search.find(pv, want, a.found, sums, next);
+    if (asks && served) {
+        job.rows = rows;
+        pv.lengths[head] = job.start + rows;
+        // after the search, so that a page which is still to be copied is not handed out
+        if (job.copy_from >= 0 && atomicSub(&pv.refs[job.copy_from], 1) == 1) atomicAdd(&pv.state[0], 1);
+    }
+    if (mine) a.jobs[tid] = job;
+    if (tid == 0) {
+        if (have > 0) atomicSub(&pv.state[0], have);
         pv.state[1] = next;
         if (refused) *refused = lost;
     }
@@ -180,8 +264,21 @@ __device__ __forceinline__ unsigned round_to_4(u32x4 x, int& scale) {
     return scale == 255 ? 0 : codes;
 }
 
+// What a call reads or writes once, 16 bytes of it. STREAM: more than the memory-side cache should keep.
+template <bool STREAM> __device__ __forceinline__ u32x4 row_piece(const __bf16* p) {
+    return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)) : *reinterpret_cast<const u32x4*>(p);
+}
+
 // Workgroups up to `copies_at` take consecutive rows, D / 8 lanes a row; those behind copy the shared page of a head each.
-template <int D>
+// The scale bytes of 16 lanes' blocks (8 lanes': D = 64) in one word, the first block lowest, in all of them.
+template <int D> __device__ __forceinline__ unsigned scales_of_row(int scale, int lane) {
+    int w = scale << (lane / 4 % (D == 64 ? 2 : 4) * 8);
+    w |= __builtin_amdgcn_update_dpp(0, w, 0x141, 0xf, 0xf, false);                                  // lane 7 - i of eight
+    if constexpr (D > 64) w |= __builtin_amdgcn_update_dpp(0, w, 0x140, 0xf, 0xf, false);            // lane 15 - i of sixteen
+    return (unsigned)w;
+}
+
+template <int D, int R, bool STREAM>
 __global__ __launch_bounds__(kThreads) void append_rows_kernel(
     Geom g, PageView pv, const __bf16* __restrict__ k, const __bf16* __restrict__ v, const int32_t* __restrict__ indices,
     const int32_t* __restrict__ cu_b, const int32_t* __restrict__ cu_seq, const int32_t* __restrict__ seqs, int same_length,
@@ -208,51 +305,74 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(
     }
     const int n_heads = g.n_items * H;
     const int lane = tid % LANES;
-    const long long row0 = first_row + (long long)blockIdx.x * ROWS;
-    const long long r = row0 + tid / LANES;
-    const long long rc = min(r, total_rows - 1);            // a row past the end is the last one again, and not stored
-    int head, t;                                            // head (of items) and its row
-    if (cu_b) {
-        head = owner_of_row(cu_b, n_heads, 1, row0);
-        while (head + 1 < n_heads && cu_b[head + 1] <= rc) ++head;
-        t = (int)(rc - cu_b[head]);
-    } else if (same_length > 0) {
-        head = (int)((unsigned)rc / (unsigned)same_length);                  // (rows are fewer than 2^31)
-        t = (int)((unsigned)rc % (unsigned)same_length);
-    } else {
-        int item = owner_of_row(cu_seq, g.n_items, H, row0);
-        while (item + 1 < g.n_items && (long long)cu_seq[item + 1] * H <= rc) ++item;
-        const int L = max(cu_seq[item + 1] - cu_seq[item], 1);
-        const unsigned in_item = (unsigned)(rc - (long long)cu_seq[item] * H);
-        head = item * H + min((int)(in_item / (unsigned)L), H - 1);
-        t = (int)(in_item % (unsigned)L);
+    const long long row0 = first_row + (long long)blockIdx.x * (ROWS * R);
+    // the head of the workgroup's first row, or its item, is found once; later rows walk forward from there
+    int walk = 0;
+    if (cu_b) walk = owner_of_row(cu_b, n_heads, 1, row0);
+    else if (same_length <= 0) walk = owner_of_row(cu_seq, g.n_items, H, row0);
+    u32x4 kk[R], vv[R];
+    int heads[R], ts[R];                                    // head (of items) and its row; -1: no row
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+        const long long r = row0 + u * ROWS + tid / LANES;
+        const long long rc = min(r, total_rows - 1);        // a row past the end is the last one again, and not stored
+        int head, t;
+        if (cu_b) {
+            while (walk + 1 < n_heads && cu_b[walk + 1] <= rc) ++walk;
+            head = walk;
+            t = (int)(rc - cu_b[head]);
+        } else if (same_length > 0) {
+            head = (int)((unsigned)rc / (unsigned)same_length);                  // (rows are fewer than 2^31)
+            t = (int)((unsigned)rc % (unsigned)same_length);
+        } else {
+            while (walk + 1 < g.n_items && (long long)cu_seq[walk + 1] * H <= rc) ++walk;
+            const int L = max(cu_seq[walk + 1] - cu_seq[walk], 1);
+            const unsigned in_item = (unsigned)(rc - (long long)cu_seq[walk] * H);
+            head = walk * H + min((int)(in_item / (unsigned)L), H - 1);
+            t = (int)(in_item % (unsigned)L);
+        }
+        const int item = head / H, h = head - item * H;
+        const int tok0 = cu_seq[item], L = cu_seq[item + 1] - tok0;
+        const int token = indices ? indices[rc] : t;
+        // an index outside the item is a caller error; cut so that it can never fault. (Loaded before it is known whether the head gets
+        // rows: a load latency less on the way of those that do)
+        const int64_t src = kv_row_offset(g, item, tok0, L, h, max(min(token, L - 1), 0)) + lane * 8;
+        const bool loads = L > 0;
+        kk[u] = row_piece<STREAM>(k + (loads ? src : 0));
+        vv[u] = row_piece<STREAM>(v + (loads ? src : 0));
+        heads[u] = head;
+        ts[u] = r < total_rows && loads ? t : -1;
     }
-    const int item = head / H, h = head - item * H;
-    const int tok0 = cu_seq[item], L = cu_seq[item + 1] - tok0;
-    const AppendJob job = a.jobs[head];
-    const int token = indices ? indices[rc] : t;
-    if (t < 0 || t >= job.rows || L <= 0) return;           // (whole groups of lanes)
-    const int x = seqs ? seqs[item] : item;
-    // an index outside the item is a caller error; cut so that it can never fault
-    const int64_t src = kv_row_offset(g, item, tok0, L, h, min(max(token, 0), L - 1)) + lane * 8;
-    const u32x4 kk = *reinterpret_cast<const u32x4*>(k + src), vv = *reinterpret_cast<const u32x4*>(v + src);
-    const int at = job.start + t, slot = at >> pv.log_p, row = at & (pv.rows() - 1);
-    const int first_new = pv.pages_of(job.start) - (job.copy_from >= 0);
-    const size_t entry = (size_t)(x * H + h) * pv.width + slot;
-    const int page = slot >= first_new ? a.found[job.first + slot - first_new] : pv.table[entry];
-    int ks, vs;
-    const unsigned kc = round_to_4(kk, ks), vc = round_to_4(vv, vs);
-    if (r >= total_rows || !pv.is_page(page)) return;
-    char* to = pv.page(page);
-    *reinterpret_cast<unsigned*>(to + pv.k_codes(row) + lane * 4) = kc;
-    *reinterpret_cast<unsigned*>(to + pv.v_codes(row) + lane * 4) = vc;
-    if ((lane & 3) == 0) {
-        to[pv.k_scales(row) + lane / 4] = (char)ks;
-        to[pv.v_scales(row) + lane / 4] = (char)vs;
-    }
-    if (lane == 0 && slot >= first_new && (row == 0 || t == 0)) {        // the first row that the page gets
-        pv.table[entry] = page;
-        pv.refs[page] = 1;
+#pragma unroll
+    for (int u = 0; u < R; ++u) {
+        const int head = heads[u], t = ts[u], item = head / H, h = head - item * H;
+        const AppendJob job = a.jobs[head];
+        int ks, vs;
+        const unsigned kc = round_to_4(kk[u], ks), vc = round_to_4(vv[u], vs);
+        const unsigned k_scales = scales_of_row<D>(ks, lane), v_scales = scales_of_row<D>(vs, lane);
+        if (t < 0 || t >= job.rows) continue;               // (whole groups of lanes)
+        const int x = seqs ? seqs[item] : item;
+        const int at = job.start + t, slot = at >> pv.log_p, row = at & (pv.rows() - 1);
+        const int first_new = pv.pages_of(job.start) - (job.copy_from >= 0);
+        const size_t entry = (size_t)(x * H + h) * pv.width + slot;
+        const int page = slot >= first_new ? a.found[job.first + slot - first_new] : pv.table[entry];
+        if (!pv.is_page(page)) continue;
+        char* to = pv.page(page);
+        *reinterpret_cast<unsigned*>(to + pv.k_codes(row) + lane * 4) = kc;
+        *reinterpret_cast<unsigned*>(to + pv.v_codes(row) + lane * 4) = vc;
+        if (lane % 16 == 0) {
+            if constexpr (D == 64) {
+                *reinterpret_cast<unsigned short*>(to + pv.k_scales(row)) = (unsigned short)k_scales;
+                *reinterpret_cast<unsigned short*>(to + pv.v_scales(row)) = (unsigned short)v_scales;
+            } else {
+                *reinterpret_cast<unsigned*>(to + pv.k_scales(row) + lane / 4) = k_scales;
+                *reinterpret_cast<unsigned*>(to + pv.v_scales(row) + lane / 4) = v_scales;
+            }
+        }
+        if (lane == 0 && slot >= first_new && (row == 0 || t == 0)) {        // the first row that the page gets
+            pv.table[entry] = page;
+            pv.refs[page] = 1;
+        }
     }
 }
 
@@ -270,7 +390,7 @@ __device__ __forceinline__ u32x4 values_of(unsigned codes, unsigned scale) {
 }
 
 // read: as many lanes to a row. Bound by the bf16 rows that it writes.
-template <int D>
+template <int D, bool STREAM>
 __global__ __launch_bounds__(kThreads) void read_kernel(
     PageView pv, const int32_t* __restrict__ first, const int32_t* __restrict__ cu, long long first_row, long long total_rows,
     u32x4* __restrict__ k_out, u32x4* __restrict__ v_out)
@@ -282,21 +402,26 @@ __global__ __launch_bounds__(kThreads) void read_kernel(
     int head = owner_of_row(cu, pv.n_heads, 1, row0);
     const long long rc = min(r, total_rows - 1);
     while (head + 1 < pv.n_heads && cu[head + 1] <= rc) ++head;
+    // (loads without branches around them: a row that is not there reads some page's, and is zero in the end)
     const long long at = rc - cu[head] + (first ? first[head] : 0);
+    const int most = (pv.width << pv.log_p) - 1, in = (int)min(max(at, 0ll), (long long)most);
+    const int page = pv.table[(size_t)head * pv.width + (in >> pv.log_p)];
+    const bool there = at >= 0 && at < pv.length(head) && pv.is_page(page);
+    const int row = in & (pv.rows() - 1);
+    const char* from = pv.page(pv.is_page(page) ? page : 0);
+    const unsigned kc = *reinterpret_cast<const unsigned*>(from + pv.k_codes(row) + lane * 4);
+    const unsigned vc = *reinterpret_cast<const unsigned*>(from + pv.v_codes(row) + lane * 4);
+    const unsigned char ks = from[pv.k_scales(row) + lane / 4], vs = from[pv.v_scales(row) + lane / 4];
     const u32x4 zero = {0, 0, 0, 0};
-    u32x4 kk = zero, vv = zero;
-    if (at >= 0 && at < pv.length(head)) {
-        const int page = pv.table[(size_t)head * pv.width + (at >> pv.log_p)];
-        if (pv.is_page(page)) {
-            const int row = (int)at & (pv.rows() - 1);
-            const char* from = pv.page(page);
-            kk = values_of(*reinterpret_cast<const unsigned*>(from + pv.k_codes(row) + lane * 4), (unsigned char)from[pv.k_scales(row) + lane / 4]);
-            vv = values_of(*reinterpret_cast<const unsigned*>(from + pv.v_codes(row) + lane * 4), (unsigned char)from[pv.v_scales(row) + lane / 4]);
-        }
-    }
+    const u32x4 kk = there ? values_of(kc, ks) : zero, vv = there ? values_of(vc, vs) : zero;
     if (r < total_rows) {
-        k_out[r * LANES + lane] = kk;
-        v_out[r * LANES + lane] = vv;
+        if constexpr (STREAM) {
+            __builtin_nontemporal_store(kk, k_out + r * LANES + lane);
+            __builtin_nontemporal_store(vv, v_out + r * LANES + lane);
+        } else {
+            k_out[r * LANES + lane] = kk;
+            v_out[r * LANES + lane] = vv;
+        }
     }
 }
 
@@ -311,19 +436,29 @@ size_t pages_append_bytes(const PageView& pv, int n_seqs, int n_items, long long
 hipError_t launch_pages_append(const Geom& g, const PageView& pv, const AppendCall& c, void* workspace, hipStream_t s)
 {
     const AppendSpace a = append_space(pv, c.n_seqs, c.n_items, c.total_rows, workspace, nullptr);
-    hipLaunchKernelGGL(append_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, pv, c.cu_budgets, c.cu_seqlens, c.seqs, c.n_items,
-                       c.n_seqs, (int)c.total_rows, a, c.refused);
+    const int heads = c.n_items * pv.H;
+#define AUDIOKV_PLAN(KERNEL, THREADS)                                                                                                    \
+    hipLaunchKernelGGL(KERNEL, dim3(1), dim3(THREADS), 0, s, pv, c.cu_budgets, c.cu_seqlens, c.seqs, c.n_items, c.n_seqs,                \
+                       (int)c.total_rows, a, c.refused)
+    if (heads <= 256 && a.most <= 2048 && c.n_seqs <= kSmallSeqs) AUDIOKV_PLAN(append_plan_small_kernel<256>, 256);
+    else if (heads <= 1024 && c.n_seqs <= kSmallSeqs) AUDIOKV_PLAN(append_plan_small_kernel<1024>, 1024);
+    else AUDIOKV_PLAN(append_plan_kernel, kPlanThreads);
+#undef AUDIOKV_PLAN
     hipError_t e = hipGetLastError();
     // a launch holds fewer than 2^32 threads: rows beyond that take further ones. Copies go along with the first
     const int rows_per_block = kThreads / (g.D / 8);
     const long long slab = (long long)rows_per_block << 22;
+    const bool stream = c.total_rows * g.D * 4 > kStreamBytes;
     for (long long first = 0; first < c.total_rows && e == hipSuccess; first += slab) {
         const long long rows = c.total_rows - first < slab ? c.total_rows - first : slab;
-        const int blocks = (int)((rows + rows_per_block - 1) / rows_per_block);
+        const int per_block = rows_per_block * (stream ? 4 : 1), blocks = (int)((rows + per_block - 1) / per_block);
         const int copies = first == 0 ? c.n_items * pv.H : 0;
-        AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL(append_rows_kernel<kD>, dim3(blocks + copies), dim3(kThreads), 0, s, g, pv,
-                                                (const __bf16*)c.k, (const __bf16*)c.v, c.indices, c.cu_budgets, c.cu_seqlens, c.seqs,
-                                                c.same_length, a, first, c.total_rows, blocks))
+#define AUDIOKV_ROWS(STREAM)                                                                                                             \
+    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL((append_rows_kernel<kD, (STREAM) ? 4 : 1, STREAM>), dim3(blocks + copies), dim3(kThreads), 0, s, g, pv,        \
+                                            (const __bf16*)c.k, (const __bf16*)c.v, c.indices, c.cu_budgets, c.cu_seqlens, c.seqs,       \
+                                            c.same_length, a, first, c.total_rows, blocks))
+        if (stream) AUDIOKV_ROWS(true) else AUDIOKV_ROWS(false)
+#undef AUDIOKV_ROWS
         e = hipGetLastError();
     }
     return e;
@@ -337,9 +472,12 @@ hipError_t launch_pages_read(const PageView& pv, const int32_t* first_dev, const
     hipError_t e = hipSuccess;
     for (long long first = 0; first < total_rows && e == hipSuccess; first += slab) {
         const long long rows = total_rows - first < slab ? total_rows - first : slab;
-        AUDIOKV_FOR_DIM(pv.D, hipLaunchKernelGGL(read_kernel<kD>, dim3((unsigned)((rows + rows_per_block - 1) / rows_per_block)),
-                                                 dim3(kThreads), 0, s, pv, first_dev, cu_rows, first, total_rows, (u32x4*)k_out,
-                                                 (u32x4*)v_out))
+        const dim3 grid((unsigned)((rows + rows_per_block - 1) / rows_per_block));
+#define AUDIOKV_READ(STREAM)                                                                                                             \
+    AUDIOKV_FOR_DIM(pv.D, hipLaunchKernelGGL((read_kernel<kD, STREAM>), grid, dim3(kThreads), 0, s, pv, first_dev, cu_rows, first,        \
+                                             total_rows, (u32x4*)k_out, (u32x4*)v_out))
+        if (total_rows * pv.D * 4 > kStreamBytes) AUDIOKV_READ(true) else AUDIOKV_READ(false)
+#undef AUDIOKV_READ
         e = hipGetLastError();
     }
     return e;
