@@ -243,12 +243,11 @@ __global__ __launch_bounds__(THREADS) void append_plan_small_kernel(
 
 // What 8 channels of a lane become: four bytes of codes, and the scale byte of the block, the same in the four lanes that hold it.
 __device__ __forceinline__ unsigned round_to_4(u32x4 x, int& scale) {
-    unsigned top = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        top = max(top, x[i] & 0x7fff);
-        top = max(top, (x[i] >> 16) & 0x7fff);
-    }
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    const auto magnitudes = [](unsigned w) { return __builtin_bit_cast(u16x2, w & 0x7fff7fffu); };
+    const u16x2 tops = __builtin_elementwise_max(__builtin_elementwise_max(magnitudes(x[0]), magnitudes(x[1])),
+                                                 __builtin_elementwise_max(magnitudes(x[2]), magnitudes(x[3])));
+    unsigned top = max(tops[0], tops[1]);
     top = max(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, 0xb1, 0xf, 0xf, false));      // lanes 1 0 3 2 of a quad
     top = max(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, 0x4e, 0xf, 0xf, false));      // lanes 2 3 0 1
     scale = scale_of(top);
@@ -263,6 +262,8 @@ __device__ __forceinline__ unsigned round_to_4(u32x4 x, int& scale) {
 #endif
     return scale == 255 ? 0 : codes;
 }
+
+constexpr int kStreamRows = 2;        // rows of a thread then: 367 thousand rows with one 66 us, two 55, four 59
 
 // What a call reads or writes once, 16 bytes of it. STREAM: more than the memory-side cache should keep.
 template <bool STREAM> __device__ __forceinline__ u32x4 row_piece(const __bf16* p) {
@@ -306,71 +307,87 @@ __global__ __launch_bounds__(kThreads) void append_rows_kernel(
     const int n_heads = g.n_items * H;
     const int lane = tid % LANES;
     const long long row0 = first_row + (long long)blockIdx.x * (ROWS * R);
-    // the head of the workgroup's first row, or its item, is found once; later rows walk forward from there
+    // The head of the workgroup's first row, or its item, is found once; later rows walk forward from there. (Begin and end of the head's
+    // rows, or of the item's, are held, and looked up again only where a row is behind them.)
     int walk = 0;
-    if (cu_b) walk = owner_of_row(cu_b, n_heads, 1, row0);
-    else if (same_length <= 0) walk = owner_of_row(cu_seq, g.n_items, H, row0);
+    long long begin = 0, end = 0;
+    if (cu_b) {
+        walk = owner_of_row(cu_b, n_heads, 1, row0);
+        begin = cu_b[walk], end = cu_b[walk + 1];
+    } else if (same_length <= 0) {
+        walk = owner_of_row(cu_seq, g.n_items, H, row0);
+        begin = (long long)cu_seq[walk] * H, end = (long long)cu_seq[walk + 1] * H;
+    }
     u32x4 kk[R], vv[R];
-    int heads[R], ts[R];                                    // head (of items) and its row; -1: no row
+    int head = -1, ts[R], entry_row[R];                      // row of the head, -1: none; row of the table
+    int64_t base = 0;                                       // where the head's first token lies in K and V, and tokens of it
+    int L = 0, table_row = 0;
+    const int64_t stride = kv_tok_stride(g);
+    AppendJob job{}, jobs[R];
 #pragma unroll
     for (int u = 0; u < R; ++u) {
         const long long r = row0 + u * ROWS + tid / LANES;
         const long long rc = min(r, total_rows - 1);        // a row past the end is the last one again, and not stored
-        int head, t;
+        int its, t;
         if (cu_b) {
-            while (walk + 1 < n_heads && cu_b[walk + 1] <= rc) ++walk;
-            head = walk;
-            t = (int)(rc - cu_b[head]);
+            while (walk + 1 < n_heads && end <= rc) begin = end, end = cu_b[++walk + 1];
+            its = walk;
+            t = (int)(rc - begin);
         } else if (same_length > 0) {
-            head = (int)((unsigned)rc / (unsigned)same_length);                  // (rows are fewer than 2^31)
+            its = (int)((unsigned)rc / (unsigned)same_length);                   // (rows are fewer than 2^31)
             t = (int)((unsigned)rc % (unsigned)same_length);
         } else {
-            while (walk + 1 < g.n_items && (long long)cu_seq[walk + 1] * H <= rc) ++walk;
-            const int L = max(cu_seq[walk + 1] - cu_seq[walk], 1);
-            const unsigned in_item = (unsigned)(rc - (long long)cu_seq[walk] * H);
-            head = walk * H + min((int)(in_item / (unsigned)L), H - 1);
-            t = (int)(in_item % (unsigned)L);
+            while (walk + 1 < g.n_items && end <= rc) begin = end, end = (long long)cu_seq[++walk + 1] * H;
+            const int of_head = max((int)(end - begin) / H, 1);
+            its = walk * H + min((int)((unsigned)(rc - begin) / (unsigned)of_head), H - 1);
+            t = (int)((unsigned)(rc - begin) % (unsigned)of_head);
         }
-        const int item = head / H, h = head - item * H;
-        const int tok0 = cu_seq[item], L = cu_seq[item + 1] - tok0;
+        if (its != head) {
+            head = its;
+            const int item = head / H, h = head - item * H, tok0 = cu_seq[item];
+            L = cu_seq[item + 1] - tok0;
+            base = kv_row_offset(g, item, tok0, L, h, 0);
+            job = a.jobs[head];
+            table_row = (seqs ? seqs[item] : item) * H + h;
+        }
         const int token = indices ? indices[rc] : t;
         // an index outside the item is a caller error; cut so that it can never fault. (Loaded before it is known whether the head gets
         // rows: a load latency less on the way of those that do)
-        const int64_t src = kv_row_offset(g, item, tok0, L, h, max(min(token, L - 1), 0)) + lane * 8;
-        const bool loads = L > 0;
-        kk[u] = row_piece<STREAM>(k + (loads ? src : 0));
-        vv[u] = row_piece<STREAM>(v + (loads ? src : 0));
-        heads[u] = head;
-        ts[u] = r < total_rows && loads ? t : -1;
+        const int64_t src = L > 0 ? base + max(min(token, L - 1), 0) * stride + lane * 8 : 0;
+        kk[u] = row_piece<STREAM>(k + src);
+        vv[u] = row_piece<STREAM>(v + src);
+        jobs[u] = job;
+        entry_row[u] = table_row;
+        ts[u] = r < total_rows && L > 0 ? t : -1;
     }
 #pragma unroll
     for (int u = 0; u < R; ++u) {
-        const int head = heads[u], t = ts[u], item = head / H, h = head - item * H;
-        const AppendJob job = a.jobs[head];
+        const AppendJob to = jobs[u];
+        const int t = ts[u];
         int ks, vs;
         const unsigned kc = round_to_4(kk[u], ks), vc = round_to_4(vv[u], vs);
         const unsigned k_scales = scales_of_row<D>(ks, lane), v_scales = scales_of_row<D>(vs, lane);
-        if (t < 0 || t >= job.rows) continue;               // (whole groups of lanes)
-        const int x = seqs ? seqs[item] : item;
-        const int at = job.start + t, slot = at >> pv.log_p, row = at & (pv.rows() - 1);
-        const int first_new = pv.pages_of(job.start) - (job.copy_from >= 0);
-        const size_t entry = (size_t)(x * H + h) * pv.width + slot;
-        const int page = slot >= first_new ? a.found[job.first + slot - first_new] : pv.table[entry];
+        if (t < 0 || t >= to.rows) continue;                // (whole groups of lanes)
+        const int at = to.start + t, slot = at >> pv.log_p, row = at & (pv.rows() - 1);
+        const int first_new = pv.pages_of(to.start) - (to.copy_from >= 0);
+        const bool fresh = slot >= first_new;
+        int32_t* entry = pv.table + (size_t)entry_row[u] * pv.width + slot;
+        const int page = fresh ? a.found[to.first + slot - first_new] : *entry;
         if (!pv.is_page(page)) continue;
-        char* to = pv.page(page);
-        *reinterpret_cast<unsigned*>(to + pv.k_codes(row) + lane * 4) = kc;
-        *reinterpret_cast<unsigned*>(to + pv.v_codes(row) + lane * 4) = vc;
+        char* bytes = pv.page(page);
+        *reinterpret_cast<unsigned*>(bytes + pv.k_codes(row) + lane * 4) = kc;
+        *reinterpret_cast<unsigned*>(bytes + pv.v_codes(row) + lane * 4) = vc;
         if (lane % 16 == 0) {
             if constexpr (D == 64) {
-                *reinterpret_cast<unsigned short*>(to + pv.k_scales(row)) = (unsigned short)k_scales;
-                *reinterpret_cast<unsigned short*>(to + pv.v_scales(row)) = (unsigned short)v_scales;
+                *reinterpret_cast<unsigned short*>(bytes + pv.k_scales(row)) = (unsigned short)k_scales;
+                *reinterpret_cast<unsigned short*>(bytes + pv.v_scales(row)) = (unsigned short)v_scales;
             } else {
-                *reinterpret_cast<unsigned*>(to + pv.k_scales(row) + lane / 4) = k_scales;
-                *reinterpret_cast<unsigned*>(to + pv.v_scales(row) + lane / 4) = v_scales;
+                *reinterpret_cast<unsigned*>(bytes + pv.k_scales(row) + lane / 4) = k_scales;
+                *reinterpret_cast<unsigned*>(bytes + pv.v_scales(row) + lane / 4) = v_scales;
             }
         }
-        if (lane == 0 && slot >= first_new && (row == 0 || t == 0)) {        // the first row that the page gets
-            pv.table[entry] = page;
+        if (lane == 0 && fresh && (row == 0 || t == 0)) {                    // the first row that the page gets
+            *entry = page;
             pv.refs[page] = 1;
         }
     }
@@ -451,10 +468,10 @@ hipError_t launch_pages_append(const Geom& g, const PageView& pv, const AppendCa
     const bool stream = c.total_rows * g.D * 4 > kStreamBytes;
     for (long long first = 0; first < c.total_rows && e == hipSuccess; first += slab) {
         const long long rows = c.total_rows - first < slab ? c.total_rows - first : slab;
-        const int per_block = rows_per_block * (stream ? 4 : 1), blocks = (int)((rows + per_block - 1) / per_block);
+        const int per_block = rows_per_block * (stream ? kStreamRows : 1), blocks = (int)((rows + per_block - 1) / per_block);
         const int copies = first == 0 ? c.n_items * pv.H : 0;
 #define AUDIOKV_ROWS(STREAM)                                                                                                             \
-    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL((append_rows_kernel<kD, (STREAM) ? 4 : 1, STREAM>), dim3(blocks + copies), dim3(kThreads), 0, s, g, pv,        \
+    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL((append_rows_kernel<kD, (STREAM) ? kStreamRows : 1, STREAM>), dim3(blocks + copies), dim3(kThreads), 0, s, g, pv,        \
                                             (const __bf16*)c.k, (const __bf16*)c.v, c.indices, c.cu_budgets, c.cu_seqlens, c.seqs,       \
                                             c.same_length, a, first, c.total_rows, blocks))
         if (stream) AUDIOKV_ROWS(true) else AUDIOKV_ROWS(false)
