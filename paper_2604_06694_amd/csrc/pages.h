@@ -58,12 +58,11 @@ __device__ __forceinline__ int owner_of_row(const int32_t* __restrict__ cu, int 
     return __builtin_amdgcn_readfirstlane(head);
 }
 
-// Sum over the lanes before this one and, in `total`, over the workgroup, whose waves' sums go through `sums` (a barrier before
-// and after).
+// Sum over the threads before this one and, in `total`, over the workgroup, whose waves' sums go through `sums` (_once: LDS that nobody
+// uses before or after).
 template <int THREADS>
-__device__ __forceinline__ int exclusive_sum(int x, int* sums, int& total) {
+__device__ __forceinline__ int exclusive_sum_once(int x, int* sums, int& total) {
     const int incl = wave_incl(x), wave = threadIdx.x >> 6;
-    __syncthreads();
     if ((threadIdx.x & 63) == 63) sums[wave] = incl;
     __syncthreads();
     int before = 0;
@@ -75,6 +74,11 @@ __device__ __forceinline__ int exclusive_sum(int x, int* sums, int& total) {
         total += s;
     }
     return before + incl - x;
+}
+template <int THREADS>
+__device__ __forceinline__ int exclusive_sum(int x, int* sums, int& total) {
+    __syncthreads();
+    return exclusive_sum_once<THREADS>(x, sums, total);
 }
 
 // What append and keep plan on the device, by one workgroup: which pages the heads get.

@@ -15,14 +15,19 @@
 //   O[channel][query] += V^T P  the lane's C, keys 4 r .. 4 r + 3 of two tiles, is its column of P as it is: the product runs over keys in
 //                               that order, and V's rows are loaded so
 // The running reference of the softmax moves only where a logit exceeds it by 2^8: a wave-wide test per unit instead of a maximum over
-// lanes and a rescaling. P goes to the second product as two bf16 numbers (16 bits of it), V in bf16 is exact.
+// lanes and a rescaling. P goes to the second product as two bf16 numbers (16 bits of it), V in bf16 is exact. Up to eight query heads
+// (PAIRS) columns c and c + 8 hold the same query, and the two numbers of P are one in each: half the instructions of the second product,
+// whose halves are added in the end. (The matrix cores' products of 4-bit keys as they are, with queries in 8 bits, are no choice: their
+// sums are off by 2^-13 of the sum of magnitudes, those of bf16 by less than 2^-23.)
 #include "pages.h"
+
+#include <algorithm>
 
 namespace audiokv {
 
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4, kUnit = 32;
+constexpr int kThreads = 256, kWaves = 4, kUnit = 32;       // of the kernels that share heads out
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
@@ -30,7 +35,7 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
 constexpr float kSlack = 8.f;       // octaves that a logit may lie above the reference
 
 struct AttendSpace {
-    int2* heads;            // [heads]: slot of the first part, parts (0: nothing to join)
+    int4* joins;            // [the fewer of heads and workgroups]: head, slot of its first part, parts (0: nothing to join)
     float* stats;           // [slot][G][2]: reference in base-2 units, sum
     float* parts;           // [slot][G][D]
 };
@@ -148,7 +153,7 @@ template <int D> struct Running {
     float ref, sum;
 };
 
-template <int D>
+template <int D, bool PAIRS>
 __device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, const bf16x8 (&q)[D / 32], float c_log2, int rows) {
     const int lane = threadIdx.x & 63, c = lane & 15, r = lane >> 4;
     f32x4 z[2];                                            // products, keys 4 r + i of either tile
@@ -187,13 +192,20 @@ __device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, cons
         for (int ct = 0; ct < D / 16; ++ct) o.out[ct] *= shrink;
     }
     const float ref = o.ref == -INFINITY ? 0.f : o.ref;
-    u32x4_t hi, lo;
+    u32x4_t hi, lo;            // PAIRS: hi is the column's own part, see above
+    [[maybe_unused]] const unsigned minus = PAIRS && (c & 8) ? 0x80000000u : 0;
+    [[maybe_unused]] const float whole = PAIRS && (c & 8) ? 1.f : 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float a = __builtin_amdgcn_exp2f(fmaf(z[i >> 1][2 * i & 3], c_log2, -ref)), b = __builtin_amdgcn_exp2f(fmaf(z[i >> 1][(2 * i & 3) + 1], c_log2, -ref));
         o.sum += a + b;
-        hi[i] = pack_bf16(a, b);
-        lo[i] = pack_bf16(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xffff0000u));
+        if constexpr (PAIRS) {         // the upper sixteen bits, or what they leave
+            const float ta = __uint_as_float((__float_as_uint(a) & 0xffff0000u) ^ minus), tb = __uint_as_float((__float_as_uint(b) & 0xffff0000u) ^ minus);
+            hi[i] = pack_bf16(fmaf(a, whole, ta), fmaf(b, whole, tb));
+        } else {
+            hi[i] = pack_bf16(a, b);
+            lo[i] = pack_bf16(a - __uint_as_float(hi[i] << 16), b - __uint_as_float(hi[i] & 0xffff0000u));
+        }
     }
 #pragma unroll
     for (int w = 0; w < (D + 127) / 128; ++w)
@@ -209,8 +221,10 @@ __device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, cons
             const int ct = w * 8 + b * 2;
             o.out[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), __builtin_bit_cast(bf16x8, hi), o.out[ct], 0, 0, 0);
             o.out[ct + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), __builtin_bit_cast(bf16x8, hi), o.out[ct + 1], 0, 0, 0);
-            o.out[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), __builtin_bit_cast(bf16x8, lo), o.out[ct], 0, 0, 0);
-            o.out[ct + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), __builtin_bit_cast(bf16x8, lo), o.out[ct + 1], 0, 0, 0);
+            if constexpr (!PAIRS) {
+                o.out[ct] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, even), __builtin_bit_cast(bf16x8, lo), o.out[ct], 0, 0, 0);
+                o.out[ct + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, odd), __builtin_bit_cast(bf16x8, lo), o.out[ct + 1], 0, 0, 0);
+            }
         }
 }
 
@@ -226,50 +240,106 @@ __device__ __forceinline__ int next_with_rows(const PageView& pv, int head) {
 
 __device__ __forceinline__ int units_of(int rows) { return (rows + kUnit - 1) / kUnit; }
 
-// First unit of workgroup w, and the workgroup that has unit u. In float64, where both are exact: numerators are below 2^42, and a quotient
-// that is no whole number is at least 2^-31 away from one. (Divisions of 64-bit integers took 130 instructions each.)
-__device__ __forceinline__ int first_unit(int units, int w, int W) { return (int)((double)units * w / W); }
-__device__ __forceinline__ int workgroup_of(int units, int u, int W) { return (int)((((double)u + 1) * W - 1) / units); }
+// n units in k shares: where share w begins, and which one has unit u. Spread evenly, so that equal heads and a multiple of their number of
+// shares end together. In float64, where both are exact: numerators are below 2^42, and a quotient that is no whole number is at least
+// 2^-31 away from one. (Divisions of 64-bit integers took 130 instructions each.)
+struct Shares {
+    int n, k;
+    __device__ __forceinline__ int begin(int w) const { return (int)((double)n * w / k); }
+    __device__ __forceinline__ int of(int u) const { return (int)((((double)u + 1) * k - 1) / n); }
+};
 
-// dynamic LDS: [wave][G][D + 4]
+constexpr int kAlignedUnits = 4;      // one more for each wave
+
 // waves of a SIMD: what two units on their way leave registers for
 template <int D> constexpr int kResident = D == 64 ? 4 : D == 128 ? 3 : 2;
 
-template <int D>
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kResident<D>, kResident<D>))) void attend_kernel(Geom g, PageView pv, const __bf16* __restrict__ q, __bf16* __restrict__ out,
-                                                          float* __restrict__ lse, AttendSpace a)
+// WHOLE: workgroup x takes head x, whatever its length; nothing is left to join.
+// dynamic LDS: [wave][G][D + 4]
+template <int D, bool PAIRS, int WAVES, bool WHOLE>
+__global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kResident<D>, kResident<D>))) void attend_kernel(
+    Geom g, PageView pv, const __bf16* __restrict__ q, __bf16* __restrict__ out, float* __restrict__ lse, AttendSpace a)
 {
+    constexpr int THREADS = 64 * WAVES;
     extern __shared__ __attribute__((aligned(16))) float merge[];
-    __shared__ int sums[kWaves];
-    __shared__ float ref_of[kWaves][16], sum_of[kWaves][16];
-    __shared__ int begin_head, begin_unit, begin_rows;
+    __shared__ int sums[2 * WAVES];
+    __shared__ float ref_of[WAVES][16], sum_of[WAVES][16];
+    __shared__ int begin_head, begin_at, begin_rows, begin_parts;
+    __shared__ int4 plan;        // for the end of a head, out of the way until then: all units, workgroups, parts of a head if aligned, by head
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), c = lane & 15, r = lane >> 4;
     const int G = g.G, PITCH = D + 4;
     const LaneOffsets<D> offsets;
 
-    // all units, and where this workgroup's first one is
-    const int each = (pv.n_heads + kThreads - 1) / kThreads, h0 = min(tid * each, pv.n_heads), h1 = min(h0 + each, pv.n_heads);
-    int mine = 0;
-    for (int h = h0; h < h1; ++h) mine += units_of(pv.length(h));
-    int total;
-    const int before = exclusive_sum<kThreads>(mine, sums, total);
-    const int W = min((int)gridDim.x, max(1, (total + kWaves - 1) / kWaves));
-    if ((int)blockIdx.x >= W || total == 0) return;
-    const int u0 = __builtin_amdgcn_readfirstlane(first_unit(total, blockIdx.x, W));
-    const int u1 = __builtin_amdgcn_readfirstlane(first_unit(total, blockIdx.x + 1, W));
-    if (mine > 0 && u0 >= before && u0 < before + mine) {
-        int h = h0, at = before, rows = pv.length(h0);
-        while (u0 >= at + units_of(rows)) {
-            at += units_of(rows);
-            rows = pv.length(++h);
+    int head, start, rows, u0, u1;
+    if constexpr (WHOLE) {
+        head = blockIdx.x;
+        start = u0 = 0;
+        rows = __builtin_amdgcn_readfirstlane(pv.length(head));
+        u1 = max(units_of(rows), 1);                                   // (a head without rows has one unit of none: zeros)
+    } else {
+        const int b = blockIdx.x, wgs = gridDim.x;
+        const bool by_head = pv.n_heads <= wgs;                        // which entry of a.joins: a head's, or a workgroup's last head's
+        int total, W;
+        if (!by_head && tid == 0) a.joins[b] = int4{0, 0, 0, 0};
+        // all units; and zeros for heads without rows, each by one workgroup
+        const int each = (pv.n_heads + THREADS - 1) / THREADS, h0 = min(tid * each, pv.n_heads), h1 = min(h0 + each, pv.n_heads);
+        int mine = 0;
+        for (int h = h0; h < h1; ++h) {
+            const int n = units_of(pv.length(h));
+            mine += n;
+            if (n == 0 && h % wgs == b) {
+                for (int e = 0; e < G * D; e += 8) *reinterpret_cast<u32x4*>(out + (size_t)h * G * D + e) = u32x4{0, 0, 0, 0};
+                for (int e = 0; lse && e < G; ++e) lse[(size_t)h * G + e] = -INFINITY;
+                if (by_head) a.joins[h] = int4{0, 0, 0, 0};
+            }
         }
-        begin_head = h;
-        begin_unit = at;
-        begin_rows = rows;
+        int before = exclusive_sum_once<THREADS>(mine, sums, total);
+        if (total == 0) return;
+        // Workgroups that have parts of two heads work on them one after the other, some 3 us. Where shares that end with the heads are
+        // not much larger, there are those instead: of `share` units at most.
+        const int share = 2 * pv.n_heads <= wgs ? max((total + wgs - pv.n_heads - 1) / (wgs - pv.n_heads), WAVES) : INT_MAX;
+        const bool aligned = share - kAlignedUnits <= total / wgs;
+        if (aligned) {
+            mine = 0;
+            for (int h = h0; h < h1; ++h) mine += (units_of(pv.length(h)) + share - 1) / share;
+            before = exclusive_sum_once<THREADS>(mine, sums + WAVES, W);
+        } else {
+            W = min(wgs, (total + WAVES - 1) / WAVES);
+        }
+        if (b >= W) return;
+        // the head in which this workgroup's share begins: `at` units (or workgroups) are before it
+        const Shares of_all{total, W};
+        const int first = aligned ? b : of_all.begin(b);
+        if (first >= before && first < before + mine) {
+            int h = h0, at = before;
+            for (;; ++h) {
+                rows = pv.length(h);
+                const int n = aligned ? (units_of(rows) + share - 1) / share : units_of(rows);
+                if (first < at + n) {
+                    begin_parts = n;
+                    break;
+                }
+                at += n;
+            }
+            begin_head = h;
+            begin_at = at;
+            begin_rows = rows;
+        }
+        __syncthreads();
+        head = __builtin_amdgcn_readfirstlane(begin_head);
+        rows = __builtin_amdgcn_readfirstlane(begin_rows);
+        start = __builtin_amdgcn_readfirstlane(begin_at);
+        if (aligned) {
+            const Shares of_head{units_of(rows), __builtin_amdgcn_readfirstlane(begin_parts)};
+            u0 = __builtin_amdgcn_readfirstlane(of_head.begin(b - start));
+            u1 = __builtin_amdgcn_readfirstlane(of_head.begin(b - start + 1));
+            start = 0;
+        } else {
+            u0 = __builtin_amdgcn_readfirstlane(first);
+            u1 = __builtin_amdgcn_readfirstlane(of_all.begin(b + 1));
+        }
+        if (tid == 0) plan = int4{total, W, aligned ? begin_parts : 0, by_head};
     }
-    __syncthreads();
-    int head = __builtin_amdgcn_readfirstlane(begin_head), start = __builtin_amdgcn_readfirstlane(begin_unit);
-    int rows = __builtin_amdgcn_readfirstlane(begin_rows);
 
     for (int u = u0; u < u1;) {
         const int units = units_of(rows);
@@ -279,7 +349,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kResid
         const int log_u = pv.log_p - 5;                                    // units to a page
         bf16x8 qf[D / 32];
         {
-            const __bf16* src = q + ((size_t)x * g.H_q + (size_t)h * G + min(c, G - 1)) * D;    // (columns from G on: copies, unused)
+            const __bf16* src = q + ((size_t)x * g.H_q + (size_t)h * G + min(PAIRS ? c & 7 : c, G - 1)) * D;    // (columns from G on: copies, unused)
 #pragma unroll
             for (int s = 0; s < D / 32; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(src + channel_of<D>(s, r));
         }
@@ -291,29 +361,29 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kResid
         // Two units on their way: while one is worked on, the next is loaded (the last one again behind it, so that every step waits
         // for as many loads), and the page of the one after that is looked up.
         if (from + wave < to) {
-            const int last = from + wave + (to - 1 - from - wave) / kWaves * kWaves;
+            const int last = from + wave + (to - 1 - from - wave) / WAVES * WAVES;
             auto page_of = [&](int i) { return __builtin_amdgcn_readfirstlane(table[min(i, last) >> log_u]); };
             auto load = [&](Rows32<D>& unit, int i, int page) {
                 load_unit<D>(unit, pv, offsets, pv.is_page(page) ? page : 0, (min(i, last) & ((1 << log_u) - 1)) * kUnit);
             };
             auto add = [&](const Rows32<D>& unit, int i, int page) {       // (rows of no page take no part)
-                add_unit<D>(o, unit, qf, g.c_log2, pv.is_page(page) ? min(kUnit, rows - i * kUnit) : 0);
+                add_unit<D, PAIRS>(o, unit, qf, g.c_log2, pv.is_page(page) ? min(kUnit, rows - i * kUnit) : 0);
             };
             Rows32<D> a0, a1;
-            int i = from + wave, p0 = page_of(i), p1 = page_of(i + kWaves);
+            int i = from + wave, p0 = page_of(i), p1 = page_of(i + WAVES);
             load(a0, i, p0);
             for (;;) {
-                int p2 = page_of(i + 2 * kWaves);
-                load(a1, i + kWaves, p1);
+                int p2 = page_of(i + 2 * WAVES);
+                load(a1, i + WAVES, p1);
                 __builtin_amdgcn_sched_barrier(0);
                 add(a0, i, p0);
-                i += kWaves;
+                i += WAVES;
                 if (i > last) break;
-                p0 = page_of(i + 2 * kWaves);
-                load(a0, i + kWaves, p2);
+                p0 = page_of(i + 2 * WAVES);
+                load(a0, i + WAVES, p2);
                 __builtin_amdgcn_sched_barrier(0);
                 add(a1, i, p1);
-                i += kWaves;
+                i += WAVES;
                 if (i > last) break;
                 p1 = p0;
                 p0 = p2;
@@ -332,8 +402,17 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kResid
             sum_of[wave][c] = sum;
         }
         __syncthreads();
-        const float all = fmaxf(fmaxf(ref_of[0][c], ref_of[1][c]), fmaxf(ref_of[2][c], ref_of[3][c]));
+        float all = ref_of[0][c];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) all = fmaxf(all, ref_of[w][c]);
         const float shrink = o.ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(o.ref - all);
+        if constexpr (PAIRS) {
+#pragma unroll
+            for (int ct = 0; ct < D / 16; ++ct)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    o.out[ct][i] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(o.out[ct][i]), 0x128, 0xf, 0xf, false));   // lane 8 away of 16
+        }
         if (c < G) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -343,24 +422,27 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kResid
                         f32x4{o.out[ct][i], o.out[ct + 1][i], o.out[ct + 2][i], o.out[ct + 3][i]} * shrink;
         }
         __syncthreads();
-        const bool whole = from == 0 && to == units;
+        const bool whole = WHOLE || (from == 0 && to == units);
         const int slot = 2 * blockIdx.x + (u != u0);
-        if (me == 0) {
-            if (whole) a.heads[head] = int2{0, 0};
-            else if (from == 0) a.heads[head] = int2{slot, workgroup_of(total, start + units - 1, W) - (int)blockIdx.x + 1};
+        if (!WHOLE && me == 0) {
+            const int4 all = plan;
+            const int n = all.z > 0 ? all.z : Shares{all.x, all.y}.of(start + units - 1) - (int)blockIdx.x + 1;
+            if (from == 0 && (all.w || !whole)) a.joins[all.w ? head : blockIdx.x] = int4{head, slot, whole ? 0 : n, 0};
         }
         auto sums_of = [&](int n, float& m) {
-            m = fmaxf(fmaxf(ref_of[0][n], ref_of[1][n]), fmaxf(ref_of[2][n], ref_of[3][n]));
+            m = ref_of[0][n];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) m = fmaxf(m, ref_of[w][n]);
             float l = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) l += sum_of[w][n] * (ref_of[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref_of[w][n] - m));   // (NaN stays NaN)
+            for (int w = 0; w < WAVES; ++w) l += sum_of[w][n] * (ref_of[w][n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ref_of[w][n] - m));   // (NaN stays NaN)
             return l;
         };
-        for (int e = me * 4; e < G * D; e += kThreads * 4) {
+        for (int e = me * 4; e < G * D; e += THREADS * 4) {
             const int n = e / D, ch = e % D;
             f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) v += *reinterpret_cast<const f32x4*>(&merge[(w * G + n) * PITCH + ch]);
+            for (int w = 0; w < WAVES; ++w) v += *reinterpret_cast<const f32x4*>(&merge[(w * G + n) * PITCH + ch]);
             if (whole) {
                 float m;
                 const float l = sums_of(n, m);
@@ -380,6 +462,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kResid
                 lse[(size_t)x * g.H_q + (size_t)h * G + me] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
             }
         }
+        if (WHOLE) return;
         u = start + to;
         start += units;
         if (u < u1) {
@@ -390,29 +473,23 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(kResid
     }
 }
 
-// One workgroup per query head: the parts of its KV head, in order. A head without rows gives zeros. A chain of loads from end to end:
-// the first parts are on their way with the statistics.
+// One workgroup per query head of a head in parts: the parts in order. A chain of loads from end to end: the first parts are on their way
+// with the statistics.
 constexpr int kMaxWorkgroups = 256 * 4, kEarly = 2;
 
 template <int D>
-__global__ __launch_bounds__(kThreads) void join_kernel(Geom g, PageView pv, __bf16* __restrict__ out, float* __restrict__ lse, AttendSpace a)
+__global__ __launch_bounds__(kThreads) void join_kernel(Geom g, __bf16* __restrict__ out, float* __restrict__ lse, AttendSpace a)
 {
     constexpr int QUADS = D / 4, GROUPS = kThreads / QUADS, WAVES = kThreads / 64;     // threads on four channels each, parts at a time
-    const int G = g.G, head = blockIdx.x / G, n = blockIdx.x - head * G, tid = threadIdx.x;
-    const int x = head / g.H_kv, h = head - x * g.H_kv;
-    const size_t row = (size_t)x * g.H_q + (size_t)h * G + n;
-    const int2 from = a.heads[head];
-    if (pv.length(head) == 0) {
-        if (tid < QUADS) *reinterpret_cast<u32x2*>(out + row * D + tid * 4) = u32x2{0, 0};
-        if (lse && tid == 0) lse[row] = -INFINITY;
-        return;
-    }
-    const int parts = min(from.y, kMaxWorkgroups);
+    const int G = g.G, entry = blockIdx.x / G, n = blockIdx.x - entry * G, tid = threadIdx.x;
+    const int4 from = a.joins[entry];
+    const int parts = min(from.z, kMaxWorkgroups);
     if (parts == 0) return;
+    const size_t row = (size_t)from.x * G + n;                              // (query heads of a KV head are neighbours)
     __shared__ float weight[kMaxWorkgroups], wave_m[WAVES], wave_l[WAVES];
     __shared__ __attribute__((aligned(16))) f32x4 red[kThreads];
     // part p of the head: the first where the head began, the others the first of the workgroups behind
-    auto slot_of = [&](int p) { return p == 0 ? from.x : (from.x & ~1) + 2 * p; };
+    auto slot_of = [&](int p) { return p == 0 ? from.y : (from.y & ~1) + 2 * p; };
     const int ch = tid % QUADS * 4, grp = tid / QUADS;
     auto part = [&](int p) { return *reinterpret_cast<const f32x4*>(a.parts + ((size_t)slot_of(p) * G + n) * D + ch); };
     f32x4 early[kEarly];
@@ -459,6 +536,12 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Geom g, PageView pv, __b
     }
 }
 
+template <int D> constexpr int kWholeWaves = 4 * kResident<D>;
+// Heads of at most this many rows go to a workgroup each, of as many waves as a CU holds, and there is no second launch.
+constexpr long long kWholeRows = 2048;
+constexpr int kWholeHeads = 512;
+bool whole_heads(const PageView& pv) { return ((long long)pv.width << pv.log_p) <= kWholeRows && pv.n_heads <= kWholeHeads; }
+
 // Workgroups: as many as the registers let run at once, so that equal shares end together
 int workgroups(const Geom& g, const PageView& pv) {
     const long long most = ((long long)pv.n_heads * pv.width << pv.log_p) / (kUnit * kWaves) + pv.n_heads;
@@ -467,12 +550,15 @@ int workgroups(const Geom& g, const PageView& pv) {
     return (int)(most < w ? most : w);
 }
 
+// heads in parts at most: every boundary between workgroups is within one head
+int joins(const Geom& g, const PageView& pv) { return std::min(pv.n_heads, workgroups(g, pv)); }
+
 AttendSpace attend_space(const Geom& g, const PageView& pv, void* workspace, size_t* bytes) {
     AttendSpace a;
     const size_t slots = 2 * (size_t)workgroups(g, pv);
     char* at = static_cast<char*>(workspace);
-    a.heads = reinterpret_cast<int2*>(at);
-    size_t off = up256((size_t)pv.n_heads * sizeof(int2));
+    a.joins = reinterpret_cast<int4*>(at);
+    size_t off = up256((size_t)joins(g, pv) * sizeof(int4));
     a.stats = reinterpret_cast<float*>(at + off);
     off += up256(slots * g.G * 2 * sizeof(float));
     a.parts = reinterpret_cast<float*>(at + off);
@@ -492,12 +578,21 @@ size_t pages_attend_bytes(const Geom& g, const PageView& pv) {
 hipError_t launch_pages_attend(const Geom& g, const PageView& pv, const void* q, void* out, float* lse, void* workspace, hipStream_t s)
 {
     const AttendSpace a = attend_space(g, pv, workspace, nullptr);
-    const dim3 grid((unsigned)workgroups(g, pv)), join((unsigned)(pv.n_heads * g.G));
-    const unsigned lds = (unsigned)(sizeof(float) * kWaves * g.G * (g.D + 4));
-    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL(attend_kernel<kD>, grid, dim3(kThreads), lds, s, g, pv, (const __bf16*)q, (__bf16*)out, lse, a))
+    const unsigned lds = (unsigned)sizeof(float) * g.G * (g.D + 4);
+#define AUDIOKV_ATTEND(PAIRS, WAVES, WHOLE)                                                                                              \
+    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL((attend_kernel<kD, PAIRS, WAVES, WHOLE>), grid, dim3(64 * (WAVES)), lds * (WAVES), s, g, pv, \
+                                            (const __bf16*)q, (__bf16*)out, lse, a))
+    if (whole_heads(pv)) {
+        const dim3 grid((unsigned)pv.n_heads);
+        if (g.G <= 8) AUDIOKV_ATTEND(true, kWholeWaves<kD>, true) else AUDIOKV_ATTEND(false, kWholeWaves<kD>, true)
+        return hipGetLastError();
+    }
+    const dim3 grid((unsigned)workgroups(g, pv)), join((unsigned)(joins(g, pv) * g.G));
+    if (g.G <= 8) AUDIOKV_ATTEND(true, kWaves, false) else AUDIOKV_ATTEND(false, kWaves, false)
+#undef AUDIOKV_ATTEND
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL(join_kernel<kD>, join, dim3(kThreads), 0, s, g, pv, (__bf16*)out, lse, a))
+    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL(join_kernel<kD>, join, dim3(kThreads), 0, s, g, (__bf16*)out, lse, a))
     return hipGetLastError();
 }
 

@@ -303,10 +303,20 @@ def test_attend(A, d, P, G):
     attend(A, cache(r, 4, 3, d, P, [0, 1, 2, 31, 32, 33, 63, 64, 65, 257, 700, 1500]), G, r)
 
 
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("G", [1, 7, 16])
+@pytest.mark.parametrize("P", [32, 128])
+def test_attend_heads_in_parts(A, d, G, P):
+    """Tables that long heads would fit in: heads are shared out among workgroups, whatever they are long."""
+    r = np.random.default_rng(d + G + P)
+    attend(A, cache(r, 4, 3, d, P, [0, 1, 2, 31, 32, 33, 63, 64, 65, 257, 700, 2900], max_pages=4000 // P), G, r)
+
+
 @pytest.mark.parametrize("lengths", [[1], [0], [5], [129], [4096], [20000], [0, 0, 0, 0, 0, 0, 0, 9], [3000, 1, 1, 1, 1, 1, 1, 1]])
 def test_attend_few(A, lengths):
     r = np.random.default_rng(sum(lengths))
-    attend(A, cache(r, 1, len(lengths), 128, 64, lengths), 4, r)
+    for most in (None, 400):
+        attend(A, cache(r, 1, len(lengths), 128, 64, lengths, max_pages=most), 4, r)
 
 
 @pytest.mark.parametrize("d", [64, 128, 256])
