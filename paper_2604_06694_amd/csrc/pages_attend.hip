@@ -32,6 +32,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
 
+constexpr size_t kStreamBytes = 256u << 20;       // of a pool: what the memory-side cache holds
 constexpr float kSlack = 8.f;       // octaves that a logit may lie above the reference
 
 struct AttendSpace {
@@ -68,24 +69,28 @@ template <int D> struct LaneOffsets {
     }
 };
 
-template <class T> __device__ __forceinline__ T at(const char* base, unsigned lane_offset, int offset) {
-    return *reinterpret_cast<const T*>(base + offset + lane_offset);
+template <class T, bool STREAM = false> __device__ __forceinline__ T at(const char* base, unsigned lane_offset, int offset) {
+    const T* p = reinterpret_cast<const T*>(base + offset + lane_offset);
+    return STREAM ? __builtin_nontemporal_load(p) : *p;
 }
 
-template <int D>
+// STREAM: what takes whole cache lines with one instruction (K's codes up to D = 128, V's at 256) passes the caches by. The rest shares
+// lines with the next instruction. For caches that the memory-side cache does not hold: 522 MB 98 -> 82 us, 1 GB at D = 128 190 -> 177, at
+// 256 181 -> 170, while one of 261 MB took 43.8 instead of 42.8.
+template <int D, bool STREAM>
 __device__ __forceinline__ void load_unit(Rows32<D>& u, const PageView& pv, const LaneOffsets<D>& of, int page, int row0) {
     const char* base = pv.page(page);
     const char *k = base + pv.k_codes(row0), *v = base + pv.v_codes(row0), *ks = base + pv.k_scales(row0), *vs = base + pv.v_scales(row0);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         if constexpr (D == 64) {
-            const u32x2 w = at<u32x2>(k, of.k, t * 16 * (D / 2));
+            const u32x2 w = at<u32x2, STREAM>(k, of.k, t * 16 * (D / 2));
             u.k[t][0] = w[0];
             u.k[t][1] = w[1];
         } else {
 #pragma unroll
             for (int b = 0; b < D / 128; ++b) {
-                const u32x4 w = at<u32x4>(k, of.k, t * 16 * (D / 2) + b * 64);
+                const u32x4 w = at<u32x4, STREAM && D == 128>(k, of.k, t * 16 * (D / 2) + b * 64);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) u.k[t][b * 4 + i] = w[i];
             }
@@ -100,7 +105,7 @@ __device__ __forceinline__ void load_unit(Rows32<D>& u, const PageView& pv, cons
         if constexpr (D == 64) u.v[n][0] = at<unsigned short>(v, of.v, row * (D / 2));
         else if constexpr (D == 128) u.v[n][0] = at<unsigned>(v, of.v, row * (D / 2));
         else {
-            const u32x2 w = at<u32x2>(v, of.v, row * (D / 2));
+            const u32x2 w = at<u32x2, STREAM>(v, of.v, row * (D / 2));
             u.v[n][0] = w[0];
             u.v[n][1] = w[1];
         }
@@ -256,7 +261,7 @@ template <int D> constexpr int kResident = D == 64 ? 4 : D == 128 ? 3 : 2;
 
 // WHOLE: workgroup x takes head x, whatever its length; nothing is left to join.
 // dynamic LDS: [wave][G][D + 4]
-template <int D, bool PAIRS, int WAVES, bool WHOLE>
+template <int D, bool PAIRS, int WAVES, bool WHOLE, bool STREAM>
 __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kResident<D>, kResident<D>))) void attend_kernel(
     Geom g, PageView pv, const __bf16* __restrict__ q, __bf16* __restrict__ out, float* __restrict__ lse, AttendSpace a)
 {
@@ -364,7 +369,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kRes
             const int last = from + wave + (to - 1 - from - wave) / WAVES * WAVES;
             auto page_of = [&](int i) { return __builtin_amdgcn_readfirstlane(table[min(i, last) >> log_u]); };
             auto load = [&](Rows32<D>& unit, int i, int page) {
-                load_unit<D>(unit, pv, offsets, pv.is_page(page) ? page : 0, (min(i, last) & ((1 << log_u) - 1)) * kUnit);
+                load_unit<D, STREAM>(unit, pv, offsets, pv.is_page(page) ? page : 0, (min(i, last) & ((1 << log_u) - 1)) * kUnit);
             };
             auto add = [&](const Rows32<D>& unit, int i, int page) {       // (rows of no page take no part)
                 add_unit<D, PAIRS>(o, unit, qf, g.c_log2, pv.is_page(page) ? min(kUnit, rows - i * kUnit) : 0);
@@ -579,16 +584,20 @@ hipError_t launch_pages_attend(const Geom& g, const PageView& pv, const void* q,
 {
     const AttendSpace a = attend_space(g, pv, workspace, nullptr);
     const unsigned lds = (unsigned)sizeof(float) * g.G * (g.D + 4);
-#define AUDIOKV_ATTEND(PAIRS, WAVES, WHOLE)                                                                                              \
-    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL((attend_kernel<kD, PAIRS, WAVES, WHOLE>), grid, dim3(64 * (WAVES)), lds * (WAVES), s, g, pv, \
-                                            (const __bf16*)q, (__bf16*)out, lse, a))
+#define AUDIOKV_ATTEND(PAIRS, WAVES, WHOLE, STREAM)                                                                                      \
+    AUDIOKV_FOR_DIM(g.D, hipLaunchKernelGGL((attend_kernel<kD, PAIRS, WAVES, WHOLE, STREAM>), grid, dim3(64 * (WAVES)), lds * (WAVES), s, g, \
+                                            pv, (const __bf16*)q, (__bf16*)out, lse, a))
     if (whole_heads(pv)) {
         const dim3 grid((unsigned)pv.n_heads);
-        if (g.G <= 8) AUDIOKV_ATTEND(true, kWholeWaves<kD>, true) else AUDIOKV_ATTEND(false, kWholeWaves<kD>, true)
+        if (g.G <= 8) AUDIOKV_ATTEND(true, kWholeWaves<kD>, true, false) else AUDIOKV_ATTEND(false, kWholeWaves<kD>, true, false)
         return hipGetLastError();
     }
     const dim3 grid((unsigned)workgroups(g, pv)), join((unsigned)(joins(g, pv) * g.G));
-    if (g.G <= 8) AUDIOKV_ATTEND(true, kWaves, false) else AUDIOKV_ATTEND(false, kWaves, false)
+    if ((size_t)pv.n_pages * pv.page_bytes() <= kStreamBytes) {
+        if (g.G <= 8) AUDIOKV_ATTEND(true, kWaves, false, false) else AUDIOKV_ATTEND(false, kWaves, false, false)
+    } else {
+        if (g.G <= 8) AUDIOKV_ATTEND(true, kWaves, false, true) else AUDIOKV_ATTEND(false, kWaves, false, true)
+    }
 #undef AUDIOKV_ATTEND
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
