@@ -320,8 +320,8 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kRes
             for (;; ++h) {
                 rows = pv.length(h);
                 const int n = aligned ? (units_of(rows) + share - 1) / share : units_of(rows);
-                if (first < at + n) {
-                    begin_parts = n;
+                if (first < at + n || h + 1 >= h1) {                   // (the second: lengths that change meanwhile lead nowhere else)
+                    begin_parts = max(n, 1);
                     break;
                 }
                 at += n;
@@ -472,6 +472,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kRes
         start += units;
         if (u < u1) {
             head = next_with_rows(pv, head + 1);
+            if (head >= pv.n_heads) return;
             rows = __builtin_amdgcn_readfirstlane(pv.length(head));
         }
         __syncthreads();                                                   // the LDS is free again

@@ -160,6 +160,8 @@ __global__ __launch_bounds__(kPlanThreads) void keep_plan_kernel(PageView pv, co
             if (rows < job.had) {
                 job.rows = rows;
                 // Rows come in order, none twice: where row r is index r, the ones before are theirs, too.
+                // (Eight places asked at once instead of one: a third of the rounds, but 512 lines for 64 heads in each, and one CU gets
+                // them no sooner: 11.8 -> 15.8 us.)
                 const int32_t* mine = indices + begin;
                 int lo = 0, hi = rows >> pv.log_p;
                 while (lo < hi) {
@@ -195,8 +197,30 @@ __global__ __launch_bounds__(kPlanThreads) void keep_plan_kernel(PageView pv, co
     }
 }
 
-// The kept rows into the new pages: consecutive rows to a workgroup, D / 32 lanes a row, each a block's codes and scale of K and V.
-// A workgroup's rows are in new pages or in pages that stay row by row; the latter have nothing to do.
+// A row as it is held, D / 32 lanes to it: a block's codes and scale of K and V each. Rows are numbered within their head.
+template <int D>
+struct HeldRow {
+    u32x4 k, v;
+    char ks, vs;
+    __device__ __forceinline__ void load(const PageView& pv, int page, int row, int lane) {
+        const char* s = pv.page(pv.is_page(page) ? page : 0);
+        row &= pv.rows() - 1;
+        k = *reinterpret_cast<const u32x4*>(s + pv.k_codes(row) + lane * 16);
+        v = *reinterpret_cast<const u32x4*>(s + pv.v_codes(row) + lane * 16);
+        ks = s[pv.k_scales(row) + lane];
+        vs = s[pv.v_scales(row) + lane];
+    }
+    __device__ __forceinline__ void store(const PageView& pv, int page, int row, int lane) const {
+        char* d = pv.page(page);
+        row &= pv.rows() - 1;
+        *reinterpret_cast<u32x4*>(d + pv.k_codes(row) + lane * 16) = k;
+        *reinterpret_cast<u32x4*>(d + pv.v_codes(row) + lane * 16) = v;
+        d[pv.k_scales(row) + lane] = ks;
+        d[pv.v_scales(row) + lane] = vs;
+    }
+};
+
+// The kept rows into the new pages, consecutive rows to a workgroup. (A row in a page that stays has nothing to do.)
 template <int D>
 __global__ __launch_bounds__(kThreads) void keep_move_kernel(PageView pv, const int32_t* __restrict__ indices,
                                                              const int32_t* __restrict__ cu_b, long long first_row,
@@ -215,25 +239,18 @@ __global__ __launch_bounds__(kThreads) void keep_move_kernel(PageView pv, const 
     const int at = min(max(indices[rc], 0), job.had - 1);              // an index outside is a caller error; cut
     const int from = pv.table[(size_t)head * pv.width + (at >> pv.log_p)], to = a.found[job.first + slot - job.same];
     if (!pv.is_page(from) || !pv.is_page(to)) return;
-    const int src = at & (pv.rows() - 1), dst = t & (pv.rows() - 1);
-    const char* s = pv.page(from);
-    char* d = pv.page(to);
-    *reinterpret_cast<u32x4*>(d + pv.k_codes(dst) + lane * 16) = *reinterpret_cast<const u32x4*>(s + pv.k_codes(src) + lane * 16);
-    *reinterpret_cast<u32x4*>(d + pv.v_codes(dst) + lane * 16) = *reinterpret_cast<const u32x4*>(s + pv.v_codes(src) + lane * 16);
-    d[pv.k_scales(dst) + lane] = s[pv.k_scales(src) + lane];
-    d[pv.v_scales(dst) + lane] = s[pv.v_scales(src) + lane];
+    HeldRow<D> row;
+    row.load(pv, from, at, lane);
+    row.store(pv, to, t, lane);
 }
 
-__global__ __launch_bounds__(kThreads) void keep_table_kernel(PageView pv, KeepSpace a)
-{
-    const int head = blockIdx.x;
-    const KeepJob job = a.jobs[head];
-    if (job.rows < 0) return;
+// The table's new entries, refs and length of a head; `before` its entries until then.
+__device__ __forceinline__ void commit_head(const PageView& pv, const KeepSpace& a, const KeepJob& job, int head, const int32_t* before) {
     int32_t* mine = pv.table + (size_t)head * pv.width;
     const int had = pv.pages_of(job.had), has = pv.pages_of(job.rows);
     int freed = 0;
-    for (int j = job.same + threadIdx.x; j < had; j += kThreads) {
-        const int page = mine[j];
+    for (int j = job.same + threadIdx.x; j < had; j += blockDim.x) {
+        const int page = before[j];
         if (pv.is_page(page)) freed += atomicSub(&pv.refs[page], 1) == 1;
         if (j < has) {
             const int now = a.found[job.first + j - job.same];
@@ -244,6 +261,48 @@ __global__ __launch_bounds__(kThreads) void keep_table_kernel(PageView pv, KeepS
     if (threadIdx.x == 0) pv.lengths[head] = job.rows;
     freed = wave_incl(freed);
     if ((threadIdx.x & 63) == 63 && freed > 0) atomicAdd(&pv.state[0], freed);
+}
+
+__global__ __launch_bounds__(kThreads) void keep_table_kernel(PageView pv, KeepSpace a)
+{
+    const KeepJob job = a.jobs[blockIdx.x];
+    if (job.rows >= 0) commit_head(pv, a, job, blockIdx.x, pv.table + (size_t)blockIdx.x * pv.width);
+}
+
+// Both for heads whose tables hold kWholeRows rows at most, a workgroup each: the old entries wait in LDS, and no other workgroup reads
+// them. (16 heads of 1100 rows: 3.9 + 3.1 us by the two kernels, 5.7 by this one.)
+constexpr long long kWholeRows = 2048;
+constexpr int kWholeThreads = 512;
+
+template <int D>
+__global__ __launch_bounds__(kWholeThreads) void keep_whole_kernel(PageView pv, const int32_t* __restrict__ indices,
+                                                                   const int32_t* __restrict__ cu_b, KeepSpace a)
+{
+    constexpr int LANES = D / 32;
+    __shared__ int32_t before[kWholeRows / 32];
+    const int head = blockIdx.x, lane = threadIdx.x % LANES;
+    const KeepJob job = a.jobs[head];
+    const int begin = max(cu_b[head], 0);
+    if (job.rows < 0) return;
+    for (int j = threadIdx.x; j < pv.pages_of(job.had); j += kWholeThreads) before[j] = pv.table[(size_t)head * pv.width + j];
+    __syncthreads();
+    constexpr int U = 4, STEP = kWholeThreads / LANES;                   // rows of a thread on their way
+    for (int t0 = (job.same << pv.log_p) + threadIdx.x / LANES; t0 < job.rows; t0 += U * STEP) {
+        int at[U], to[U];
+        HeldRow<D> row[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int t = min(t0 + u * STEP, job.rows - 1);
+            at[u] = min(max(indices[begin + t], 0), job.had - 1);
+            to[u] = a.found[job.first + (t >> pv.log_p) - job.same];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) row[u].load(pv, before[at[u] >> pv.log_p], at[u], lane);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t0 + u * STEP < job.rows && pv.is_page(before[at[u] >> pv.log_p]) && pv.is_page(to[u])) row[u].store(pv, to[u], t0 + u * STEP, lane);
+    }
+    commit_head(pv, a, job, head, before);
 }
 
 }  // namespace
@@ -281,6 +340,11 @@ hipError_t launch_pages_keep(const PageView& pv, const int32_t* indices, const i
     const KeepSpace a = keep_space(pv, total_rows, workspace, nullptr);
     hipLaunchKernelGGL(keep_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, pv, indices, cu_budgets, (int)total_rows, a, refused);
     hipError_t e = hipGetLastError();
+    if ((long long)pv.width << pv.log_p <= kWholeRows) {
+        if (e != hipSuccess) return e;
+        AUDIOKV_FOR_DIM(pv.D, hipLaunchKernelGGL(keep_whole_kernel<kD>, dim3(pv.n_heads), dim3(kWholeThreads), 0, s, pv, indices, cu_budgets, a))
+        return hipGetLastError();
+    }
     const int rows_per_block = kThreads / (pv.D / 32);
     const long long slab = (long long)rows_per_block << 22;
     for (long long first = 0; first < total_rows && e == hipSuccess; first += slab) {

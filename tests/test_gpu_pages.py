@@ -81,6 +81,19 @@ def test_append_to_given_sequences(A):
         same(c, pages)
 
 
+def test_append_to_a_few_of_many_sequences(A):
+    """More sequences than the small plan keeps owners of, and more items than it has threads: the general one, with sequences named
+    twice."""
+    r = np.random.default_rng(20)
+    c = cache(r, 5000, 1, 64, 32, r.integers(0, 70, 5000), spare=2600)
+    c.fork(np.where(np.arange(5000) % 7 == 3, np.arange(5000) - 1, np.arange(5000)))
+    pages = upload(A, c)
+    for seqs in ([4999, 17, 4999, -1], r.integers(-3, 5003, 1300)):
+        s = Source(r, 1, 64, r.integers(1, 4, len(seqs)))
+        assert s.call(A, c, pages, seqs) == c.append(s.items(), seqs) == 0
+        same(c, pages)
+
+
 def test_more_items_than_sequences(A):
     r = np.random.default_rng(2)
     c = cache(r, 2, 1, 64, 32, [3, 64], spare=9, max_pages=9)
