@@ -171,22 +171,19 @@ class Pages:
         return self.lengths.numel() // p.n_kv_heads
 
     def _c(self, p: Params, at: int) -> _CPages:
-        """The C struct, after a look at types, sizes and the device."""
+        """The C struct, after a look at types, sizes and the device (in one expression, as Slots does)."""
         pool, table, lengths, refs, state = self.pool, self.table, self.lengths, self.refs, self.state
-        heads, n_pages = lengths.numel(), refs.numel()
-        if heads % p.n_kv_heads:
-            raise ValueError(f"pages.lengths has {heads} values, which is no number of sequences of {p.n_kv_heads} KV heads")
-        for t, name in ((table, "table"), (lengths, "lengths"), (refs, "refs"), (state, "state")):
-            if t.dtype is not _I32 or t.get_device() != at or not t.is_contiguous():
-                raise ValueError(f"pages.{name} must be a contiguous tensor of dtype {_I32} on the current device, {at}")
-        if table.dim() != 2 or table.shape[0] != heads:
-            raise ValueError(f"pages.table must be [{heads}, entries], one row per head in pages.lengths")
-        if state.numel() != 2:
-            raise ValueError("pages.state must have two values")
-        if pool.dtype is not _U8 or pool.get_device() != at or not pool.is_contiguous() or pool.numel() < n_pages * self.page_rows * p.head_dim * 17 // 16:
-            raise ValueError(f"pages.pool must be a contiguous tensor of {n_pages} pages, {n_pages * self.page_rows * p.head_dim * 17 // 16} values of "
-                             f"dtype {_U8}, on the current device, {at}")
-        return _CPages(_PAGES_SIZE, self.page_rows, n_pages, table.shape[1], pool.data_ptr(), table.data_ptr(), lengths.data_ptr(),
+        heads, n_pages, size = lengths.numel(), refs.numel(), table.shape
+        need = n_pages * self.page_rows * p.head_dim * 17 // 16
+        if (heads % p.n_kv_heads or len(size) != 2 or size[0] != heads or state.numel() != 2 or pool.numel() < need or pool.dtype is not _U8
+                or not (table.dtype is lengths.dtype is refs.dtype is state.dtype is _I32)
+                or not (pool.get_device() == table.get_device() == lengths.get_device() == refs.get_device() == state.get_device() == at)
+                or not (pool.is_contiguous() and table.is_contiguous() and lengths.is_contiguous() and refs.is_contiguous()
+                        and state.is_contiguous())):
+            raise ValueError(f"pages: lengths must be one value for each of {p.n_kv_heads} KV heads of every sequence, table [{heads}, entries], "
+                             f"state two values, refs one value per page, all {_I32}, and pool {need} values of {_U8}: contiguous tensors on "
+                             f"the current device, {at}")
+        return _CPages(_PAGES_SIZE, self.page_rows, n_pages, size[1], pool.data_ptr(), table.data_ptr(), lengths.data_ptr(),
                        refs.data_ptr(), state.data_ptr())
 
     def _sizes(self) -> _CPages:
@@ -720,8 +717,8 @@ def _values(t: Optional[torch.Tensor], n: int, dtype, at: int, name: str) -> Opt
     """The address of a tensor of n values or more, if given."""
     if t is None:
         return None
-    if _need_at(t, dtype, at, name).numel() < n:
-        raise ValueError(f"{name} has {t.numel()} values, {n} needed")
+    if t.dtype is not dtype or t.get_device() != at or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name} must be a contiguous tensor of {n} values of dtype {dtype} on the current device, {at}")
     return t.data_ptr()
 
 
@@ -744,7 +741,7 @@ def pages_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, seql
     cg = pages._c(p, at)
     n_seqs, n_items, heads, lens = pages.n_seqs(p), len(seqlens), len(seqlens) * p.n_kv_heads, _host_lens(seqlens)
     _need_at(k, _BF16, at, "k"); _need_at(v, _BF16, at, "v")
-    rows = sum(lens) * p.n_kv_heads
+    rows = int(sum(seqlens)) * p.n_kv_heads
     end = rows * p.head_dim if p.kv_stride_tok == 0 else _rows_end(p, seqlens)
     if _room(p, k) < end or _room(p, v) < end:
         raise ValueError(f"k or v has room for {min(_room(p, k), _room(p, v))} values, {end} needed")
