@@ -62,8 +62,8 @@ def build(jobs: int = 8, verbose: bool = True) -> str:
 
 # Sources whose host code carries the library's own logic (argument validation, workspace and launch planning):
 # the sanitizer build instruments these and links the other objects as they are.
-SANITIZED = ["accumulate.hip", "api.hip", "evict_accumulated.hip", "score.hip", "shared.hip"]
-CHECKERS = ["abi_host_check", "abi_accumulated_check", "abi_accumulated_limits_check"]
+SANITIZED = ["accumulate.hip", "api.hip", "evict_accumulated.hip", "pages_attend.hip", "pages_share.hip", "pages_store.hip", "score.hip", "shared.hip"]
+CHECKERS = ["abi_host_check", "abi_accumulated_check", "abi_accumulated_limits_check", "abi_pages_check"]
 SAN_FLAGS = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
              "-Xarch_host", "-fno-sanitize-recover=undefined"]
 

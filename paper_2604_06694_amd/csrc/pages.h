@@ -42,7 +42,21 @@ __host__ __device__ __forceinline__ int scale_of(unsigned top) {
     return top >= 0x7f80 ? 255 : e < 2 ? 2 : e > 252 ? 252 : e;
 }
 
-// Rows of queues: largest g with cu[g] * times <= p (cu is a non-decreasing exclusive scan; p uniform). Every round probes 64 entries
+// How the units of attend are shared out (pages_attend.hip).
+// n units in k shares: where share w begins, and which one has unit u. Spread evenly, so that equal heads and a multiple of their number of
+// shares end together. In float64, where both are exact: numerators are below 2^42, and a quotient that is no whole number is at least
+// 2^-31 away from one. (Divisions of 64-bit integers took 130 instructions each.)
+struct Shares {
+    int n, k;
+    __host__ __device__ __forceinline__ int begin(int w) const { return (int)((double)n * w / k); }
+    __host__ __device__ __forceinline__ int of(int u) const { return (int)((((double)u + 1) * k - 1) / n); }
+};
+
+// A workgroup has the parts of two heads at most, and a slot for each: 2 w for the one with which its share begins, 2 w + 1 for another.
+// Part p of a head whose first part is in slot `first`: the others are the first of the workgroups behind.
+__host__ __device__ __forceinline__ int part_slot(int first, int p) { return p == 0 ? first : (first & ~1) + 2 * p; }
+
+// Largest g with cu[g] * times <= p (cu is a non-decreasing exclusive scan; p uniform). Every round probes 64 entries
 // at equal distances, one per lane: one load latency for up to 64 of them, two up to 4096.
 __device__ __forceinline__ int owner_of_row(const int32_t* __restrict__ cu, int n, int times, long long p) {
     int head = 0;
@@ -150,6 +164,11 @@ struct PageSearch {
 };
 
 inline size_t up256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }    // parts of a workspace begin at multiples of 256 bytes
+
+// Part of a workspace; without one (a size is asked for) there is no address.
+template <class T> T* part_at(void* workspace, size_t offset) {
+    return workspace ? reinterpret_cast<T*>(static_cast<char*>(workspace) + offset) : nullptr;
+}
 
 // CALL with kD, the head's channels, a constant
 #define AUDIOKV_FOR_DIM(D, CALL)                                 \

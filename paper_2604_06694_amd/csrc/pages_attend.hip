@@ -245,15 +245,6 @@ __device__ __forceinline__ int next_with_rows(const PageView& pv, int head) {
 
 __device__ __forceinline__ int units_of(int rows) { return (rows + kUnit - 1) / kUnit; }
 
-// n units in k shares: where share w begins, and which one has unit u. Spread evenly, so that equal heads and a multiple of their number of
-// shares end together. In float64, where both are exact: numerators are below 2^42, and a quotient that is no whole number is at least
-// 2^-31 away from one. (Divisions of 64-bit integers took 130 instructions each.)
-struct Shares {
-    int n, k;
-    __device__ __forceinline__ int begin(int w) const { return (int)((double)n * w / k); }
-    __device__ __forceinline__ int of(int u) const { return (int)((((double)u + 1) * k - 1) / n); }
-};
-
 constexpr int kAlignedUnits = 4;      // one more for each wave
 
 // waves of a SIMD: what two units on their way leave registers for
@@ -494,8 +485,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Geom g, __bf16* __restri
     const size_t row = (size_t)from.x * G + n;                              // (query heads of a KV head are neighbours)
     __shared__ float weight[kMaxWorkgroups], wave_m[WAVES], wave_l[WAVES];
     __shared__ __attribute__((aligned(16))) f32x4 red[kThreads];
-    // part p of the head: the first where the head began, the others the first of the workgroups behind
-    auto slot_of = [&](int p) { return p == 0 ? from.y : (from.y & ~1) + 2 * p; };
+    auto slot_of = [&](int p) { return part_slot(from.y, p); };
     const int ch = tid % QUADS * 4, grp = tid / QUADS;
     auto part = [&](int p) { return *reinterpret_cast<const f32x4*>(a.parts + ((size_t)slot_of(p) * G + n) * D + ch); };
     f32x4 early[kEarly];
@@ -562,12 +552,12 @@ int joins(const Geom& g, const PageView& pv) { return std::min(pv.n_heads, workg
 AttendSpace attend_space(const Geom& g, const PageView& pv, void* workspace, size_t* bytes) {
     AttendSpace a;
     const size_t slots = 2 * (size_t)workgroups(g, pv);
-    char* at = static_cast<char*>(workspace);
-    a.joins = reinterpret_cast<int4*>(at);
-    size_t off = up256((size_t)joins(g, pv) * sizeof(int4));
-    a.stats = reinterpret_cast<float*>(at + off);
+    size_t off = 0;
+    a.joins = part_at<int4>(workspace, off);
+    off += up256((size_t)joins(g, pv) * sizeof(int4));
+    a.stats = part_at<float>(workspace, off);
     off += up256(slots * g.G * 2 * sizeof(float));
-    a.parts = reinterpret_cast<float*>(at + off);
+    a.parts = part_at<float>(workspace, off);
     off += slots * g.G * g.D * sizeof(float);
     if (bytes) *bytes = off;
     return a;

@@ -27,7 +27,7 @@ ForkSpace fork_space(const PageView& pv, void* workspace, size_t* bytes) {
     ForkSpace f;
     f.rows = static_cast<int32_t*>(workspace);
     const size_t at = up256((size_t)pv.n_heads * 4);
-    f.entries = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + at);
+    f.entries = part_at<int32_t>(workspace, at);
     if (bytes) *bytes = at + up256((size_t)pv.n_heads * pv.width * 4);
     return f;
 }
@@ -132,7 +132,7 @@ KeepSpace keep_space(const PageView& pv, long long total_rows, void* workspace, 
     KeepSpace a;
     a.jobs = static_cast<KeepJob*>(workspace);
     const size_t at = up256((size_t)pv.n_heads * sizeof(KeepJob));
-    a.found = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + at);
+    a.found = part_at<int32_t>(workspace, at);
     const long long n = (total_rows >> pv.log_p) + pv.n_heads;       // a head's last page may be begun
     a.most = (int)(n < pv.n_pages ? n : pv.n_pages);
     if (bytes) *bytes = at + up256((size_t)a.most * 4);

@@ -41,14 +41,14 @@ AppendSpace append_space(const PageView& pv, int n_seqs, int n_items, long long 
     AppendSpace a{};
     const long long heads = (long long)n_items * pv.H;
     a.most = (int)most_pages(pv, heads, total_rows);
-    char* at = static_cast<char*>(workspace);
-    a.jobs = reinterpret_cast<AppendJob*>(at);
-    size_t off = up256((size_t)heads * sizeof(AppendJob));
-    a.bad = reinterpret_cast<int32_t*>(at + off);
+    size_t off = 0;
+    a.jobs = part_at<AppendJob>(workspace, off);
+    off += up256((size_t)heads * sizeof(AppendJob));
+    a.bad = part_at<int32_t>(workspace, off);
     off += up256((size_t)n_items * 4);
-    a.owner = reinterpret_cast<int32_t*>(at + off);
+    a.owner = part_at<int32_t>(workspace, off);
     off += up256((size_t)n_seqs * 4);
-    a.found = reinterpret_cast<int32_t*>(at + off);
+    a.found = part_at<int32_t>(workspace, off);
     off += up256((size_t)a.most * 4);
     if (bytes) *bytes = off;
     return a;
