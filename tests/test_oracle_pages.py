@@ -40,6 +40,15 @@ def test_codes_by_hand(y, magnitude):
     assert O.code_of(-y) == O.code_of(y) + 8
 
 
+def test_ties_of_rows_are_those_of_single_values():
+    x = np.array([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5, 7, 6.5, 0.1, 0, 1, 2, 3, 4, 6])
+    row = np.concatenate([x, -x, x / 8, -x / 4 * 1.5])
+    codes, es = O.encode(row[None])
+    c, e = O.encode_block(row[:32])
+    assert es[0].tolist() == [127, O.scale_byte(row[32:])] and e == 127
+    assert c.tolist() == [O.code_of(v) for v in row[:32]] and np.array_equal(codes[0, :16], c[::2] | c[1::2] << 4)
+
+
 def test_what_is_held_is_the_nearest_that_can_be():
     """Against all 15 values that a block's scale allows; and twice through the format is once."""
     r = np.random.default_rng(1)
@@ -142,6 +151,16 @@ def test_what_there_are_no_pages_for():
     assert list(c.lengths) == [64, 0, 0] and c.free == 2
     assert c.append([[rows(r, 5, 64)], [rows(r, 5, 64)], [rows(r, 5, 64)]], [1, 1, 7]) == 0      # twice the same, and none
     assert list(c.lengths) == [64, 5, 0]
+
+
+def test_a_copy_needs_a_page():
+    r = np.random.default_rng(7)
+    c = O.Cache(2, 1, 64, 2, 3, 32)
+    c.append([[rows(r, 40, 64)]])
+    c.fork([0, 0])
+    assert c.append([[rows(r, 1, 64)]], [1]) == 1 and list(c.lengths) == [40, 40] and c.free == 0
+    c.fork([0, -1])
+    assert c.append([[rows(r, 1, 64)]], [0]) == 0 and c.lengths[0] == 41          # not shared any more
 
 
 def test_attention_written_out():
