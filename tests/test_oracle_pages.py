@@ -143,6 +143,18 @@ def test_keep_by_hand():
     assert c.keep([list(range(40))]) == 0 and c.lengths[0] == 35
 
 
+def test_kept_rows_are_those_that_were_asked_for():
+    r = np.random.default_rng(8)
+    c = O.Cache(1, 2, 64, 30, 6, 32)
+    c.append([[rows(r, 130, 64), rows(r, 101, 64)]])
+    before = [c.rows(0), c.rows(1)]
+    index = [np.sort(r.choice(130, 97, replace=False)), np.arange(64)]
+    assert c.keep(index) == 0
+    sound(c)
+    for g in range(2):
+        assert all(np.array_equal(a, b[index[g]]) for a, b in zip(c.rows(g), before[g]))
+
+
 def test_what_there_are_no_pages_for():
     r = np.random.default_rng(5)
     c = O.Cache(3, 1, 64, 4, 3, 32)
