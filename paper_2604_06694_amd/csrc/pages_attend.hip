@@ -245,7 +245,9 @@ __device__ __forceinline__ int next_with_rows(const PageView& pv, int head) {
 
 __device__ __forceinline__ int units_of(int rows) { return (rows + kUnit - 1) / kUnit; }
 
-constexpr int kAlignedUnits = 4;      // one more for each wave
+// By how many units the largest share may grow so that shares end with heads: one for each wave. (64 ragged heads 16.3 -> 15.1 us, 12 at
+// D = 256 16.6 -> 14.9; 64 equal heads, which end together anyway, 12.3 -> 13.4, for the sum over heads is formed twice.)
+constexpr int kAlignedUnits = 4;
 
 // waves of a SIMD: what two units on their way leave registers for
 template <int D> constexpr int kResident = D == 64 ? 4 : D == 128 ? 3 : 2;
@@ -293,14 +295,14 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kRes
         if (total == 0) return;
         // Workgroups that have parts of two heads work on them one after the other, some 3 us. Where shares that end with the heads are
         // not much larger, there are those instead: of `share` units at most.
-        const int share = 2 * pv.n_heads <= wgs ? max((total + wgs - pv.n_heads - 1) / (wgs - pv.n_heads), WAVES) : INT_MAX;
+        const int share = 2 * pv.n_heads <= wgs ? max((int)(((unsigned)total + wgs - pv.n_heads - 1) / (wgs - pv.n_heads)), WAVES) : INT_MAX;
         const bool aligned = share - kAlignedUnits <= total / wgs;
         if (aligned) {
             mine = 0;
             for (int h = h0; h < h1; ++h) mine += (units_of(pv.length(h)) + share - 1) / share;
             before = exclusive_sum_once<THREADS>(mine, sums + WAVES, W);
         } else {
-            W = min(wgs, (total + WAVES - 1) / WAVES);
+            W = min(wgs, total / WAVES + 1);
         }
         if (b >= W) return;
         // the head in which this workgroup's share begins: `at` units (or workgroups) are before it
@@ -533,10 +535,14 @@ __global__ __launch_bounds__(kThreads) void join_kernel(Geom g, __bf16* __restri
 }
 
 template <int D> constexpr int kWholeWaves = 4 * kResident<D>;
-// Heads of at most this many rows go to a workgroup each, of as many waves as a CU holds, and there is no second launch.
-constexpr long long kWholeRows = 2048;
-constexpr int kWholeHeads = 512;
-bool whole_heads(const PageView& pv) { return ((long long)pv.width << pv.log_p) <= kWholeRows && pv.n_heads <= kWholeHeads; }
+// Short heads go to a workgroup each, of as many waves as a CU holds, and there is no second launch. By what a table can hold, since
+// lengths are not known here. Kernel times of whole heads, and in parts with the join: 4 heads of 500 rows 6.8, 9.3 us, of 2000 12.2, 11.5
+// (and the host launches once, some 3 us less), 64 of 2000 13.2, 13.5, 256 of 500 8.1, 15.2, 256 of 2000 16.1, 22.3, 512 of 500 14.8, 20,
+// 1792 of 500 47.7, 38; at D = 256, where a CU holds eight waves, 16 of 500 11.1, 10.6, of 1000 14.3, 11.5, but 256 of 1500 21.6, 26.3.
+bool whole_heads(const PageView& pv) {
+    const long long rows = (long long)pv.width << pv.log_p;
+    return pv.n_heads <= 512 && rows <= (pv.D < 256 || pv.n_heads >= 128 ? 2048 : 512);
+}
 
 // Workgroups: as many as the registers let run at once, so that equal shares end together
 int workgroups(const Geom& g, const PageView& pv) {

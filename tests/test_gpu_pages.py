@@ -317,6 +317,15 @@ def test_attend(A, d, P, G):
 
 
 @pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("G", [1, 8, 9, 16])
+def test_attend_short_tables(A, d, G):
+    """A workgroup per head: few heads, and more of them with longer tables."""
+    r = np.random.default_rng(d + G)
+    attend(A, cache(r, 4, 3, d, 32, [0, 1, 2, 31, 32, 33, 63, 64, 65, 257, 400, 512], max_pages=16), G, r)
+    attend(A, cache(r, 50, 3, d, 128, np.where(r.random(150) < 0.8, r.integers(0, 60, 150), r.integers(0, 2049, 150)), max_pages=16), G, r)
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
 @pytest.mark.parametrize("G", [1, 7, 16])
 @pytest.mark.parametrize("P", [32, 128])
 def test_attend_heads_in_parts(A, d, G, P):
