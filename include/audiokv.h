@@ -488,10 +488,11 @@ int32_t audiokv_page_bytes(const audiokv_params* params, int32_t page_rows, size
 /* Rounds rows of K and V to 4 bits and puts them behind the rows that their heads have.
  * k, v, cu_seqlens_dev, seqlens_host, n_items: as for audiokv_compact (the kv_layout or
  * the strides of params; lengths L_i >= 1). Head h of item i gets rows indices[cu_budgets[g]
- * + t] of it, g = i * n_kv_heads + h, as audiokv_select / _evict write them; indices and
- * cu_budgets NULL: all L_i rows (a step's new row per sequence: n_items of length 1).
- * total_rows (host): the sum of the budgets, or of L_i * n_kv_heads; without indices the
- * call computes it and the argument is not used.
+ * + t] of it, g = i * n_kv_heads + h, as audiokv_select / _evict write them (of no rows at
+ * all indices may be NULL); without cu_budgets (NULL, as indices then): all L_i rows (a
+ * step's new row per sequence: n_items of length 1). total_rows (host): the sum of the
+ * budgets, or of L_i * n_kv_heads; without cu_budgets the call computes it and the
+ * argument is not used.
  * seqs_dev: the sequence of every item (int32 [n_items]), or NULL: item i is sequence i,
  * n_items <= n_seqs. An item takes no part where that is outside [0, n_seqs), or a
  * sequence that an item before it has named: a batch of fixed size can be captured into

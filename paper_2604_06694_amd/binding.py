@@ -746,7 +746,7 @@ def pages_append(p: Params, pages: Pages, k: torch.Tensor, v: torch.Tensor, seql
     if _room(p, k) < end or _room(p, v) < end:
         raise ValueError(f"k or v has room for {min(_room(p, k), _room(p, v))} values, {end} needed")
     _table(cu_seqlens, n_items, at, "cu_seqlens"); _table(cu_budgets, heads, at, "cu_budgets")
-    if indices is None:
+    if cu_budgets is None:
         total_rows = rows
     idx, to, no = (_values(indices, total_rows, _I32, at, "indices"), _values(seqs, n_items, _I32, at, "seqs"),
                    _values(refused, 1, _I32, at, "refused"))

@@ -966,9 +966,12 @@ int32_t audiokv_pages_append(const audiokv_params* params, const audiokv_pages* 
     audiokv_params any_window = *params;
     any_window.window = 0;
     AUDIOKV_TRY(check_batch(&any_window, n_items, seqlens_host, &b));
-    if ((indices_dev == nullptr) != (cu_budgets_dev == nullptr))
-        return fail(AUDIOKV_E_INVALID_ARG, "indices and cu_budgets come together");
-    if (!indices_dev) total_rows = b.total_tokens * params->n_kv_heads;
+    if (!cu_budgets_dev) {
+        if (indices_dev) return fail(AUDIOKV_E_INVALID_ARG, "indices need cu_budgets");
+        total_rows = b.total_tokens * params->n_kv_heads;
+    } else if (!indices_dev && total_rows != 0) {              // (of no rows, indices have no address)
+        return fail(AUDIOKV_E_INVALID_ARG, "cu_budgets and total_rows %lld need indices", (long long)total_rows);
+    }
     AUDIOKV_TRY(check_append(pv, n_items, total_rows));
     if (total_rows > b.total_tokens * params->n_kv_heads)
         return fail(AUDIOKV_E_INVALID_ARG, "total_rows %lld: the items have %lld", (long long)total_rows, b.total_tokens * params->n_kv_heads);

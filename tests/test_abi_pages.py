@@ -73,12 +73,13 @@ def test_no_sequences(A, call):
 def test_append_refusals(A):
     p = A.Params(8, 2, 64, 0)
     for bad in (dict(k=None), dict(v=None), dict(cu=None), dict(k=ODD), dict(v=ODD), dict(lens=None, items=2), dict(lens=(5, 0)),
-                dict(lens=(5, -1)), dict(items=-1), dict(idx=PTR), dict(cu_b=PTR), dict(lens=(1,) * 5),       # five items, four sequences
+                dict(lens=(5, -1)), dict(items=-1), dict(idx=PTR), dict(cu_b=PTR, rows=5), dict(cu_b=PTR, rows=-1), dict(lens=(1,) * 5),       # five items, four sequences
                 dict(idx=PTR, cu_b=PTR, rows=-1), dict(idx=PTR, cu_b=PTR, rows=25), dict(ws=None), dict(ws=ODD)):
         assert append(A, p, cache(A), **bad) == -1, bad
     assert append(A, p, cache(A), size=64) == -3
     assert append(A, p, cache(A), lens=(1,) * 5, seqs=PTR, size=64) == -3
     assert append(A, p, cache(A), idx=PTR, cu_b=PTR, rows=24, size=64) == -3
+    assert append(A, p, cache(A), cu_b=PTR, rows=0, size=64) == -3                # budgets of zero: no indices
     assert append(A, p, cache(A), lens=(2**30, 2**30)) == -2
     assert append(A, A.Params(8, 2, 64, 0, kv_stride_head=640, kv_stride_tok=64), cache(A)) == -1     # two items, no item stride
     assert append(A, p, cache(A), lens=(), k=None, v=None, cu=None, ws=None) == 0

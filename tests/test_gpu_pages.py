@@ -70,6 +70,17 @@ def test_append_sizes(A, H, n, lens):
     same(c, pages)
 
 
+def test_append_to_the_first_sequences_and_of_nothing(A):
+    """Fewer items than sequences; budgets of zero, of some heads, of an item, of all."""
+    r = np.random.default_rng(21)
+    c = cache(r, 5, 2, 64, 32, [3, 64, 31, 0, 20, 90, 32, 1, 64, 7], spare=30, max_pages=9)
+    pages = upload(A, c)
+    for lens, kept in (([40, 3], None), ([40, 33, 20], [0, 7, 0, 0, 20, 0]), ([5, 9], [0])):
+        s = Source(r, 2, 64, lens, kept)
+        assert s.call(A, c, pages) == c.append(s.items()) == 0
+        same(c, pages)
+
+
 def test_append_to_given_sequences(A):
     """In any order; a sequence that is none, and one named twice: the first item that does."""
     r = np.random.default_rng(1)
@@ -348,6 +359,29 @@ def test_attend_many_heads(A, d):
     lengths = np.where(r.random(900) < 0.7, 0, r.integers(1, 90, 900))
     lengths[[0, 400, 899]] = 800, 1200, 0
     attend(A, cache(r, 300, 3, d, 32, lengths), 2, r)
+
+
+@pytest.mark.parametrize("d,G", [(64, 4), (64, 16), (128, 7), (128, 12), (256, 2), (256, 9)])
+def test_attend_in_a_large_pool(A, d, G):
+    """A pool that the memory-side cache does not hold: rows are streamed."""
+    r = np.random.default_rng(d + G)
+    c = cache(r, 3, 2, d, 64, [0, 1, 33, 700, 2900, 1025], max_pages=64)
+    pages = upload(A, c)
+    n = (300 << 20) // c.page_bytes
+    pool = torch.zeros(n * c.page_bytes, dtype=torch.uint8, device="cuda")
+    pool[:pages.pool.numel()] = pages.pool
+    pages.pool, pages.refs = pool, torch.cat((pages.refs, torch.zeros(n - c.n_pages, dtype=torch.int32, device="cuda")))
+    q = bf16(r.standard_normal((3, 2 * G, d)) * 2.0 ** -6).cuda()
+    lse = torch.empty((3, 2 * G), device="cuda")
+    out = A.pages_attend(params(A, c, G), pages, q, lse=lse)
+    attend_error(c, values(q), d ** -0.5, values(out), values(lse))
+
+
+@pytest.mark.parametrize("d,H,lengths", [(64, 1, [300_000]), (128, 2, [100_000, 5]), (256, 1, [60_001])])
+def test_attend_one_long_head(A, d, H, lengths):
+    """As many parts of a head as there are workgroups."""
+    r = np.random.default_rng(d)
+    attend(A, cache(r, 1, H, d, 256, lengths), 1, r)
 
 
 @pytest.mark.parametrize("q_scale,scale", [(2.0 ** -2, None), (8.0, None), (64.0, None), (2.0 ** -6, 1.0), (2.0 ** -6, 1e-6)])

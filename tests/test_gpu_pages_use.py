@@ -126,6 +126,53 @@ def test_a_captured_step_is_replayed(A):
         attend_error(other, values(q), d ** -0.5, values(eager))
 
 
+@pytest.mark.parametrize("n,most", [(3, 40), (40, 90)])
+def test_captured_cuts_are_replayed(A, n, most):
+    """keep and read in a graph, with small and large tables, filled by indices and budgets; a fork eagerly between the replays."""
+    r = np.random.default_rng(n)
+    H, d, P = 2, 64, 32
+    c = cache(r, n, H, d, P, r.integers(900, 1200, n * H), spare=n * H * 120, max_pages=most)
+    p, pages = params(A, c), upload(A, c)
+    total = int(c.lengths.sum())
+    idx, cus, refused = ints(np.zeros(total)), ints(np.zeros(n * H + 1)), ints([0])
+    k, v = (torch.zeros((total, d), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    ws = torch.randint(0, 255, (max(A.pages_keep_workspace_bytes(p, pages, total), A.pages_fork_workspace_bytes(p, pages)),), dtype=torch.uint8, device="cuda")
+
+    def step():
+        A.pages_keep(p, pages, idx, cus, total, refused=refused, workspace=ws)
+        A.pages_read(p, pages, cus, total, k_out=k, v_out=v)
+
+    def fill(kept):
+        idx[:sum(len(x) for x in kept)] = ints(np.concatenate(kept))
+        cus.copy_(cu([len(x) for x in kept]))
+
+    fill([np.arange(int(m)) for m in c.lengths])          # (a head that keeps all of its rows stays as it is)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    same(c, pages)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for turn in range(4):
+        kept = [np.sort(r.choice(m, m - int(r.integers(0, 60)), replace=False)) for m in c.lengths]
+        fill(kept)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert c.keep(kept) == int(refused) == 0
+        same(c, pages)
+        counts = [len(x) for x in kept]
+        for got, ref in zip((k, v), c.read([0] * (n * H), counts) if turn == 0 else (None, None)):
+            assert ref is None or np.array_equal(values(got[:sum(counts)]), ref)
+        parents = r.integers(0, n, n)
+        A.pages_fork(p, pages, ints(parents), workspace=ws)
+        c.fork(parents)
+        same(c, pages)
+
+
 def test_on_another_stream(A):
     r = np.random.default_rng(2)
     c = cache(r, 3, 2, 64, 32, [40, 31, 64], spare=50, max_pages=9)
