@@ -506,7 +506,7 @@ int32_t audiokv_page_bytes(const audiokv_params* params, int32_t page_rows, size
  * that max_pages refuses) are more than there are free, gets no rows, and neither does
  * one of which a head would need more than max_pages. Their heads stay as they are;
  * refused_dev (int32, or NULL) becomes the number of heads that should have got rows so
- * and did not. */
+ * and did not (with n_items = 0 nothing is enqueued, and it stays what it was). */
 int32_t audiokv_pages_append_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,
                                              int32_t n_items, int64_t total_rows, size_t* out_bytes);
 int32_t audiokv_pages_append(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,

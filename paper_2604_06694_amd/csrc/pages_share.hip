@@ -74,16 +74,18 @@ __global__ __launch_bounds__(kThreads) void fork_give_kernel(PageView pv, const 
     if ((threadIdx.x & 63) == 63 && freed > 0) atomicAdd(&pv.state[0], freed);
 }
 
-// Both for small tables, U entries a thread of one workgroup: what the first launch lists is in registers here.
-constexpr int kForkEntries = 4;       // 4096 entries: 16 heads of 17 pages 3.6 + 3.4 us by the two kernels, 4.6 by this one
+// Both for small tables, U entries a thread of one workgroup: what the first launch lists is in registers here. (Entries of tables, us by
+// the two kernels and by this one: 272 3.4 + 3.2, 2.8; 1024 3.4 + 3.2, 3.9; 2048 3.7 + 3.2, 6.5, and a launch less; 4096 3.6 + 3.3, 14.)
+constexpr int kForkEntries = 2;
 
+template <int U>
 __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageView pv, const int32_t* __restrict__ parents,
                                                                   const int32_t* __restrict__ drop, int n_seqs)
 {
     const int entries = pv.n_heads * pv.width;
-    int rows[kForkEntries], was[kForkEntries], before[kForkEntries], now[kForkEntries];
+    int rows[U], was[U], before[U], now[U];
 #pragma unroll
-    for (int u = 0; u < kForkEntries; ++u) {
+    for (int u = 0; u < U; ++u) {
         const int e = min((int)threadIdx.x + u * kPlanThreads, entries - 1), head = e / pv.width, j = e - head * pv.width;
         const int x = head / pv.H, h = head - x * pv.H;
         const int parent = parents ? parents[x] : x;
@@ -96,12 +98,12 @@ __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageView pv, c
         now[u] = j < pv.pages_of(rows[u]) ? theirs : -1;
     }
 #pragma unroll
-    for (int u = 0; u < kForkEntries; ++u)
+    for (int u = 0; u < U; ++u)
         if ((int)threadIdx.x + u * kPlanThreads < entries && now[u] != before[u] && pv.is_page(now[u])) atomicAdd(&pv.refs[now[u]], 1);
     __syncthreads();          // all new owners are counted, and all of the table is read
     int freed = 0;
 #pragma unroll
-    for (int u = 0; u < kForkEntries; ++u) {
+    for (int u = 0; u < U; ++u) {
         const int e = threadIdx.x + u * kPlanThreads;
         if (e >= entries) break;
         const int head = e / pv.width, j = e - head * pv.width;
@@ -139,18 +141,19 @@ KeepSpace keep_space(const PageView& pv, long long total_rows, void* workspace, 
     return a;
 }
 
-__global__ __launch_bounds__(kPlanThreads) void keep_plan_kernel(PageView pv, const int32_t* __restrict__ indices,
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void keep_plan_kernel(PageView pv, const int32_t* __restrict__ indices,
                                                                  const int32_t* __restrict__ cu_b, int total_rows, KeepSpace a,
                                                                  int32_t* __restrict__ refused)
 {
-    __shared__ int sums[kPlanThreads / 64 + 1];
+    __shared__ int sums[THREADS / 64 + 1];
     __shared__ int served_pages, lost;
     const int tid = threadIdx.x, P = pv.rows();
-    PageSearch<kPlanThreads, 8> search(pv, pv.state[1]);
+    PageSearch<THREADS, THREADS == 256 ? 4 : 8> search(pv, pv.state[1]);
     if (tid == 0) served_pages = lost = 0;
     const int n_free = min(max(pv.state[0], 0), a.most);
     int running = 0;
-    for (int base = 0; base < pv.n_heads; base += kPlanThreads) {
+    for (int base = 0; base < pv.n_heads; base += THREADS) {
         const int head = base + tid;
         KeepJob job{-1, 0, 0, 0};
         int need = 0;
@@ -159,14 +162,20 @@ __global__ __launch_bounds__(kPlanThreads) void keep_plan_kernel(PageView pv, co
             job.had = pv.length(head);
             if (rows < job.had) {
                 job.rows = rows;
-                // Rows come in order, none twice: where row r is index r, the ones before are theirs, too.
-                // (Eight places asked at once instead of one: a third of the rounds, but 512 lines for 64 heads in each, and one CU gets
-                // them no sooner: 11.8 -> 15.8 us.)
+                // Rows come in order, none twice: where row r is index r, the ones before are theirs, too. The first page and the
+                // last are asked together, for heads that keep a choice of their rows have no whole page, and heads that lose the
+                // last ones only such (64 heads of 8000 rows 14.9 -> 13.4 us, 16 of 30000 13.8 -> 11.9).
                 const int32_t* mine = indices + begin;
+                const auto whole = [&](int pages) { return mine[pages * P - 1] == pages * P - 1; };
                 int lo = 0, hi = rows >> pv.log_p;
+                if (hi > 0) {
+                    const bool first = whole(1), all = whole(hi);
+                    lo = all ? hi : first;
+                    hi = all || !first ? lo : hi - 1;
+                }
                 while (lo < hi) {
                     const int mid = (lo + hi + 1) >> 1;
-                    if (mine[mid * P - 1] == mid * P - 1) lo = mid;
+                    if (whole(mid)) lo = mid;
                     else hi = mid - 1;
                 }
                 job.same = lo;
@@ -174,7 +183,7 @@ __global__ __launch_bounds__(kPlanThreads) void keep_plan_kernel(PageView pv, co
             }
         }
         int total;
-        job.first = running + exclusive_sum<kPlanThreads>(need, sums, total);
+        job.first = running + exclusive_sum<THREADS>(need, sums, total);
         running += total;
         // Heads are served while the free pages last.
         if (job.first + need <= n_free) {
@@ -270,7 +279,7 @@ __global__ __launch_bounds__(kThreads) void keep_table_kernel(PageView pv, KeepS
 }
 
 // Both for heads whose tables hold kWholeRows rows at most, a workgroup each: the old entries wait in LDS, and no other workgroup reads
-// them. (16 heads of 1100 rows: 3.9 + 3.1 us by the two kernels, 5.7 by this one.)
+// them. (16 heads of 1100 rows: 3.4 + 3.1 us by the two kernels, 5.7 by this one, 256 of 2000 16.7 + 5.2 and 17.0.)
 constexpr long long kWholeRows = 2048;
 constexpr int kWholeThreads = 512;
 
@@ -317,8 +326,10 @@ hipError_t launch_pages_fork(const PageView& pv, const int32_t* parents, const i
 {
     const ForkSpace f = fork_space(pv, workspace, nullptr);
     const int n_seqs = pv.n_heads / pv.H;
-    if ((long long)pv.n_heads * pv.width <= kForkEntries * kPlanThreads) {
-        hipLaunchKernelGGL(fork_small_kernel, dim3(1), dim3(kPlanThreads), 0, s, pv, parents, drop, n_seqs);
+    const long long entries = (long long)pv.n_heads * pv.width;
+    if (entries <= kForkEntries * kPlanThreads) {
+        if (entries <= kPlanThreads) hipLaunchKernelGGL(fork_small_kernel<1>, dim3(1), dim3(kPlanThreads), 0, s, pv, parents, drop, n_seqs);
+        else hipLaunchKernelGGL(fork_small_kernel<kForkEntries>, dim3(1), dim3(kPlanThreads), 0, s, pv, parents, drop, n_seqs);
         return hipGetLastError();
     }
     hipLaunchKernelGGL(fork_take_kernel, dim3(pv.n_heads), dim3(kThreads), 0, s, pv, parents, drop, n_seqs, f);
@@ -338,7 +349,10 @@ hipError_t launch_pages_keep(const PageView& pv, const int32_t* indices, const i
                              int32_t* refused, void* workspace, hipStream_t s)
 {
     const KeepSpace a = keep_space(pv, total_rows, workspace, nullptr);
-    hipLaunchKernelGGL(keep_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, pv, indices, cu_budgets, (int)total_rows, a, refused);
+    if (pv.n_heads <= 256 && a.most <= 2048)
+        hipLaunchKernelGGL(keep_plan_kernel<256>, dim3(1), dim3(256), 0, s, pv, indices, cu_budgets, (int)total_rows, a, refused);
+    else
+        hipLaunchKernelGGL(keep_plan_kernel<kPlanThreads>, dim3(1), dim3(kPlanThreads), 0, s, pv, indices, cu_budgets, (int)total_rows, a, refused);
     hipError_t e = hipGetLastError();
     if ((long long)pv.width << pv.log_p <= kWholeRows) {
         if (e != hipSuccess) return e;

@@ -16,7 +16,10 @@ namespace audiokv {
 namespace {
 
 constexpr int kThreads = 256, kPlanThreads = 1024;
-constexpr long long kStreamBytes = 64LL << 20;      // of bf16 rows that pass the memory-side cache by
+// Bytes of bf16 rows, K and V, from which they pass the caches by. append (the rows written just before, or 2 sets in turn; us with and
+// without): 97 MB 23.2, 23.6 or 28.3, 23.3, 117 MB 26.9, 27.5 or 32.2, 31.8, 156 MB 34.9, 35.2 or 40.8, 44.6. read and a decoding step on
+// what it wrote: 4 MB 16.3, 15.8, 8 MB 17.4, 17.6, 16 MB 19.8, 20.7, 32 MB 24.9, 25.9, 62 MB 36.8, 37.8.
+constexpr long long kAppendStream = 128LL << 20, kReadStream = 8LL << 20;
 
 struct AppendJob {
     int start, rows;        // where the head's new rows begin, how many (0: nothing to do)
@@ -160,7 +163,7 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(
 
 // The same for up to THREADS heads, one a thread, and up to kSmallSeqs sequences: what is a pass over the workspace there is a register
 // or LDS here, and the counts of the first pages that the search looks at are loaded beside the rest. What is left is the chain item ->
-// sequence -> length -> table -> refs and the barriers. (192 heads: 12.2 us by the kernel above, 7.3 so.)
+// sequence -> length -> table -> refs and the barriers. (192 heads: 10.8 us by the kernel above, 5.9 so; 1000 heads: 16.9 and 13.3.)
 constexpr int kSmallSeqs = 4096;
 
 template <int THREADS>
@@ -465,7 +468,7 @@ hipError_t launch_pages_append(const Geom& g, const PageView& pv, const AppendCa
     // a launch holds fewer than 2^32 threads: rows beyond that take further ones. Copies go along with the first
     const int rows_per_block = kThreads / (g.D / 8);
     const long long slab = (long long)rows_per_block << 22;
-    const bool stream = c.total_rows * g.D * 4 > kStreamBytes;
+    const bool stream = c.total_rows * g.D * 4 > kAppendStream;
     for (long long first = 0; first < c.total_rows && e == hipSuccess; first += slab) {
         const long long rows = c.total_rows - first < slab ? c.total_rows - first : slab;
         const int per_block = rows_per_block * (stream ? kStreamRows : 1), blocks = (int)((rows + per_block - 1) / per_block);
@@ -493,7 +496,7 @@ hipError_t launch_pages_read(const PageView& pv, const int32_t* first_dev, const
 #define AUDIOKV_READ(STREAM)                                                                                                             \
     AUDIOKV_FOR_DIM(pv.D, hipLaunchKernelGGL((read_kernel<kD, STREAM>), grid, dim3(kThreads), 0, s, pv, first_dev, cu_rows, first,        \
                                              total_rows, (u32x4*)k_out, (u32x4*)v_out))
-        if (total_rows * pv.D * 4 > kStreamBytes) AUDIOKV_READ(true) else AUDIOKV_READ(false)
+        if (total_rows * pv.D * 4 > kReadStream) AUDIOKV_READ(true) else AUDIOKV_READ(false)
 #undef AUDIOKV_READ
         e = hipGetLastError();
     }
