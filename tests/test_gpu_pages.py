@@ -151,6 +151,33 @@ def test_append_beyond_a_table_row(A):
         same(c, pages)
 
 
+@pytest.mark.parametrize("d,lens", [(64, [30000, 1, 121222]), (128, [37000, 40001]), (256, [6, 21000, 18000])])
+@pytest.mark.parametrize("kept", [False, True])
+def test_append_of_many_rows_is_that_of_fewer_at_a_time(A, d, lens, kept):
+    """137 MB and more of K and V in one call, and item by item, below the size from which rows pass the caches by."""
+    g = torch.Generator(device="cuda").manual_seed(d)
+    H, P, ends = 4, 64, np.cumsum([0] + lens)
+    k, v = (torch.randn(int(ends[-1]) * H * d, device="cuda", generator=g).bfloat16() for _ in range(2))
+    p = A.Params(H, H, d, 0)
+    pages = [A.Pages.empty(p, len(lens), sum(-(-n // P) for n in lens) * H, -(-max(lens) // P), P) for _ in range(2)]
+    for c in pages:
+        c.pool.zero_()
+    r = np.random.default_rng(d)
+    rows = [[np.sort(r.choice(n, n - n // 9, replace=False)) if kept else np.arange(n) for _ in range(H)] for n in lens]
+
+    def call(c, items):
+        part = slice(int(ends[items[0]]) * H * d, int(ends[items[-1] + 1]) * H * d)
+        counts = [len(x) for i in items for x in rows[i]]
+        more = dict(indices=ints(np.concatenate([x for i in items for x in rows[i]])), cu_budgets=cu(counts), total_rows=sum(counts)) if kept else {}
+        A.pages_append(p, c, k[part], v[part], [lens[i] for i in items], seqs=ints(items), **more)
+    call(pages[0], list(range(len(lens))))
+    for i in range(len(lens)):
+        call(pages[1], [i])
+    for name in ("pool", "table", "lengths", "refs", "state"):
+        assert torch.equal(getattr(pages[0], name), getattr(pages[1], name)), name
+    assert pages[0].lengths.tolist() == [len(x) for item in rows for x in item]
+
+
 def test_append_searches_round_a_large_pool(A):
     """More pages than one round of the search looks at, few of them free, and the search begins near the end."""
     r = np.random.default_rng(6)
@@ -197,6 +224,16 @@ def test_read(A, d, P):
             assert (np.abs(got[small]) <= 2.0 ** -126).all()
 
 
+@pytest.mark.parametrize("d,rows", [(64, 33000), (128, 17001), (256, 8200)])
+def test_read_of_many_rows(A, d, rows):
+    r = np.random.default_rng(d)
+    lens = [rows // 2, 0, rows - rows // 2 - 777, 777]
+    c = cache(r, 2, 2, d, 64, lens)
+    k, v = A.pages_read(params(A, c), upload(A, c), cu(lens), rows)
+    for got, want in zip((k, v), c.read([0] * 4, lens)):
+        assert np.array_equal(values(got), want)
+
+
 def test_what_is_read_can_be_decoded_and_scored(A):
     """The way back: bf16 rows as compact packs them, for decode_attend and for accumulate."""
     r = np.random.default_rng(8)
@@ -226,6 +263,18 @@ def test_fork(A, seed):
             parents = np.where(r.random(n) < 0.3, np.arange(n), parents)
         drop = r.integers(-2, 90, n) if r.random() < 0.6 else None
         A.pages_fork(params(A, c), pages, None if parents is None else ints(parents), drop=None if drop is None else ints(drop))
+        c.fork(parents, drop)
+        same(c, pages)
+
+
+@pytest.mark.parametrize("n,H,entries", [(1, 1, 40), (32, 4, 8), (25, 3, 14), (64, 2, 16), (43, 3, 16), (9, 1, 228)])
+def test_fork_of_tables_of(A, n, H, entries):
+    r = np.random.default_rng(entries)
+    c = cache(r, n, H, 64, 32, r.integers(0, entries * 32 + 1, n * H), max_pages=entries)
+    pages = upload(A, c)
+    for parents in (r.integers(-1, n, n), r.permutation(n), np.zeros(n, dtype=np.int64)):
+        drop = r.integers(0, 50, n)
+        A.pages_fork(params(A, c), pages, ints(parents), drop=ints(drop))
         c.fork(parents, drop)
         same(c, pages)
 
@@ -296,6 +345,29 @@ def test_keep_many_heads(A):
     c = cache(r, 700, 2, 64, 32, r.integers(0, 70, 1400), spare=2100)
     pages = upload(A, c)
     keep(A, c, pages, [np.sort(r.choice(n, int(r.integers(0, n + 1)), replace=False)) for n in c.lengths])
+
+
+@pytest.mark.parametrize("n,spare", [(64, 300), (64, 2500), (65, 300)])
+def test_keep_plans(A, n, spare):
+    """256 heads and more; a beginning of whole pages, of one page, of all but the last rows, and none."""
+    r = np.random.default_rng(n + spare)
+    c = cache(r, n, 4, 64, 32, r.integers(0, 300, n * 4), spare=spare)
+    pages = upload(A, c)
+    for _ in range(2):
+        kept = []
+        for g, m in enumerate(c.lengths):
+            first = [min(m, 32), min(m, 128), max(m - 5, 0), 0][g % 4]
+            rest = np.arange(first, m) if g % 4 == 2 else np.sort(r.choice(np.arange(first, m), (m - first) // 2, replace=False))
+            kept.append(np.concatenate([np.arange(first), rest[:len(rest) - g % 2]]))
+        keep(A, c, pages, kept)
+
+
+def test_keep_of_long_heads(A):
+    r = np.random.default_rng(14)
+    c = cache(r, 2, 2, 64, 32, [3000, 2049, 2500, 64], spare=300)
+    pages = upload(A, c)
+    first = [1024, 0, 2400, 32]
+    keep(A, c, pages, [np.concatenate([np.arange(f), np.sort(r.choice(np.arange(f, n), (n - f) // 2, replace=False))]) for f, n in zip(first, c.lengths)])
 
 
 def test_keep_cuts_indices(A):

@@ -8,7 +8,7 @@ from test_accumulated_code import private_bytes                                 
 from test_kernel_code import code_objects, named, pytestmark, resources             # noqa: F401 (fixtures)
 
 KERNELS = {"append_plan_kernel": 1, "append_plan_small_kernel<": 2, "append_rows_kernel<": 6, "read_kernel<": 6, "fork_take_kernel": 1,
-           "fork_give_kernel": 1, "fork_small_kernel": 1, "keep_plan_kernel": 1, "keep_move_kernel<": 3, "keep_table_kernel": 1,
+           "fork_give_kernel": 1, "fork_small_kernel<": 2, "keep_plan_kernel<": 2, "keep_move_kernel<": 3, "keep_table_kernel": 1,
            "keep_whole_kernel<": 3, "attend_kernel<": 18, "::join_kernel<": 3}
 
 
