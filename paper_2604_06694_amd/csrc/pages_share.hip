@@ -149,7 +149,7 @@ __global__ __launch_bounds__(THREADS) void keep_plan_kernel(PageView pv, const i
     __shared__ int sums[THREADS / 64 + 1];
     __shared__ int served_pages, lost;
     const int tid = threadIdx.x, P = pv.rows();
-    PageSearch<THREADS, THREADS == 256 ? 4 : 8> search(pv, pv.state[1]);
+    PageSearch<THREADS, kLooked<THREADS>> search(pv, pv.state[1]);
     if (tid == 0) served_pages = lost = 0;
     const int n_free = min(max(pv.state[0], 0), a.most);
     int running = 0;

@@ -71,7 +71,7 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(
     __shared__ int sums[kPlanThreads / 64 + 1];
     __shared__ int served_pages, lost, freed;
     const int tid = threadIdx.x, H = pv.H, heads = n_items * H;
-    PageSearch<kPlanThreads, 8> search(pv, pv.state[1]);
+    PageSearch<kPlanThreads, kLooked<kPlanThreads>> search(pv, pv.state[1]);
     if (tid == 0) served_pages = lost = freed = 0;
     for (int i = tid; i < n_items; i += kPlanThreads) a.bad[i] = 0;
     if (seqs) {
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(THREADS) void append_plan_small_kernel(
     const int state = pv.state[0];
     int x = mine ? (seqs ? seqs[item] : item) : -1;
     const int rows = mine ? rows_of(cu_b, cu_seq, H, tid, total_rows) : 0;
-    PageSearch<THREADS, THREADS == 256 ? 4 : 8> search(pv, pv.state[1]);
+    PageSearch<THREADS, kLooked<THREADS>> search(pv, pv.state[1]);
     if (tid == 0) want = lost = 0;
     if (mine) bad[item] = 0;
     if (seqs) {
