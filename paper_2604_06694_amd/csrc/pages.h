@@ -101,17 +101,18 @@ __device__ __forceinline__ int exclusive_sum(int x, int* sums, int& total) {
 // round's counts are loaded ahead (PageSearch), since where it begins is known before how many are wanted.
 template <int THREADS, int U>
 struct PageSearch {
-    int begin, page[U];
-    bool free[U];
+    int begin, page[U], refs[U];
 
     __device__ __forceinline__ void load(const PageView& pv, int base) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const long long i = (long long)base + ((threadIdx.x >> 6) * U + u) * 64 + (threadIdx.x & 63);
-            long long p = begin + i;
-            if (p >= pv.n_pages) p -= pv.n_pages;
-            page[u] = (int)min(p, (long long)pv.n_pages - 1);
-            free[u] = i < pv.n_pages && pv.refs[page[u]] == 0;
+            const unsigned n = pv.n_pages, i = base + ((threadIdx.x >> 6) * U + u) * 64 + (threadIdx.x & 63);      // (below 2^31 + THREADS * U)
+            const bool there = i < n;
+            unsigned p = begin + i;
+            p -= p >= n ? n : 0;
+            page[u] = there ? p : 0;
+            refs[u] = pv.refs[page[u]];
+            refs[u] = there ? refs[u] : 1;
         }
     }
     __device__ __forceinline__ PageSearch(const PageView& pv, int from) : begin(min(max(from, 0), pv.n_pages - 1)) { load(pv, 0); }
@@ -127,7 +128,7 @@ struct PageSearch {
             int mine = 0;
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                free_in[u] = __builtin_amdgcn_ballot_w64(free[u]);
+                free_in[u] = __builtin_amdgcn_ballot_w64(refs[u] == 0);
                 mine += __builtin_popcountll(free_in[u]);
             }
             __syncthreads();
@@ -142,8 +143,8 @@ struct PageSearch {
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int to = at + __builtin_popcountll(free_in[u] & ((1ull << lane) - 1));
-                if (free[u] && to < want) {
+                const int to = __builtin_amdgcn_mbcnt_hi((unsigned)(free_in[u] >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)free_in[u], at));
+                if (refs[u] == 0 && to < want) {
                     found[to] = page[u];
                     if (to == want - 1) sums[WAVES] = page[u];
                 }
