@@ -165,8 +165,8 @@ struct PageSearch {
 };
 
 // Pages of a thread in a round: rounds come one after the other, and what a round does for its pages is vector work of one CU. (192 heads
-// that get three pages by 256 threads 6.5, 7.1, 8.2, 13.3 us with 1, 2, 4, 16; 64 heads that get 4300 by 1024 12.0, 11.7, 16.7 with 1, 8, 16.)
-template <int THREADS> constexpr int kLooked = THREADS == 256 ? 2 : 8;
+// that get three pages by 256 threads 6.4 us with 1, 2 or 4, 64 heads that get 4300 by 1024 threads 9.7, 9.1, 9.6 with 4, 8, 16.)
+template <int THREADS> constexpr int kLooked = THREADS == 256 ? 4 : 8;
 
 inline size_t up256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }    // parts of a workspace begin at multiples of 256 bytes
 

@@ -164,7 +164,7 @@ __global__ __launch_bounds__(THREADS) void keep_plan_kernel(PageView pv, const i
                 job.rows = rows;
                 // Rows come in order, none twice: where row r is index r, the ones before are theirs, too. The first page and the
                 // last are asked together, for heads that keep a choice of their rows have no whole page, and heads that lose the
-                // last ones only such (64 heads of 8000 rows 14.9 -> 13.4 us, 16 of 30000 13.8 -> 11.9).
+                // last ones only such (64 heads of 8000 rows 9.6 -> 8.2 us).
                 const int32_t* mine = indices + begin;
                 const auto whole = [&](int pages) { return mine[pages * P - 1] == pages * P - 1; };
                 int lo = 0, hi = rows >> pv.log_p;
@@ -279,7 +279,7 @@ __global__ __launch_bounds__(kThreads) void keep_table_kernel(PageView pv, KeepS
 }
 
 // Both for heads whose tables hold kWholeRows rows at most, a workgroup each: the old entries wait in LDS, and no other workgroup reads
-// them. (16 heads of 1100 rows: 3.4 + 3.1 us by the two kernels, 5.7 by this one, 256 of 2000 16.7 + 5.2 and 17.0.)
+// them. (16 heads of 1100 rows: 3.5 + 3.2 us by the two kernels, 6.2 by this one, 256 of 2000 16.8 + 5.0 and 17.0.)
 constexpr long long kWholeRows = 2048;
 constexpr int kWholeThreads = 512;
 
@@ -349,6 +349,7 @@ hipError_t launch_pages_keep(const PageView& pv, const int32_t* indices, const i
                              int32_t* refused, void* workspace, hipStream_t s)
 {
     const KeepSpace a = keep_space(pv, total_rows, workspace, nullptr);
+    // (fewer waves meet sooner at the barriers: 16 heads of 1100 rows 3.5 us by 256 threads, 4.6 by 1024, 64 of 500 5.2, 6.2)
     if (pv.n_heads <= 256 && a.most <= 2048)
         hipLaunchKernelGGL(keep_plan_kernel<256>, dim3(1), dim3(256), 0, s, pv, indices, cu_budgets, (int)total_rows, a, refused);
     else

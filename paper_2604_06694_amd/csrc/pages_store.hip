@@ -163,7 +163,7 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(
 
 // The same for up to THREADS heads, one a thread, and up to kSmallSeqs sequences: what is a pass over the workspace there is a register
 // or LDS here, and the counts of the first pages that the search looks at are loaded beside the rest. What is left is the chain item ->
-// sequence -> length -> table -> refs and the barriers. (192 heads: 10.8 us by the kernel above, 5.9 so; 1000 heads: 16.9 and 13.3.)
+// sequence -> length -> table -> refs and the barriers. (192 heads: 7.2 us by the kernel above, 4.3 so; 1000 heads: 10.9 and 8.2.)
 constexpr int kSmallSeqs = 4096;
 
 template <int THREADS>
