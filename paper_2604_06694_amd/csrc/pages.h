@@ -1,5 +1,6 @@
 // The cache in 4 bits and in pages (audiokv_pages): where things lie, and how rows are rounded and read. A header of its own
-// because the limits and the walk over segments are checked on the host as well (tests/pages_check.cpp).
+// because the limits, the walk over segments and fork's second launch are checked on the host as well (tests/pages_check.cpp,
+// tests/pages_fork_check.cpp).
 //
 // A page holds P rows of one KV head: K's codes [P][D / 2], V's codes, K's scales [P][D / 32], V's scales. Rows of codes are 32 to
 // 128 bytes, so that sections begin at multiples of 16 bytes whatever P (a multiple of 32) is.
@@ -167,6 +168,36 @@ struct PageSearch {
 // Pages of a thread in a round: rounds come one after the other, and what a round does for its pages is vector work of one CU. (192 heads
 // that get three pages by 256 threads 6.4 us with 1, 2 or 4, 64 heads that get 4300 by 1024 threads 9.7, 9.1, 9.6 with 4, 8, 16.)
 template <int THREADS> constexpr int kLooked = THREADS == 256 ? 4 : 8;
+
+// What fork's first launch leaves for its second, in the workspace.
+struct ForkSpace {
+    int2* rows;             // [heads]: length before and after the call
+    int32_t* entries;       // [heads][width]: table after the call, as far as it is not what it was
+};
+
+// What one of a head's threads does in fork's second launch. On the host as well, because threads run in any order and one of them writes
+// the length (tests/pages_fork_check.cpp): the length before the call comes from the workspace. owner_goes(page): is the page free now?
+// Returns how many are.
+template <class OwnerGoes>
+__host__ __device__ __forceinline__ int fork_give(const PageView& pv, const ForkSpace& f, const int32_t* parents, int n_seqs, int head,
+                                                  int thread, int threads, OwnerGoes owner_goes) {
+    const int x = head / pv.H, parent = parents ? parents[x] : x;
+    const bool same = parent == x || (unsigned)parent >= (unsigned)n_seqs;      // no entry changes, some may go
+    const int was = f.rows[head].x, rows = f.rows[head].y;
+    const int had = pv.pages_of(was), has = pv.pages_of(rows), last = had > has ? had : has;
+    int32_t* mine = pv.table + (size_t)head * pv.width;
+    int freed = 0;
+    for (int j = thread; j < last; j += threads) {
+        const int now = j < has ? same ? mine[j] : f.entries[(size_t)head * pv.width + j] : -1;
+        if (j < had) {
+            const int page = mine[j];
+            if (page != now && pv.is_page(page)) freed += owner_goes(page);
+        }
+        if (j < has && !same) mine[j] = now;
+    }
+    if (rows != was && thread == 0) pv.lengths[head] = rows;
+    return freed;
+}
 
 inline size_t up256(size_t bytes) { return (bytes + 255) & ~(size_t)255; }    // parts of a workspace begin at multiples of 256 bytes
 

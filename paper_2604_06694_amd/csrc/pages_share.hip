@@ -2,8 +2,8 @@
 // No arithmetic: table entries and counts, and for keep the kept rows' bytes.
 //
 // fork is two launches over the table, because a sequence may take over pages of one whose own entries change in the same call: the
-// first lists every new entry in the workspace and counts the pages' new owners, the second takes away the old owners and writes the
-// table. A page is free when its last owner goes, which only the second launch can bring about, once for every page: what it adds to
+// first lists every new entry and every length in the workspace and counts the pages' new owners, the second takes away the old owners and
+// writes table and lengths (fork_give in pages.h). A page is free when its last owner goes, which only the second launch can bring about, once for every page: what it adds to
 // state[0] does not depend on the order. Entries that stay as they are touch no count (after a reorder of beams that share their
 // prompt nearly all do), which spares the atomics on pages that many sequences have.
 //
@@ -19,14 +19,10 @@ constexpr int kThreads = 256, kPlanThreads = 1024;
 
 // ---- fork --------------------------------------------------------------------------------------------------------------------------
 
-struct ForkSpace {
-    int32_t* rows;          // [heads]: length after the call
-    int32_t* entries;       // [heads][width]: table after the call, as far as it is not what it was
-};
 ForkSpace fork_space(const PageView& pv, void* workspace, size_t* bytes) {
     ForkSpace f;
-    f.rows = static_cast<int32_t*>(workspace);
-    const size_t at = up256((size_t)pv.n_heads * 4);
+    f.rows = static_cast<int2*>(workspace);
+    const size_t at = up256((size_t)pv.n_heads * sizeof(int2));
     f.entries = part_at<int32_t>(workspace, at);
     if (bytes) *bytes = at + up256((size_t)pv.n_heads * pv.width * 4);
     return f;
@@ -40,10 +36,10 @@ __global__ __launch_bounds__(kThreads) void fork_take_kernel(PageView pv, const 
     const int parent = parents ? parents[x] : x;
     const bool taken = (unsigned)parent < (unsigned)n_seqs;
     const int from = taken ? parent * pv.H + h : head;
-    const int rows = taken ? max(pv.length(from) - (drop ? max(drop[x], 0) : 0), 0) : 0;
-    if (threadIdx.x == 0) f.rows[head] = rows;
+    const int was = pv.length(head), rows = taken ? max(pv.length(from) - (drop ? max(drop[x], 0) : 0), 0) : 0;
+    if (threadIdx.x == 0) f.rows[head] = int2{was, rows};
     if (from == head) return;                              // its own pages, or none
-    const int had = pv.pages_of(pv.length(head)), has = pv.pages_of(rows);
+    const int had = pv.pages_of(was), has = pv.pages_of(rows);
     const int32_t *mine = pv.table + (size_t)head * pv.width, *theirs = pv.table + (size_t)from * pv.width;
     for (int j = threadIdx.x; j < has; j += kThreads) {
         const int page = theirs[j];
@@ -54,22 +50,7 @@ __global__ __launch_bounds__(kThreads) void fork_take_kernel(PageView pv, const 
 
 __global__ __launch_bounds__(kThreads) void fork_give_kernel(PageView pv, const int32_t* __restrict__ parents, int n_seqs, ForkSpace f)
 {
-    const int head = blockIdx.x, x = head / pv.H;
-    const int parent = parents ? parents[x] : x;
-    const bool same = parent == x || (unsigned)parent >= (unsigned)n_seqs;      // no entry changes, some may go
-    const int rows = f.rows[head], was = pv.length(head);
-    const int had = pv.pages_of(was), has = pv.pages_of(rows);
-    int32_t* mine = pv.table + (size_t)head * pv.width;
-    int freed = 0;
-    for (int j = threadIdx.x; j < max(had, has); j += kThreads) {
-        const int now = j < has ? same ? mine[j] : f.entries[(size_t)head * pv.width + j] : -1;
-        if (j < had) {
-            const int page = mine[j];
-            if (page != now && pv.is_page(page)) freed += atomicSub(&pv.refs[page], 1) == 1;
-        }
-        if (j < has && !same) mine[j] = now;
-    }
-    if (rows != was && threadIdx.x == 0) pv.lengths[head] = rows;
+    int freed = fork_give(pv, f, parents, n_seqs, blockIdx.x, threadIdx.x, kThreads, [&](int page) { return atomicSub(&pv.refs[page], 1) == 1; });
     freed = wave_incl(freed);
     if ((threadIdx.x & 63) == 63 && freed > 0) atomicAdd(&pv.state[0], freed);
 }
