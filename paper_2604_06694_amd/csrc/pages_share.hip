@@ -64,7 +64,8 @@ __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageView pv, c
                                                                   const int32_t* __restrict__ drop, int n_seqs)
 {
     const int entries = pv.n_heads * pv.width;
-    int rows[U], was[U], before[U], now[U];
+    int rows[U], was[U], mine[U], theirs[U];
+    bool goes[U], comes[U];          // its owner before the call, after it
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int e = min((int)threadIdx.x + u * kPlanThreads, entries - 1), head = e / pv.width, j = e - head * pv.width;
@@ -74,25 +75,25 @@ __global__ __launch_bounds__(kPlanThreads) void fork_small_kernel(PageView pv, c
         const int from = taken ? parent * pv.H + h : head;
         was[u] = pv.length(head);
         rows[u] = taken ? max(pv.length(from) - (drop ? max(drop[x], 0) : 0), 0) : 0;
-        const int mine = pv.table[e], theirs = pv.table[(size_t)from * pv.width + j];
-        before[u] = j < pv.pages_of(was[u]) ? mine : -1;
-        now[u] = j < pv.pages_of(rows[u]) ? theirs : -1;
+        mine[u] = pv.table[e];
+        theirs[u] = pv.table[(size_t)from * pv.width + j];
+        const bool had = j < pv.pages_of(was[u]), has = j < pv.pages_of(rows[u]), stays = had && has && mine[u] == theirs[u];
+        goes[u] = had && !stays && pv.is_page(mine[u]);
+        comes[u] = has && !stays;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
-        if ((int)threadIdx.x + u * kPlanThreads < entries && now[u] != before[u] && pv.is_page(now[u])) atomicAdd(&pv.refs[now[u]], 1);
+        if ((int)threadIdx.x + u * kPlanThreads < entries && comes[u] && pv.is_page(theirs[u])) atomicAdd(&pv.refs[theirs[u]], 1);
     __syncthreads();          // all new owners are counted, and all of the table is read
     int freed = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int e = threadIdx.x + u * kPlanThreads;
         if (e >= entries) break;
-        const int head = e / pv.width, j = e - head * pv.width;
-        if (now[u] != before[u]) {
-            if (pv.is_page(before[u])) freed += atomicSub(&pv.refs[before[u]], 1) == 1;
-            if (j < pv.pages_of(rows[u])) pv.table[e] = now[u];
-        }
-        if (j == 0 && rows[u] != was[u]) pv.lengths[head] = rows[u];
+        if (goes[u]) freed += atomicSub(&pv.refs[mine[u]], 1) == 1;
+        if (comes[u]) pv.table[e] = theirs[u];
+        const int head = e / pv.width;
+        if (e == head * pv.width && rows[u] != was[u]) pv.lengths[head] = rows[u];
     }
     freed = wave_incl(freed);
     if ((threadIdx.x & 63) == 63 && freed > 0) atomicAdd(&pv.state[0], freed);

@@ -34,3 +34,17 @@ def test_long_heads_grow_shrink_and_end(A, n, H, entries):
         c.fork(parents, drop)
         same(c, pages)
     assert c.free == c.n_pages
+
+
+@pytest.mark.parametrize("entries", [8, 600])
+def test_an_entry_that_is_no_page_is_taken_over(A, entries):
+    """-1, and numbers beyond the pool, among a parent's entries: the child's are the same, and not what stood there before."""
+    r = np.random.default_rng(entries)
+    c = cache(r, 4, 1, 64, 32, [200, 70, 40, 0], max_pages=entries)
+    pages = upload(A, c)
+    for n in (-1, c.n_pages, 2**31 - 1, -2**31):
+        pages.table[0, 3] = n
+        A.pages_fork(params(A, c), pages, ints([0, 0, -1, 0]))
+        assert pages.table[1, :7].tolist() == pages.table[3, :7].tolist() == pages.table[0, :7].tolist()
+        A.pages_fork(params(A, c), pages, ints([0, -1, -1, -1]))
+        pages.table[1:, 3] = int(pages.table[0, 0])               # what stands behind a head's rows has no meaning
