@@ -466,7 +466,8 @@ int32_t audiokv_evict_accumulated(const audiokv_params* params, const audiokv_sl
  * lengths, refs and state[1] zero and state[0] = n_pages is an empty cache. All pointers
  * are device memory. The calls below keep the numbers in step; none of them looks
  * for numbers that are not (a page number outside the pool is never followed, a length
- * beyond a table row is cut). "Sequences" may be (sequence, layer) pairs.
+ * beyond a table row is cut, and where state[0] promises more pages than are free, heads
+ * are served with those that are). "Sequences" may be (sequence, layer) pairs.
  * Calls that change a cache (append, fork, keep) must be ordered after each other and
  * after and before others on it, by a stream or events. n_seqs * n_kv_heads <= 2^20,
  * and n_seqs * n_kv_heads * max_pages * page_rows / 32 < 2^31. */

@@ -118,8 +118,9 @@ struct PageSearch {
     }
     __device__ __forceinline__ PageSearch(const PageView& pv, int from) : begin(min(max(from, 0), pv.n_pages - 1)) { load(pv, 0); }
 
-    // The first `want` free pages, in the order in which they are looked at, to found[]. Returns how many there were, and in `next`
-    // where the following search begins. sums: THREADS / 64 + 1 ints of LDS. (A barrier before the first and after the last use of LDS.)
+    // The first `want` free pages, in the order in which they are looked at, to found[]. Returns how many there were, `want` at most, and
+    // in `next` where the following search begins. Fewer than `want`: the state said that there were more; the caller wants that many
+    // then, and calls again. sums: THREADS / 64 + 1 ints of LDS. (A barrier before the first and after the last use of LDS.)
     __device__ int find(const PageView& pv, int want, int32_t* __restrict__ found, int* sums, int& next) {
         constexpr int WAVES = THREADS / 64;
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -158,9 +159,8 @@ struct PageSearch {
         }
         __syncthreads();
         next = begin;
-        // (fewer than wanted: the state said that there were more. The next search begins where this one did)
         if (want > 0 && have >= want) next = sums[WAVES] + 1 == pv.n_pages ? 0 : sums[WAVES] + 1;
-        for (int i = have + threadIdx.x; i < want; i += THREADS) found[i] = -1;
+        if (have < want) load(pv, 0);
         return min(have, want);
     }
 };

@@ -177,9 +177,26 @@ __global__ __launch_bounds__(THREADS) void keep_plan_kernel(PageView pv, const i
         if (head < pv.n_heads) a.jobs[head] = job;
     }
     __syncthreads();
-    const int want = served_pages;
-    int next;
-    const int have = search.find(pv, want, a.found, sums, next);
+    int next, have;
+    for (;;) {
+        const int want = served_pages;
+        have = search.find(pv, want, a.found, sums, next);
+        if (have == want) break;
+        if (tid == 0) served_pages = 0;      // (the state promised more)
+        __syncthreads();
+        for (int head = tid; head < pv.n_heads; head += THREADS) {
+            const KeepJob job = a.jobs[head];
+            const int end = job.first + (job.rows < 0 ? 0 : pv.pages_of(job.rows) - job.same);
+            if (job.rows < 0 || end == job.first) continue;
+            if (end <= have) {
+                atomicMax(&served_pages, end);
+            } else {
+                a.jobs[head].rows = -1;
+                atomicAdd(&lost, 1);
+            }
+        }
+        __syncthreads();
+    }
     __syncthreads();
     if (tid == 0) {
         pv.state[0] -= have;

@@ -126,18 +126,24 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(
     }
     __syncthreads();
     // Items are served while the free pages last: the ends of their pages do not fall.
-    const int n_free = min(max(pv.state[0], 0), a.most);
+    int n_free = min(max(pv.state[0], 0), a.most);
     auto end_of = [&](int item) { return item + 1 < n_items ? a.jobs[(item + 1) * H].first : running; };
     auto served = [&](int item) {
         const int end = end_of(item);
         return !a.bad[item] && (end <= n_free || end == a.jobs[item * H].first);
     };
-    for (int i = tid; i < n_items; i += kPlanThreads)
-        if (end_of(i) <= n_free) atomicMax(&served_pages, end_of(i));
-    __syncthreads();
-    const int want = served_pages;
-    int next;
-    const int have = search.find(pv, want, a.found, sums, next);
+    int next, have;
+    for (;;) {
+        for (int i = tid; i < n_items; i += kPlanThreads)
+            if (end_of(i) <= n_free) atomicMax(&served_pages, end_of(i));
+        __syncthreads();
+        const int want = served_pages;
+        have = search.find(pv, want, a.found, sums, next);
+        if (have == want) break;
+        n_free = have;                       // (the state promised more)
+        if (tid == 0) served_pages = 0;
+        __syncthreads();
+    }
     // lengths, and what shared pages lose: after the search, so that a page which is still to be copied is not handed out
     __syncthreads();
     for (int g = tid; g < heads; g += kPlanThreads) {
@@ -171,7 +177,7 @@ __global__ __launch_bounds__(THREADS) void append_plan_small_kernel(
     PageView pv, const int32_t* __restrict__ cu_b, const int32_t* __restrict__ cu_seq, const int32_t* __restrict__ seqs, int n_items,
     int n_seqs, int total_rows, AppendSpace a, int32_t* __restrict__ refused)
 {
-    __shared__ int sums[THREADS / 64 + 1], begins[THREADS + 1], bad[THREADS], owner[kSmallSeqs];
+    __shared__ int sums[THREADS / 64 + 1], begins[THREADS], bad[THREADS], owner[kSmallSeqs];
     __shared__ int want, lost;
     const int tid = threadIdx.x, H = pv.H, heads = n_items * H;
     const bool mine = tid < heads;
@@ -219,17 +225,23 @@ __global__ __launch_bounds__(THREADS) void append_plan_small_kernel(
     int total;
     job.first = exclusive_sum<THREADS>(fits ? need : 0, sums, total);
     begins[tid] = job.first;
-    if (tid == 0) begins[THREADS] = total;
     __syncthreads();
     // Items are served while the free pages last: the ends of their pages do not fall.
-    const int n_free = min(max(state, 0), a.most);
+    int n_free = min(max(state, 0), a.most), next, have;
     const int last = (item + 1) * H, end = last < THREADS ? begins[last] : total;
-    const bool served = fits && (end <= n_free || end == begins[item * H]);
-    if (served && need > 0) atomicMax(&want, end);
-    if (asks && !served) atomicAdd(&lost, 1);
-    __syncthreads();
-    int next;
-    const int have = search.find(pv, want, a.found, sums, next);
+    bool served;
+    for (;;) {
+        served = fits && (end <= n_free || end == begins[item * H]);
+        if (served && need > 0) atomicMax(&want, end);
+        if (asks && !served) atomicAdd(&lost, 1);
+        __syncthreads();
+        const int wanted = want;
+        have = search.find(pv, wanted, a.found, sums, next);
+        if (have == wanted) break;
+        n_free = have;                       // (the state promised more)
+        if (tid == 0) want = lost = 0;
+        __syncthreads();
+    }
     if (asks && served) {
         job.rows = rows;
         pv.lengths[head] = job.start + rows;
