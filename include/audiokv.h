@@ -523,7 +523,10 @@ int32_t audiokv_pages_append(const audiokv_params* params, const audiokv_pages* 
  * softmax's denominator (two parts of a cache are joined by it). A query without rows,
  * or whose logits are all -infinity, gives zeros and -infinity. Products, statistics and
  * sums are fp32; for its product with V a weight is taken to 2^-16 of it, and out is
- * bf16. n_q_heads / n_kv_heads <= 16. The pages may be read by several calls at once. */
+ * bf16. Finite values have a finite mean: where the sums over 2^n rows might overflow
+ * (V of 2^(117 - n) and more), weights are taken up to 2^n smaller, and what is below
+ * fp32's normal numbers then may count as zero. n_q_heads / n_kv_heads <= 16. The pages
+ * may be read by several calls at once. */
 int32_t audiokv_pages_attend_workspace_bytes(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs,
                                              size_t* out_bytes);
 int32_t audiokv_pages_attend(const audiokv_params* params, const audiokv_pages* pages, int32_t n_seqs, const void* q_dev,

@@ -14,11 +14,11 @@
 //                               its scale one byte, and the conversion to bf16 is exact (a magnitude of e2m1 has two bits)
 //   O[channel][query] += V^T P  the lane's C, keys 4 r .. 4 r + 3 of two tiles, is its column of P as it is: the product runs over keys in
 //                               that order, and V's rows are loaded so
-// The running reference of the softmax moves only where a logit exceeds it by 2^8: a wave-wide test per unit instead of a maximum over
-// lanes and a rescaling. P goes to the second product as two bf16 numbers (16 bits of it), V in bf16 is exact. Up to eight query heads
-// (PAIRS) columns c and c + 8 hold the same query, and the two numbers of P are one in each: half the instructions of the second product,
-// whose halves are added in the end. (The matrix cores' products of 4-bit keys as they are, with queries in 8 bits, are no choice: their
-// sums are off by 2^-13 of the sum of magnitudes, those of bf16 by less than 2^-23.)
+// The running reference of the softmax moves only where a logit exceeds it by 2^8, or V's scales say that a sum might overflow: a wave-wide
+// test per unit instead of a maximum over lanes and a rescaling. P goes to the second product as two bf16 numbers (16 bits of it), V in
+// bf16 is exact. Up to eight query heads (PAIRS) columns c and c + 8 hold the same query, and the two numbers of P are one in each: half
+// the instructions of the second product, whose halves are added in the end. (The matrix cores' products of 4-bit keys as they are, with
+// queries in 8 bits, are no choice: their sums are off by 2^-13 of the sum of magnitudes, those of bf16 by less than 2^-23.)
 #include "pages.h"
 
 #include <algorithm>
@@ -34,6 +34,11 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
 
 constexpr size_t kStreamBytes = 256u << 20;       // of a pool: what the memory-side cache holds
 constexpr float kSlack = 8.f;       // octaves that a logit may lie above the reference
+
+// What the reference has to do with V. A head of 2^n rows or fewer sums up that many terms, a weight times a value of V each, which is
+// 6 * 2^e at most at a scale 2^e. That stays below 0.75 * 2^128 where weights are 2^kSlack at most and e is up to 117 - n; beyond it the
+// reference moves to the unit's largest logit, and to e + n - 125 octaves above it where that is positive (31 at most).
+constexpr int kAnyWeight = 117;
 
 struct AttendSpace {
     int4* joins;            // [the fewer of heads and workgroups]: head, slot of its first part, parts (0: nothing to join)
@@ -152,6 +157,14 @@ __device__ __forceinline__ unsigned pack_bf16(float a, float b) {             //
     return __builtin_bit_cast(unsigned, x);
 }
 
+// Of three scales as exponent_of leaves them. (In asm: fmaxf makes two instructions of one, to quiet a NaN first. A scale that says NaN hides
+// the others of its lane here; the lane's channels are NaN whatever they are.)
+__device__ __forceinline__ float max_magnitude(float a, float b, float c) {
+    float m;
+    asm("v_max3_f32 %0, |%1|, |%2|, |%3|" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+}
+
 // What a wave knows of a head so far. Column c = lane & 15 is a query; `sum` is the lane's share of it.
 template <int D> struct Running {
     f32x4 out[D / 16];      // out[ct][i]: channel (4 r + i) * D / 16 + ct
@@ -159,7 +172,7 @@ template <int D> struct Running {
 };
 
 template <int D, bool PAIRS>
-__device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, const bf16x8 (&q)[D / 32], float c_log2, int rows) {
+__device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, const bf16x8 (&q)[D / 32], float c_log2, int rows, int log_rows) {
     const int lane = threadIdx.x & 63, c = lane & 15, r = lane >> 4;
     f32x4 z[2];                                            // products, keys 4 r + i of either tile
 #pragma unroll
@@ -186,9 +199,17 @@ __device__ __forceinline__ void add_unit(Running<D>& o, const Rows32<D>& u, cons
         }
     }
     float top = fmaxf(fmaxf(fmaxf(z[0][0], z[0][1]), fmaxf(z[0][2], z[0][3])), fmaxf(fmaxf(z[1][0], z[1][1]), fmaxf(z[1][2], z[1][3]))) * c_log2;
-    if (__builtin_amdgcn_ballot_w64(top > o.ref + kSlack) != 0) {
+    const float large = max_magnitude(max_magnitude(max_magnitude(max_magnitude(vs[0], vs[1], vs[2]), vs[3], vs[4]), vs[5], vs[6]), vs[7], vs[7]);
+    const unsigned long long largest = __builtin_amdgcn_ballot_w64(large >= __uint_as_float((unsigned)(127 + kAnyWeight + 1 - log_rows) << 23));
+    if ((__builtin_amdgcn_ballot_w64(top > o.ref + kSlack) | largest) != 0) {
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
+        if (largest != 0) {
+            float all = large;
+#pragma unroll
+            for (int m = 32; m > 0; m >>= 1) all = fmaxf(all, __shfl_xor(all, m, 64));
+            top += (float)max((int)(__float_as_uint(all) >> 23) - 127 + log_rows - (kAnyWeight + 8), 0);
+        }
         const float ref = fmaxf(o.ref, top);
         const float shrink = o.ref == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(o.ref - ref);
         o.ref = ref;
@@ -340,7 +361,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kRes
     }
 
     for (int u = u0; u < u1;) {
-        const int units = units_of(rows);
+        const int units = units_of(rows), log_rows = rows > 1 ? 32 - __builtin_clz(rows - 1) : 0;
         const int from = u - start, to = min(units, u1 - start);           // units of this head
         const int x = head / g.H_kv, h = head - x * g.H_kv;
         const int32_t* table = pv.table + (size_t)head * pv.width;
@@ -365,7 +386,7 @@ __global__ __launch_bounds__(64 * WAVES) __attribute__((amdgpu_waves_per_eu(kRes
                 load_unit<D, STREAM>(unit, pv, offsets, pv.is_page(page) ? page : 0, (min(i, last) & ((1 << log_u) - 1)) * kUnit);
             };
             auto add = [&](const Rows32<D>& unit, int i, int page) {       // (rows of no page take no part)
-                add_unit<D, PAIRS>(o, unit, qf, g.c_log2, pv.is_page(page) ? min(kUnit, rows - i * kUnit) : 0);
+                add_unit<D, PAIRS>(o, unit, qf, g.c_log2, pv.is_page(page) ? min(kUnit, rows - i * kUnit) : 0, log_rows);
             };
             Rows32<D> a0, a1;
             int i = from + wave, p0 = page_of(i), p1 = page_of(i + WAVES);
