@@ -142,6 +142,7 @@ class Slots:
 
 
 _PAGES_SIZE = C.sizeof(_CPages)
+_MOST = 2**31 - 1                          # (entries of a table: the C struct's sizes have 32 bits, and ctypes would drop the rest)
 _U8 = torch.uint8
 
 
@@ -175,19 +176,21 @@ class Pages:
         pool, table, lengths, refs, state = self.pool, self.table, self.lengths, self.refs, self.state
         heads, n_pages, size = lengths.numel(), refs.numel(), table.shape
         need = n_pages * self.page_rows * p.head_dim * 17 // 16
-        if (heads % p.n_kv_heads or len(size) != 2 or size[0] != heads or state.numel() != 2 or pool.numel() < need or pool.dtype is not _U8
-                or not (table.dtype is lengths.dtype is refs.dtype is state.dtype is _I32)
+        if (heads % p.n_kv_heads or len(size) != 2 or size[0] != heads or table.numel() > _MOST or state.numel() != 2
+                or pool.numel() < need or pool.dtype is not _U8 or not (table.dtype is lengths.dtype is refs.dtype is state.dtype is _I32)
                 or not (pool.get_device() == table.get_device() == lengths.get_device() == refs.get_device() == state.get_device() == at)
                 or not (pool.is_contiguous() and table.is_contiguous() and lengths.is_contiguous() and refs.is_contiguous()
                         and state.is_contiguous())):
-            raise ValueError(f"pages: lengths must be one value for each of {p.n_kv_heads} KV heads of every sequence, table [{heads}, entries], "
-                             f"state two values, refs one value per page, all {_I32}, and pool {need} values of {_U8}: contiguous tensors on "
-                             f"the current device, {at}")
+            raise ValueError(f"pages: lengths must be one value for each of {p.n_kv_heads} KV heads of every sequence, table [{heads}, entries] "
+                             f"of less than 2^31 values, state two values, refs one value per page, all {_I32}, and pool {need} values of "
+                             f"{_U8}: contiguous tensors on the current device, {at}")
         return _CPages(_PAGES_SIZE, self.page_rows, n_pages, size[1], pool.data_ptr(), table.data_ptr(), lengths.data_ptr(),
                        refs.data_ptr(), state.data_ptr())
 
     def _sizes(self) -> _CPages:
         """The C struct of a size query, which looks at no pointer."""
+        if self.table.numel() > _MOST:
+            raise ValueError("pages: table must have less than 2^31 values")
         return _CPages(_PAGES_SIZE, self.page_rows, self.refs.numel(), self.table.shape[1], None, None, None, None, None)
 
 
