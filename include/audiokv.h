@@ -467,7 +467,10 @@ int32_t audiokv_evict_accumulated(const audiokv_params* params, const audiokv_sl
  * are device memory. The calls below keep the numbers in step; none of them looks
  * for numbers that are not (a page number outside the pool is never followed, a length
  * beyond a table row is cut, and where state[0] promises more pages than are free, heads
- * are served with those that are). "Sequences" may be (sequence, layer) pairs.
+ * are served with those that are). "Sequences" may be (sequence, layer) pairs; and
+ * caches may share pool, refs and state, such as the layers of a model with a slice
+ * of one table and of one list of lengths each: a call works on its slice, in which
+ * sequences are numbered from 0, and calls on any of them are ordered like calls on one.
  * Calls that change a cache (append, fork, keep) must be ordered after each other and
  * after and before others on it, by a stream or events. n_seqs * n_kv_heads <= 2^20,
  * and n_seqs * n_kv_heads * max_pages * page_rows / 32 < 2^31. */

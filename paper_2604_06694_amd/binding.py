@@ -148,7 +148,8 @@ _U8 = torch.uint8
 
 @dataclass
 class Pages:
-    """A cache in 4 bits and in pages: device tensors, see audiokv_pages. `empty` makes one."""
+    """A cache in 4 bits and in pages: device tensors, see audiokv_pages. `empty` makes one. A layer or a sequence of it is one, too, with slices of
+    table and lengths and the same pool, refs and state."""
     pool: torch.Tensor                       # uint8, n_pages * page_bytes
     table: torch.Tensor                      # int32 [n_seqs * n_kv_heads, max_pages]
     lengths: torch.Tensor                    # int32 [n_seqs * n_kv_heads]
