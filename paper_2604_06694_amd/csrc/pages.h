@@ -165,8 +165,10 @@ struct PageSearch {
     }
 };
 
-// Pages of a thread in a round: rounds come one after the other, and what a round does for its pages is vector work of one CU. (192 heads
-// that get three pages by 256 threads 6.4 us with 1, 2 or 4, 64 heads that get 4300 by 1024 threads 9.7, 9.1, 9.6 with 4, 8, 16.)
+// Pages of a thread in a round: rounds come one after the other, and what a round does for its pages is vector work of one CU. Kernel times
+// with 1, 2, 4 and 8 pages a thread of 256: 192 heads that get three pages 4.0, 4.0, 4.2, 4.4 us, the same in a pool of 8000 with 100 free
+// ones behind the rest 17.3, 12.1, 8.9, 7.3, a keep of 112 heads 7.9, 6.7, 6.2, 6.4. With 4, 8 and 16 a thread of 1024: 64 heads that get
+// 4300 pages 10.0, 8.9, 9.6, 112 heads that get 5800 7.3, 7.1, 9.1.
 template <int THREADS> constexpr int kLooked = THREADS == 256 ? 4 : 8;
 
 // What fork's first launch leaves for its second, in the workspace.

@@ -9,7 +9,7 @@
 // a head goes to the workspace (at most two parts a workgroup, its first and its last) and a second launch joins it. No atomics;
 // every sum has a fixed order.
 //
-// A wave takes every fourth unit. Both products are 16 x 16 x 32 on the matrix cores, with the query heads as columns, padded to 16:
+// The waves of a workgroup take its units in turn. Both products are 16 x 16 x 32 on the matrix cores, with the query heads as columns, padded to 16:
 //   C[key][query] = K Q^T       lane (c = lane & 15, r = lane >> 4) holds row c of K, channels of scale block r: its codes are one load,
 //                               its scale one byte, and the conversion to bf16 is exact (a magnitude of e2m1 has two bits)
 //   O[channel][query] += V^T P  the lane's C, keys 4 r .. 4 r + 3 of two tiles, is its column of P as it is: the product runs over keys in
@@ -32,7 +32,9 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4_t;
 
-constexpr size_t kStreamBytes = 256u << 20;       // of a pool: what the memory-side cache holds
+// Bytes of a pool: what the memory-side cache holds. How much of a larger pool is in use is not known here; where it is little and read again
+// and again, streaming costs (a pool of 2 GB, with and without: 9 MB in use 11.8, 11.5 us, 35 MB 16.2, 15.5, 104 MB 26.9, 26.1, 226 MB 42.9, 41.8).
+constexpr size_t kStreamBytes = 256u << 20;
 constexpr float kSlack = 8.f;       // octaves that a logit may lie above the reference
 
 // What the reference has to do with V. A head of 2^n rows or fewer sums up that many terms, a weight times a value of V each, which is
@@ -559,7 +561,7 @@ template <int D> constexpr int kWholeWaves = 4 * kResident<D>;
 // Short heads go to a workgroup each, of as many waves as a CU holds, and there is no second launch. By what a table can hold, since
 // lengths are not known here. Kernel times of whole heads, and in parts with the join: 4 heads of 500 rows 6.8, 9.3 us, of 2000 12.2, 11.5
 // (and the host launches once, some 3 us less), 64 of 2000 13.2, 13.5, 256 of 500 8.1, 15.2, 256 of 2000 16.1, 22.3, 512 of 500 14.8, 20,
-// 1792 of 500 47.7, 38; at D = 256, where a CU holds eight waves, 16 of 500 11.1, 10.6, of 1000 14.3, 11.5, but 256 of 1500 21.6, 26.3.
+// 1792 of 500 47.7, 38 (so a head of 900 rows in a table for 32768 takes 11.7 us with the binding, in one for 1024 8.9); at D = 256, where a CU holds eight waves, 16 of 500 11.1, 10.6, of 1000 14.3, 11.5, but 256 of 1500 21.6, 26.3.
 bool whole_heads(const PageView& pv) {
     const long long rows = (long long)pv.width << pv.log_p;
     return pv.n_heads <= 512 && rows <= (pv.D < 256 || pv.n_heads >= 128 ? 2048 : 512);

@@ -169,7 +169,8 @@ __global__ __launch_bounds__(kPlanThreads) void append_plan_kernel(
 
 // The same for up to THREADS heads, one a thread, and up to kSmallSeqs sequences: what is a pass over the workspace there is a register
 // or LDS here, and the counts of the first pages that the search looks at are loaded beside the rest. What is left is the chain item ->
-// sequence -> length -> table -> refs and the barriers. (192 heads: 7.2 us by the kernel above, 4.3 so; 1000 heads: 10.9 and 8.2.)
+// sequence -> length -> table -> refs and the barriers. (192 heads by the kernel above and so: 7.4 and 3.2 us where none needs a page, 8.9 and
+// 6.3 where many do and some copy; 1000 heads 9.5 and 5.5 where none needs one, 9.5 and 8.8 where each does.)
 constexpr int kSmallSeqs = 4096;
 
 template <int THREADS>
@@ -285,7 +286,6 @@ template <bool STREAM> __device__ __forceinline__ u32x4 row_piece(const __bf16* 
     return STREAM ? __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)) : *reinterpret_cast<const u32x4*>(p);
 }
 
-// Workgroups up to `copies_at` take consecutive rows, D / 8 lanes a row; those behind copy the shared page of a head each.
 // The scale bytes of 16 lanes' blocks (8 lanes': D = 64) in one word, the first block lowest, in all of them.
 template <int D> __device__ __forceinline__ unsigned scales_of_row(int scale, int lane) {
     int w = scale << (lane / 4 % (D == 64 ? 2 : 4) * 8);
@@ -294,6 +294,7 @@ template <int D> __device__ __forceinline__ unsigned scales_of_row(int scale, in
     return (unsigned)w;
 }
 
+// Workgroups up to `copies_at` take consecutive rows, D / 8 lanes a row; those behind copy the shared page of a head each.
 template <int D, int R, bool STREAM>
 __global__ __launch_bounds__(kThreads) void append_rows_kernel(
     Geom g, PageView pv, const __bf16* __restrict__ k, const __bf16* __restrict__ v, const int32_t* __restrict__ indices,
